@@ -537,6 +537,165 @@ pw_status pw_planner_step_layer(pw_planner* p, const pw_layer* layer, int free_b
                                 uint64_t kv_block_bytes, pw_plan_summary* out);
 pw_status pw_planner_apply(pw_planner* p, pw_layer* layer, void* side_stream, size_t* delta_total);
 
+/* ---- A decoder layer's operators around its experts ------------------------
+ * What a serving step runs besides the paged experts: the norms, 8-bit
+ * projections, the KV cache that the freed pages make room for with the
+ * attention that reads it, and the routers of group-limited layers. They need
+ * no layer handle, keep nothing from call to call and allocate nothing; rules
+ * for streams and errors are those above. No call reads device data on the
+ * host, so all of them can be captured into a graph. Element strides are in
+ * elements.
+ *
+ * 8-bit values are OCP e4m3 (no infinity; 0x7F and 0xFF are NaN). The codes of
+ * a group of values v are e4m3(v / s) (nearest, ties to even) with the fp32
+ * scale s = max(amax |v| / 448, 2^-126). A group that holds an infinity has s
+ * infinite; a NaN stays a NaN in its own place.                              */
+
+/* Element types of the calls below, beside pw_dtype's. */
+enum { PW_F32 = 2 };
+
+/* Root-mean-square norm with the residual's addition. Per row:
+ *   z = x + residual (fp32; residual NULL: z = x)
+ *   y = z * rsqrt(mean(z^2) + eps) * weight (weight NULL: 1), in fp32
+ * and, each where its pointer is not NULL,
+ *   sum_out [T,H] act   z, rounded once (may be x's or residual's own buffer)
+ *   y16     [T,H] act   y, rounded once (may be x's own buffer)
+ *   y8      [T,H] e4m3  codes of y in groups of 128 columns, with their scales
+ *   y8_scale [T,H/128] fp32 (both or neither).
+ * The norm is taken of z before it is rounded.
+ *   act: PW_F16 or PW_BF16 (x, residual, weight, sum_out, y16).
+ *   ldx, ldr: row strides of x and residual, at least H and multiples of 8;
+ *   the outputs' rows are packed.
+ * Constraints: 1 <= H <= 32768, a multiple of 8, and of 128 with y8; eps >= 0
+ * and finite; 16-byte aligned rows; an output to write (PW_EINVAL otherwise).
+ * T = 0 does nothing.                                                        */
+pw_status pw_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                      int T, int H, float eps, int act, void* sum_out, void* y16, void* y8, float* y8_scale,
+                      void* stream);
+
+/* Product of 8-bit matrices with block scales:
+ *   y[m,n] = sum over 128-blocks b of K: a_scale[m,b] w_scale[n / 128, b] *
+ *            sum of a[m,k] w[n,k] over the block,
+ * accumulated in fp32 and rounded once.
+ *   a [M,K] e4m3, row stride lda; a_scale [M, K/128] fp32, packed (as
+ *   pw_rms_norm writes them); w [N,K] e4m3, row stride ldw; w_scale
+ *   [ceil(N/128), K/128] fp32, packed; y [M,N] of y_type (PW_F16, PW_BF16 or
+ *   PW_F32), row stride ldy >= N.
+ * Constraints: K a positive multiple of 128; N >= 1; lda, ldw >= K, multiples
+ * of 16; a and w 16-byte aligned; y aligned to its elements; one row's and one
+ * tile's offsets stay below 2^31 bytes: lda, ldw <= 2^22 (PW_EINVAL otherwise).
+ * ws: device workspace of at least pw_gemm_fp8_workspace bytes, 16-byte aligned
+ * (PW_ENOMEM below; may be NULL where that is 0), in use until `stream` passes
+ * the call. M = 0 does nothing. Deterministic: a fixed order of summation.       */
+pw_status pw_gemm_fp8_workspace(int M, int N, int K, size_t* ws_bytes);
+pw_status pw_gemm_fp8(const void* a, int64_t lda, const float* a_scale, const void* w, int64_t ldw,
+                      const float* w_scale, int M, int N, int K, void* y, int64_t ldy, int y_type, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/* A paged KV cache of one attention layer: n_blocks blocks of block_tokens
+ * tokens in caller-owned device memory, block i at pool + i * block_stride. A
+ * stride of 256 makes the block numbers offsets in units of 256 bytes, so that
+ * blocks may lie anywhere in a larger pool (slots that a downshift freed).
+ *
+ * Inside a block, per key head h: the keys, then the values, block_tokens *
+ * head_dim elements each; after the last head, for 8-bit caches, the keys'
+ * scales [n_kv_heads][block_tokens] and the values' scales, fp32. Tokens t and
+ * channels d lie in the order in which the attention's matrix instructions take
+ * them (a wave's load is 1 KB of contiguous memory, and no value is moved
+ * between lanes):
+ *   keys, 16 bits: tile (t/16, d/32) of 1024 bytes at index (t/16) (D/32) +
+ *     d/32; lane l = 16 (d/8 mod 4) + t mod 16; byte 16 l + 2 (d mod 8).
+ *   keys, 8 bits: tile (t/16, d/64); lane as above; byte 16 l + 8 (d/32 mod 2)
+ *     + d mod 8.
+ *   values, 16 bits: tile (t/32, d/16) of 1024 bytes at index (t/32) (D/16) +
+ *     d/16; lane l = 16 (t/4 mod 4) + d mod 16; element 4 (t/16 mod 2) + t mod
+ *     4 of the lane's eight.
+ *   values, 8 bits: tile (t/32, d/32); lane as above; byte 16 l + 8 (d/16 mod
+ *     2) + 4 (t/16 mod 2) + t mod 4.
+ * In 8-bit caches a group of codes is one token's key (or value) of one head.
+ *
+ * Constraints (PW_EINVAL otherwise): head_dim 64, 128, 192 or 256;
+ * block_tokens 32, 64, 128 or 256; 1 <= n_kv_heads <= 1024; act PW_F16 or
+ * PW_BF16; bits 16 or 8; 1 <= n_blocks; block_stride a positive multiple of
+ * 256 below 2^40; pool 256-byte aligned.                                     */
+typedef struct {
+    void* pool;
+    int64_t block_stride;  /* bytes from one block to the next                 */
+    int n_blocks;          /* block numbers are 0 .. n_blocks - 1              */
+    int block_tokens;
+    int n_kv_heads, head_dim;
+    int act;               /* type of queries, new keys and values, outputs    */
+    int bits;              /* 16: cached in act; 8: e4m3 codes with scales     */
+} pw_kv_cache;
+
+/* Bytes of one block (pool and n_blocks are not looked at). */
+pw_status pw_kv_block_bytes(const pw_kv_cache* cache, size_t* bytes);
+
+/* Write T tokens' keys and values into the cache. k and v: act, element (t, h,
+ * d) at t * ld + h * ldh + d (ld, ldh multiples of 8, 16-byte aligned).
+ * slots [T] int64 device: block number * block_tokens + position in the block;
+ * a slot that is negative or past the last block writes nothing. Two tokens of
+ * one call in one slot: undefined which one stays. Other slots of a block are
+ * not touched.                                                               */
+pw_status pw_kv_append(const pw_kv_cache* cache, const void* k, const void* v, int64_t ld, int64_t ldh,
+                       const int64_t* slots, int T, void* stream);
+
+/* Attention of one new token per sequence over its cached keys and values (the
+ * new token's own are appended first):
+ *   out[b,h] = sum_t softmax_t(scale * q[b,h] . k_t) v_t over the positions
+ *   max(0, len - window) <= t < len, len = seq_lens[b]; window 0: all. Query
+ *   head h reads key head h / (n_q_heads / n_kv_heads).
+ *   q: act, element (b, h, d) at b * ldq + h * ldqh + d (multiples of 8,
+ *   16-byte aligned); out: act [B, n_q_heads, head_dim] packed, 16-byte aligned.
+ *   block_table [B] rows of int32, row stride ld_table: entry t / block_tokens
+ *   is the block of position t.
+ *   lse [B, n_q_heads] fp32 or NULL: log of the softmax's denominator (natural,
+ *   scores as scaled), to join attention over several parts.
+ *   max_len: the caller's bound of seq_lens (the host does not read them); a
+ *   longer sequence counts as max_len long. ld_table * block_tokens >= max_len.
+ * A sequence of length 0 (or less) gives zeros and an lse of -infinity.
+ * Positions in a block outside 0 .. n_blocks - 1 are left out. What lies in
+ * the cache outside the attended positions is not used, NaN and infinities
+ * included. Scores, softmax and sums are in fp32.
+ * Constraints: B >= 0; n_q_heads a multiple of n_kv_heads; max_len >= 0, below
+ * 2^31 - 256; window >= 0; scale finite (PW_EINVAL otherwise); B *
+ * n_q_heads < 2^23 (PW_EUNSUPPORTED: split the batch).
+ * ws: device workspace of at least pw_attn_workspace bytes, 16-byte aligned
+ * (PW_ENOMEM below; may be NULL where that is 0), in use until `stream` passes
+ * the call. Deterministic: the split of a sequence and the order of the joins
+ * depend on the arguments alone.                                             */
+pw_status pw_attn_workspace(const pw_kv_cache* cache, int B, int n_q_heads, int max_len, int window,
+                            size_t* ws_bytes);
+pw_status pw_attn_decode(const pw_kv_cache* cache, const void* q, int64_t ldq, int64_t ldqh, int n_q_heads,
+                         const int32_t* block_table, int64_t ld_table, const int32_t* seq_lens, int B,
+                         int max_len, float scale, int window, void* out, float* lse, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* Group-limited routing and token permutation. For each token, with p_e =
+ * sigmoid(l_e) or softmax(l)_e of its logits and c_e = p_e + bias_e (bias NULL:
+ * 0), both held in 64 bits:
+ *   the experts lie in n_groups groups of E / n_groups; a group's score is the
+ *   sum of its group_top (1 or 2) largest c; the top_groups groups of the
+ *   largest scores are kept, then the K experts of the largest c in them (ties
+ *   to the lower group and expert), in decreasing order of c;
+ *   w = p_e, divided by the sum of the K where renorm != 0, times w_scale.
+ * The bias decides the choice only. An expert whose logit is -infinity or NaN,
+ * or whose c is NaN or -infinity, is not eligible (its p is 0 where its logit
+ * is); a logit of +infinity counts as 3e38. Where fewer than K are eligible the
+ * rest are the ineligible experts of the lowest index, with weight 0; a token
+ * without an eligible expert has weights 0.
+ *   logits [T,E] of logit_type (PW_F32, PW_F16, PW_BF16), packed; bias [E]
+ *   fp32; shared-expert columns, their gates and the outputs as in
+ *   pw_route_topk_shared.
+ * Constraints: those of pw_route_topk_shared; n_groups >= 1 divides E, n_groups
+ * <= 64, 1 <= top_groups <= n_groups, K <= top_groups * (E / n_groups); w_scale
+ * finite (PW_EINVAL otherwise). T = 0 writes offsets only.                   */
+enum { PW_SCORE_SOFTMAX = 0, PW_SCORE_SIGMOID = 1 };
+pw_status pw_route_grouped(const void* logits, int logit_type, const float* bias, int T, int E, int K, int score,
+                           int n_groups, int top_groups, int group_top, int renorm, float w_scale, int n_shared,
+                           const float* shared_gate, int32_t* topk_ids, float* topk_w, int32_t* offsets,
+                           int32_t* sorted_slot, int32_t* slot_pos, void* stream);
+
 /* ---- Ceiling probes (diagnostics beside the hot path) ---------------------
  * What the device delivers, for reading the kernels' roofline fractions
  * against the achievable as well as the published peaks.

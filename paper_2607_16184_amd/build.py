@@ -42,7 +42,12 @@ SOURCES = {
     "pw_tgemm.hip": [],
     "pw_probe.hip": [],
     "pw_scratch.hip": [],
+    "pw_norm.hip": [],
+    "pw_gemm8.hip": [],
+    "pw_attn.hip": [],
+    "pw_route.hip": [],
     "pw_api.cpp": [],
+    "pw_ops_api.cpp": [],
     "pw_state.cpp": [],
     "pw_plan.cpp": [],
 }

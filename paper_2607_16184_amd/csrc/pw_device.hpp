@@ -98,6 +98,47 @@ __device__ __forceinline__ u32x4 ld16_nt(const uint8_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
 
+// Two values rounded to nearest even, as one 32-bit pair. NaN stays NaN (the
+// hardware's conversions keep it; the bit formula of bf16_rne need not).
+template <int ACT>
+__device__ __forceinline__ uint32_t pack16(float a, float b) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+  if constexpr (ACT == PW_BF16)
+    return __builtin_bit_cast(uint32_t, bf16x2_t{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+  else
+    return __builtin_bit_cast(uint32_t, f16x2_t{static_cast<_Float16>(a), static_cast<_Float16>(b)});
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit floating point (e4m3) with a scale per group
+// ---------------------------------------------------------------------------
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
+}
+// Largest value of the lane's row of 16 lanes, in every lane of it.
+__device__ __forceinline__ float row16_max(float m) {
+  m = fmaxf(m, dpp_f32<0xB1>(m));    // quad_perm 1,0,3,2
+  m = fmaxf(m, dpp_f32<0x4E>(m));    // quad_perm 2,3,0,1
+  m = fmaxf(m, dpp_f32<0x141>(m));   // row_half_mirror
+  return fmaxf(m, dpp_f32<0x140>(m));   // row_mirror
+}
+// Scale of a group of largest magnitude m. (The divisions here and below are
+// correctly rounded: v / s is at most 448 (1 + 2^-23), which rounds to 448.)
+__device__ __forceinline__ float f8_scale(float m) { return fmaxf(m / 448.0f, 0x1p-126f); }
+__device__ __forceinline__ u32x2 f8_codes8(const float* v, float s) {
+  u32x2 o;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i] / s, v[4 * i + 1] / s, 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2] / s, v[4 * i + 3] / s, c, true);
+    o[i] = static_cast<uint32_t>(c);
+  }
+  return o;
+}
+
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
 
 // Bytes of one 16-row x 128-value tile of a page at `B` bits.

@@ -1,0 +1,204 @@
+"""A decoder layer's operators around its paged experts, on torch tensors.
+
+PyTorch supplies device memory and streams only; every computation is a call
+into libpagedweight.so (see include/pw.h for the formulas and constraints).
+Outputs are written where ``out`` points, as a serving loop that keeps its
+buffers wants it, or into new tensors. Shapes, types and strides are checked
+here, sizes and alignment by the library (:class:`pw.PWError`).
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import pw
+from .layer import PagedLayer, _stream
+
+_TYPE = {torch.float16: pw.PW_F16, torch.bfloat16: pw.PW_BF16, torch.float32: pw.PW_F32}
+_F8 = torch.float8_e4m3fn
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _ptr(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _packed(t: Optional[torch.Tensor], shape, dtype, name: str):
+    _need(t is None or (t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.is_cuda),
+          "%s must be a contiguous device tensor of %s, %s" % (name, tuple(shape), dtype))
+
+
+class _Workspace:
+    """A device buffer that grows to what the calls of one handle need."""
+
+    def __init__(self, device):
+        self.device, self.t, self.bytes = device, None, 0
+
+    def ptr(self, need: int) -> int:
+        if need > self.bytes:
+            self.t = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self.bytes = need
+        return _ptr(self.t)
+
+
+# ---------------------------------------------------------------------------
+# Norm
+# ---------------------------------------------------------------------------
+
+NormOut = Tuple[Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor], Optional[torch.Tensor]]
+
+
+def norm_buffers(T: int, H: int, act: torch.dtype, residual: bool = True, y16: bool = True, y8: bool = False,
+                 device="cuda") -> NormOut:
+    """(sum, y16, y8, y8_scale) of ``rms_norm``, None for those not wanted."""
+    return (torch.empty((T, H), dtype=act, device=device) if residual else None,
+            torch.empty((T, H), dtype=act, device=device) if y16 else None,
+            torch.empty((T, H), dtype=_F8, device=device) if y8 else None,
+            torch.empty((T, H // 128), dtype=torch.float32, device=device) if y8 else None)
+
+
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, *,
+             eps: float = 1e-5, y16: bool = True, y8: bool = False, out: NormOut = None, stream=None) -> NormOut:
+    """Root-mean-square norm of x (+ residual): (sum, y16, y8, y8_scale), the
+    wanted ones of them or those that ``out`` holds (pw_rms_norm)."""
+    T, H = x.shape
+    act = x.dtype
+    _need(act in (torch.float16, torch.bfloat16) and x.is_cuda and x.stride(1) == 1, "x must be 16-bit rows on the device")
+    _need(residual is None or (residual.shape == x.shape and residual.dtype == act and residual.stride(1) == 1),
+          "residual must have x's shape and type")
+    _packed(weight, (H,), act, "weight")
+    if out is None:
+        out = norm_buffers(T, H, act, residual is not None, y16, y8, x.device)
+    s, y, q, qs = out
+    _packed(s, (T, H), act, "the sum")
+    _packed(y, (T, H), act, "y16")
+    _packed(q, (T, H), _F8, "y8")
+    _packed(qs, (T, H // 128), torch.float32, "y8_scale")
+    # (a single row may have any stride)
+    pw.pw_rms_norm(x.data_ptr(), x.stride(0) if T > 1 else H, _ptr(residual),
+                   residual.stride(0) if residual is not None and T > 1 else H, _ptr(weight), T, H, eps, _TYPE[act], _ptr(s),
+                   _ptr(y), _ptr(q), _ptr(qs), _stream(stream))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# 8-bit product
+# ---------------------------------------------------------------------------
+
+class Linear8:
+    """y = x W^T of 8-bit rows: W [N, K] e4m3 with one scale per 128 x 128
+    block [ceil(N / 128), K / 128]."""
+
+    def __init__(self, w8: torch.Tensor, w_scale: torch.Tensor):
+        _need(w8.dtype == _F8 and w8.dim() == 2 and w8.stride(1) == 1 and w8.is_cuda, "w8 must be e4m3 rows on the device")
+        self.N, self.K = w8.shape
+        _need(self.K % 128 == 0, "K must be a multiple of 128")
+        _packed(w_scale, (-(-self.N // 128), self.K // 128), torch.float32, "w_scale")
+        self.w8, self.w_scale = w8, w_scale
+        self._ws = _Workspace(w8.device)
+
+    def forward(self, x8: torch.Tensor, x_scale: torch.Tensor, out: torch.Tensor = None, dtype=torch.bfloat16,
+                stream=None) -> torch.Tensor:
+        """x8 [M, K] e4m3 rows with x_scale [M, K / 128] (as rms_norm gives
+        them) -> [M, N] (pw_gemm_fp8)."""
+        M, N, K = x8.shape[0], self.N, self.K
+        _need(x8.dtype == _F8 and x8.dim() == 2 and x8.shape[1] == K and x8.stride(1) == 1, "x8 must be [M, K] e4m3 rows")
+        _packed(x_scale, (M, K // 128), torch.float32, "x_scale")
+        if out is None:
+            out = torch.empty((M, N), dtype=dtype, device=x8.device)
+        _need(out.shape == (M, N) and out.dtype in _TYPE and (N == 1 or out.stride(1) == 1), "out must be [M, N] rows")
+        need = pw.pw_gemm_fp8_workspace(M, N, K)
+        pw.pw_gemm_fp8(x8.data_ptr(), x8.stride(0) if M > 1 else K, x_scale.data_ptr(), self.w8.data_ptr(),
+                       self.w8.stride(0) if N > 1 else K, self.w_scale.data_ptr(), M, N, K, out.data_ptr(),
+                       out.stride(0) if M > 1 else N, _TYPE[out.dtype], self._ws.ptr(need), need, _stream(stream))
+        return out
+
+
+# ---------------------------------------------------------------------------
+# KV cache
+# ---------------------------------------------------------------------------
+
+class KVCache:
+    """Paged keys and values of one attention layer: n_blocks blocks of
+    block_tokens tokens, in ``act`` or (fp8) as e4m3 codes with a scale per
+    token and head. ``pool``: a uint8 device tensor to keep the blocks in (e.g.
+    one that also holds weight pages), block i at byte i * block_stride."""
+
+    def __init__(self, n_blocks: int, block_tokens: int, kv_heads: int, head_dim: int, act: torch.dtype, fp8: bool = False,
+                 pool: torch.Tensor = None, block_stride: int = None, device="cuda"):
+        _need(act in (torch.float16, torch.bfloat16), "act must be a 16-bit type")
+        self.act, self.head_dim, self.kv_heads = act, head_dim, kv_heads
+        self.desc = pw.pw_kv_cache(None, 0, n_blocks, block_tokens, kv_heads, head_dim, _TYPE[act], 8 if fp8 else 16)
+        self.block_bytes = pw.pw_kv_block_bytes(self.desc)
+        self.desc.block_stride = block_stride or self.block_bytes
+        if pool is None:
+            pool = torch.empty(max(n_blocks - 1, 0) * self.desc.block_stride + self.block_bytes, dtype=torch.uint8, device=device)
+        _need(pool.dtype == torch.uint8 and pool.is_contiguous() and pool.is_cuda, "the pool must be contiguous device bytes")
+        _need(block_stride is not None or pool.numel() >= n_blocks * self.block_bytes, "the pool is smaller than its blocks")
+        self.pool = pool
+        self.desc.pool = pool.data_ptr()
+        self._ws = _Workspace(pool.device)
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
+        """Write k, v [T, kv_heads, head_dim] to the slots [T] int64 (block *
+        block_tokens + position in it; negative: nothing) (pw_kv_append)."""
+        T = k.shape[0]
+        _need(k.shape == (T, self.kv_heads, self.head_dim) and v.shape == k.shape, "k and v must be [T, kv_heads, head_dim]")
+        _need(k.dtype == self.act and v.dtype == self.act and k.stride() == v.stride() and k.stride(2) == 1,
+              "k and v must be of the cache's type, with equal strides and contiguous channels")
+        _packed(slots, (T,), torch.int64, "slots")
+        pw.pw_kv_append(self.desc, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), slots.data_ptr(), T, _stream(stream))
+
+    def attend(self, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, max_len: int, scale: float = None,
+               window: int = 0, out: torch.Tensor = None, lse: torch.Tensor = None, stream=None) -> torch.Tensor:
+        """Attention of one token per sequence: q [B, heads, head_dim] over the
+        first lens[b] cached tokens of the blocks block_table[b] (the last
+        ``window`` of them) -> [B, heads, head_dim] (pw_attn_decode)."""
+        B, heads, D = q.shape
+        _need(q.dtype == self.act and D == self.head_dim and q.stride(2) == 1, "q must be [B, heads, head_dim] of the cache's type")
+        _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.shape[0] == B
+              and (block_table.stride(1) == 1 or block_table.shape[1] == 1), "block_table must be [B, blocks] int32")
+        _packed(lens, (B,), torch.int32, "lens")
+        _need(block_table.shape[1] * self.desc.block_tokens >= max_len, "the block table is shorter than max_len")
+        if out is None:
+            out = torch.empty((B, heads, D), dtype=self.act, device=q.device)
+        _packed(out, (B, heads, D), self.act, "out")
+        _packed(lse, (B, heads), torch.float32, "lse")
+        need = pw.pw_attn_workspace(self.desc, B, heads, max_len, window)
+        pw.pw_attn_decode(self.desc, q.data_ptr(), q.stride(0), q.stride(1), heads, block_table.data_ptr(),
+                          block_table.stride(0) if B > 1 else block_table.shape[1],
+                          lens.data_ptr(), B, max_len, D ** -0.5 if scale is None else scale, window, out.data_ptr(),
+                          _ptr(lse), self._ws.ptr(need), need, _stream(stream))
+        return out
+
+
+# ---------------------------------------------------------------------------
+# Routing
+# ---------------------------------------------------------------------------
+
+_SCORE = {"softmax": pw.PW_SCORE_SOFTMAX, "sigmoid": pw.PW_SCORE_SIGMOID}
+
+
+def route_grouped(logits: torch.Tensor, K: int, score: str = "softmax", bias: torch.Tensor = None, groups: int = 1,
+                  top_groups: int = 1, group_top: int = 1, renorm: bool = True, scale: float = 1.0, n_shared: int = 0,
+                  gate: torch.Tensor = None, out=None, stream=None):
+    """Routing for PagedLayer.forward from logits [T, E]: (ids, w, offsets,
+    sorted_slot, slot_pos), n_shared shared-expert columns after the K routed
+    ones (pw_route_grouped)."""
+    T, E = logits.shape
+    _packed(logits, (T, E), logits.dtype, "logits")
+    _need(logits.dtype in _TYPE, "logits must be fp32, fp16 or bf16")
+    _need(score in _SCORE, "score must be softmax or sigmoid")
+    _packed(bias, (E,), torch.float32, "bias")
+    _packed(gate, (T, n_shared), torch.float32, "gate")
+    Kt = K + n_shared
+    ids, w, offsets, ss, sp = out if out is not None else PagedLayer.routing_buffers(T, E + n_shared, Kt, logits.device)
+    pw.pw_route_grouped(logits.data_ptr(), _TYPE[logits.dtype], _ptr(bias), T, E, K, _SCORE[score], groups, top_groups,
+                        group_top, int(renorm), scale, n_shared, _ptr(gate), ids.data_ptr(), w.data_ptr(),
+                        offsets.data_ptr(), ss.data_ptr(), sp.data_ptr(), _stream(stream))
+    return ids, w, offsets, ss, sp

@@ -21,7 +21,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpagedweight.so")
 
 PW_OK, PW_EINVAL, PW_ENOMEM, PW_EBUSY, PW_EUNSUPPORTED, PW_EHIP, PW_ESTATE = range(7)
-PW_F16, PW_BF16 = 0, 1
+PW_F16, PW_BF16, PW_F32 = 0, 1, 2
+PW_SCORE_SOFTMAX, PW_SCORE_SIGMOID = 0, 1
 PW_GATE, PW_UP, PW_DOWN = 0, 1, 2
 PW_PAGE_ABSENT, PW_PAGE_RESIDENT, PW_PAGE_REQUANT_PENDING, PW_PAGE_RELOAD_PENDING = 0, 1, 2, 3
 PW_PH_GATEUP, PW_PH_DOWN, PW_PH_COMBINE, PW_PH_REQUANT, PW_PH_GEMM, PW_NPHASE = 0, 1, 2, 3, 4, 5
@@ -61,6 +62,12 @@ class pw_plan_summary(ctypes.Structure):
                 ("n_units", ctypes.c_int)]
 
 
+class pw_kv_cache(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("block_stride", ctypes.c_int64),
+                ("n_blocks", ctypes.c_int), ("block_tokens", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("act", ctypes.c_int), ("bits", ctypes.c_int)]
+
+
 class PWError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__("%s: %s" % (_status_name(status), msg))
@@ -80,6 +87,7 @@ def _load():
         _build.build_all()
     L = ctypes.CDLL(LIB_PATH)
     vp, i32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+    i64, f32 = ctypes.c_int64, ctypes.c_float
     P = ctypes.POINTER
     sig = {
         "pw_table_entries": (sz, [P(pw_layer_desc)]),
@@ -125,6 +133,15 @@ def _load():
         "pw_planner_create_for_layer": (i32, [vp, P(ctypes.c_double), P(pw_planner_config), P(vp)]),
         "pw_planner_step_layer": (i32, [vp, vp, i32, i32, ctypes.c_uint64, P(pw_plan_summary)]),
         "pw_planner_apply": (i32, [vp, vp, vp, P(sz)]),
+        "pw_rms_norm": (i32, [vp, i64, vp, i64, vp, i32, i32, f32, i32, vp, vp, vp, vp, vp]),
+        "pw_gemm_fp8_workspace": (i32, [i32, i32, i32, P(sz)]),
+        "pw_gemm_fp8": (i32, [vp, i64, vp, vp, i64, vp, i32, i32, i32, vp, i64, i32, vp, sz, vp]),
+        "pw_kv_block_bytes": (i32, [P(pw_kv_cache), P(sz)]),
+        "pw_kv_append": (i32, [P(pw_kv_cache), vp, vp, i64, i64, vp, i32, vp]),
+        "pw_attn_workspace": (i32, [P(pw_kv_cache), i32, i32, i32, i32, P(sz)]),
+        "pw_attn_decode": (i32, [P(pw_kv_cache), vp, i64, i64, i32, vp, i64, vp, i32, i32, f32, i32, vp, vp, vp, sz, vp]),
+        "pw_route_grouped": (i32, [vp, i32, vp, i32, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, vp, vp, vp, vp, vp,
+                                   vp]),
         "pw_last_error": (ctypes.c_char_p, []),
         "pw_status_str": (ctypes.c_char_p, [i32]),
     }
@@ -451,3 +468,56 @@ def pw_layer_load_pages_apl(layer: int, es, projs, rbs, bits, row_ptrs, ws_ptr: 
     ptrs = (ctypes.c_void_p * max(n, 1))(*row_ptrs)
     _check(_lib.pw_layer_load_pages_apl(layer, n, arr(*es), arr(*projs), arr(*rbs), arr(*bits), ptrs, ws_ptr,
                                         ws_bytes, stream))
+
+
+# --------------------------------------------------------------------------
+# operators around the experts
+# --------------------------------------------------------------------------
+
+def pw_rms_norm(x_ptr: int, ldx: int, residual_ptr: int, ldr: int, weight_ptr: int, T: int, H: int, eps: float, act: int,
+                sum_ptr: int, y16_ptr: int, y8_ptr: int, y8_scale_ptr: int, stream: int):
+    _check(_lib.pw_rms_norm(x_ptr, ldx, residual_ptr, ldr, weight_ptr, T, H, eps, act, sum_ptr, y16_ptr, y8_ptr,
+                            y8_scale_ptr, stream))
+
+
+def pw_gemm_fp8_workspace(M: int, N: int, K: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.pw_gemm_fp8_workspace(M, N, K, ctypes.byref(out)))
+    return out.value
+
+
+def pw_gemm_fp8(a_ptr: int, lda: int, a_scale_ptr: int, w_ptr: int, ldw: int, w_scale_ptr: int, M: int, N: int, K: int,
+                y_ptr: int, ldy: int, y_type: int, ws_ptr: int, ws_bytes: int, stream: int):
+    _check(_lib.pw_gemm_fp8(a_ptr, lda, a_scale_ptr, w_ptr, ldw, w_scale_ptr, M, N, K, y_ptr, ldy, y_type, ws_ptr, ws_bytes,
+                            stream))
+
+
+def pw_kv_block_bytes(cache: pw_kv_cache) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.pw_kv_block_bytes(ctypes.byref(cache), ctypes.byref(out)))
+    return out.value
+
+
+def pw_kv_append(cache: pw_kv_cache, k_ptr: int, v_ptr: int, ld: int, ldh: int, slots_ptr: int, T: int, stream: int):
+    _check(_lib.pw_kv_append(ctypes.byref(cache), k_ptr, v_ptr, ld, ldh, slots_ptr, T, stream))
+
+
+def pw_attn_workspace(cache: pw_kv_cache, B: int, n_q_heads: int, max_len: int, window: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.pw_attn_workspace(ctypes.byref(cache), B, n_q_heads, max_len, window, ctypes.byref(out)))
+    return out.value
+
+
+def pw_attn_decode(cache: pw_kv_cache, q_ptr: int, ldq: int, ldqh: int, n_q_heads: int, table_ptr: int, ld_table: int,
+                   lens_ptr: int, B: int, max_len: int, scale: float, window: int, out_ptr: int, lse_ptr: int, ws_ptr: int,
+                   ws_bytes: int, stream: int):
+    _check(_lib.pw_attn_decode(ctypes.byref(cache), q_ptr, ldq, ldqh, n_q_heads, table_ptr, ld_table, lens_ptr, B, max_len,
+                               scale, window, out_ptr, lse_ptr, ws_ptr, ws_bytes, stream))
+
+
+def pw_route_grouped(logits_ptr: int, logit_type: int, bias_ptr: int, T: int, E: int, K: int, score: int, n_groups: int,
+                     top_groups: int, group_top: int, renorm: int, w_scale: float, n_shared: int, gate_ptr: int, ids_ptr: int,
+                     w_ptr: int, offsets_ptr: int, sorted_slot_ptr: int, slot_pos_ptr: int, stream: int):
+    _check(_lib.pw_route_grouped(logits_ptr, logit_type, bias_ptr, T, E, K, score, n_groups, top_groups, group_top, renorm,
+                                 w_scale, n_shared, gate_ptr, ids_ptr, w_ptr, offsets_ptr, sorted_slot_ptr, slot_pos_ptr,
+                                 stream))
