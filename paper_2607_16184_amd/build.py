@@ -43,7 +43,7 @@ SOURCES = {
     "pw_probe.hip": [],
     "pw_scratch.hip": [],
     "pw_norm.hip": [],
-    "pw_gemm8.hip": [],
+    "pw_gemm8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "pw_attn.hip": [],
     "pw_route.hip": [],
     "pw_api.cpp": [],
