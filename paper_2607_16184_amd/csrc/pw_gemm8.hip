@@ -7,6 +7,8 @@
 // multiplies all of them by the same w_scale * a_scale. (Both operands hold
 // bytes 32 g .. 32 g + 31 of their row's block in lane group g; which k that is
 // for the hardware does not matter, it is the same for both.)
+#include <type_traits>
+
 #include "pw_device.hpp"
 #include "pw_lds.hpp"
 #include "pw_ops.hpp"
@@ -51,6 +53,23 @@ __device__ __forceinline__ void store4(const Gemm8Args& a, int m, int n, f32x4 v
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     if (n + j < a.N) store_y(a, m, n + j, v[j]);
+}
+
+// 16 bytes of one row's columns from n on, as one store where they are all there
+// and aligned.
+template <int E>
+__device__ __forceinline__ void store_piece(const Gemm8Args& a, int m, int n, u32x4 v) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a.y) + (m * a.ldy + n) * E;
+  if (n + 16 / E <= a.N && (at & 15) == 0) {
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(at));
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 16 / E; ++j) {
+    if (n + j >= a.N) break;
+    if constexpr (E == 4) reinterpret_cast<uint32_t*>(at)[j] = v[j];
+    else reinterpret_cast<uint16_t*>(at)[j] = static_cast<uint16_t>(v[j / 2] >> (16 * (j & 1)));
+  }
 }
 
 // Streaming kernel: 16 weight rows x 16 MT tokens per workgroup, whose four
@@ -115,24 +134,27 @@ hipError_t launch_stream(const Gemm8Args& a, hipStream_t st) {
 // Tiled kernel: TN weight rows x TM tokens per workgroup, WN x WM waves. K
 // advances by one scale block (128) per stage; two stages lie in LDS. Global
 // loads write LDS directly, 8 whole 128-byte lines per load, with the 16-byte
-// pieces of a row permuted by the row index so that the operand reads meet no
-// bank conflict. A wave reads the column operands (tokens) of a stage once and
+// pieces of a row permuted by half the row index: the 16 rows that a quarter of
+// an operand read takes then lie in 16 different sixteenths of the 64 banks
+// (permuted by the row index itself, rows r and r + 8 share theirs and reads
+// take twice the cycles). A wave reads the column operands (tokens) of a stage once and
 // the row operands tile by tile, two ahead; the multiply-adds of a row tile run
 // under the next one's matrix instructions. The barrier that publishes the next
 // stage stands before the last row tile, whose operands are in registers by
-// then, so that the next stage's first operands arrive under it, and loads have
-// a whole stage's time to land.
+// then, so that the next stage's first operands arrive under it. The loads of a
+// stage go out over several row tiles: all at once they queue up in the address
+// unit and hold the wave back.
 template <int TN, int TM, int WN, int WM>
 struct Geo8 {
   static constexpr int kWaves = WN * WM;
   static constexpr int RN = TN / WN / 16, RM = TM / WM / 16;     // a wave's 16 x 16 tiles
   static constexpr int NW = TN / 8 / kWaves, NX = TM / 8 / kWaves;   // a wave's 1 KB loads of a stage
-  // weights, tokens, and 256 bytes of scales per wave: 64 tokens' each, then the
-  // weight blocks', then (the same again) what no one reads
-  static constexpr int kX = TN * 128, kXs = kX + TM * 128, kWs = kXs + TM * 4;
-  static constexpr int kSlot = kXs + kWaves * 256;
-  static_assert(TM / 64 < kWaves, "a wave for the weight scales");
-  static constexpr int kLds = 2 * kSlot;
+  // two slots of weights and tokens, two of the tokens' scales of kSc stages
+  static constexpr int kX = TN * 128, kSlot = kX + TM * 128;
+  static constexpr int kSc = 8, kScSlot = TM * kSc * 4, kScOff = 2 * kSlot;
+  static constexpr int NS = TM / 8 / kWaves;                     // a wave's loads of scales: 8 tokens x kSc stages each
+  static constexpr int kLds = kScOff + 2 * kScSlot;
+  static_assert(NS <= kSc && kSc % NS == 0, "the scales of the next stages are loaded over kSc stages");
 };
 
 template <int TN, int TM, int WN, int WM>
@@ -157,45 +179,52 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
   const int n0 = in / deep * TN, m0 = (kDeep * grp + in % deep) * TM;
 
   // the wave's loads: rows 8 q .. 8 q + 7 of its share, lane l the piece (l mod
-  // 8) ^ (row mod 8) of row l / 8; rows past the end repeat the last one
-  const int lrow = lane >> 3, piece = (lane & 7) ^ lrow;
+  // 8) ^ (row / 2 mod 8) of row l / 8; rows past the end repeat the last one
+  const int lrow = lane >> 3;
+  const auto piece = [&](int q) { return (lane & 7) ^ (lrow >> 1) ^ (4 * (q & 1)); };
   uint32_t woff[G::NW], xoff[G::NX];
 #pragma unroll
   for (int q = 0; q < G::NW; ++q) {
     const int r = min(n0 + (wave * G::NW + q) * 8 + lrow, a.N - 1) - n0;
-    woff[q] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.ldw) + 16 * piece;
+    woff[q] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.ldw) + 16 * piece(wave * G::NW + q);
   }
 #pragma unroll
   for (int q = 0; q < G::NX; ++q) {
     const int r = min(m0 + (wave * G::NX + q) * 8 + lrow, a.M - 1) - m0;
-    xoff[q] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.lda) + 16 * piece;
+    xoff[q] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.lda) + 16 * piece(wave * G::NX + q);
   }
   const uint8_t* wbase = uniform_ptr(a.w + n0 * a.ldw);
   const uint8_t* xbase = uniform_ptr(a.a + m0 * a.lda);
-  // scales: the first TM / 64 waves load 64 tokens' each, the others the scales
-  // of the tile's weight blocks (every wave one load: a branch would cut the
-  // loop's schedule in two)
-  uint32_t soff;
-  const uint8_t* sbase;
-  if (wave < TM / 64) {
-    soff = static_cast<uint32_t>(min(m0 + 64 * wave + lane, a.M - 1) - m0) * static_cast<uint32_t>(KB) * 4u;
-    sbase = uniform_ptr(reinterpret_cast<const uint8_t*>(a.a_scale + static_cast<size_t>(m0) * KB));
-  } else {
-    soff = static_cast<uint32_t>(min(n0 / 128 + min(lane, TN / 128 - 1), (a.N - 1) / 128) - n0 / 128) * static_cast<uint32_t>(KB) * 4u;
-    sbase = uniform_ptr(reinterpret_cast<const uint8_t*>(a.w_scale + static_cast<size_t>(n0 / 128) * KB));
-  }
-  const auto load = [&](int s, int slot) {
+  // Scales of the tokens come for kSc stages at a time: a load takes 8 tokens x
+  // kSc stages, lane l token l mod 8 and stage l / 8 (a load for one stage would
+  // touch a cache line per token, as many as all operand loads of the stage).
+  // They are spread over the stages before: stage s loads a share of those of
+  // the next kSc (each share more than once, so that every stage has the same
+  // count of loads). The weight block's scales lie in a register, a stage in a
+  // lane.
+  const uint8_t* sbase = uniform_ptr(reinterpret_cast<const uint8_t*>(a.a_scale + static_cast<size_t>(m0) * KB));
+  const auto load_scales = [&](int chunk, int q) {
+    const int o = wave * G::NS + q;
+    const int r = min(m0 + 8 * o + (lane & 7), a.M - 1) - m0, st = min(chunk * G::kSc + lrow, KB - 1);
+    lds_load4(lds0 + G::kScOff + (chunk & 1) * G::kScSlot + o * 256,
+              (static_cast<uint32_t>(r) * static_cast<uint32_t>(KB) + static_cast<uint32_t>(st)) * 4u, sbase);
+  };
+  const float* wsp = a.w_scale + static_cast<size_t>(min((n0 + wn * G::RN * 16) / 128, (a.N - 1) / 128)) * KB;
+  int ws64 = 0;
+  const auto fetch_ws = [&](int s) { ws64 = __float_as_int(wsp[min(s + lane, KB - 1)]); };
+  // the wave's loads of stage s, one at a time
+  const auto load = [&](int s, int slot, int q) {
     const int b = s < KB ? s : KB - 1;               // past the end: the last block again, not used
     const uint32_t d = lds0 + slot * G::kSlot;
-#pragma unroll
-    for (int q = 0; q < G::NW; ++q) lds_load16(d + (wave * G::NW + q) * 1024, woff[q], wbase + b * 128);
-#pragma unroll
-    for (int q = 0; q < G::NX; ++q) lds_load16(d + G::kX + (wave * G::NX + q) * 1024, xoff[q], xbase + b * 128);
-    lds_load4(d + G::kXs + wave * 256, soff, sbase + b * 4);
+    if (q < G::NX) lds_load16(d + G::kX + (wave * G::NX + q) * 1024, xoff[q], xbase + b * 128);
+    else lds_load16(d + (wave * G::NW + q - G::NX) * 1024, woff[q - G::NX], wbase + b * 128);
   };
+  // They go out over kOver row tiles from the barrier on, kPer at each.
+  constexpr int kOver = G::RN == 8 ? 4 : 2, kPer = (G::NX + G::NW) / kOver;
+  static_assert(kPer * kOver == G::NX + G::NW, "whole shares");
 
-  // operand reads: row c of a 16-row tile, pieces 2 lg and 2 lg + 1
-  const uint32_t p0 = 128 * c + 16 * ((2 * lg) ^ (c & 7)), p1 = 128 * c + 16 * ((2 * lg + 1) ^ (c & 7));
+  // operand reads: row c of a 16-row tile, pieces lg and lg + 4
+  const uint32_t p0 = 128 * c + 16 * (lg ^ (c >> 1)), p1 = p0 ^ 64;
   const auto read = [&](int off) { return F8Frag{lds16(lds + off + p0), lds16(lds + off + p1)}; };
   const auto read_w = [&](int slot, int i) { return read(slot * G::kSlot + (wn * G::RN + i) * 2048); };
   const auto read_x = [&](int slot, int j) { return read(slot * G::kSlot + G::kX + (wm * G::RM + j) * 2048); };
@@ -203,7 +232,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
 
   F8Frag wf[2], xf[G::RM];
   f32x4 acc[G::RN][G::RM], d[2][G::RM];
-  float f[G::RM], fn[G::RM], wsn = 0.0f;
+  float f[G::RM], fn[G::RM];
 #pragma unroll
   for (int i = 0; i < G::RN; ++i)
 #pragma unroll
@@ -213,27 +242,35 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
     d[1][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     f[j] = 0.0f;
   }
-  const auto read_scales = [&](int slot) {
-    wsn = lds_f32(slot * G::kSlot + G::kWs + wn * G::RN * 16 / 128 * 4);
+  const auto read_scales = [&](int s) {
+    const int off = G::kScOff + (s / G::kSc & 1) * G::kScSlot + s % G::kSc * 32;
 #pragma unroll
-    for (int j = 0; j < G::RM; ++j) fn[j] = lds_f32(slot * G::kSlot + G::kXs + ((wm * G::RM + j) * 16 + c) * 4);
+    for (int j = 0; j < G::RM; ++j)
+      fn[j] = lds_f32(off + ((wm * G::RM + j) * 2 + (c >> 3)) * 256 + (c & 7) * 4);
   };
   const auto add = [&](int i, int j, int p) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(d[p][j][e], f[j], acc[i][j][e]);
   };
 
-  load(0, 0);
-  wait_vm<0>();
+#pragma unroll
+  for (int q = 0; q < G::NS; ++q) load_scales(0, q);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) load(0, 0, q);
+#pragma unroll
+  for (int q = 0; q < 2 * kPer; ++q) load(1, 1, q);
+  wait_vm<2 * kPer>();
   wg_barrier();
-  load(1, 1);
   wf[0] = read_w(0, 0);
   wf[1] = read_w(0, 1);
 #pragma unroll
   for (int j = 0; j < G::RM; ++j) xf[j] = read_x(0, j);
   read_scales(0);
 
-  for (int s = 0; s < KB; ++s) {
+  // (64 stages at a time: a branch in the loop would cut its schedule in two)
+  for (int s0 = 0; s0 < KB; s0 += 64) {
+  fetch_ws(s0);
+  for (int s = s0; s < min(s0 + 64, KB); ++s) {
     const int slot = s & 1;
 #pragma unroll
     for (int i = 0; i < G::RN; ++i) {
@@ -247,32 +284,63 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
         __builtin_amdgcn_sched_barrier(0);
       }
       if (i == 0) {
+        const float ws = __int_as_float(__builtin_amdgcn_readlane(ws64, s & 63));
 #pragma unroll
-        for (int j = 0; j < G::RM; ++j) f[j] = fn[j] * wsn;
+        for (int j = 0; j < G::RM; ++j) f[j] = fn[j] * ws;
       }
       if (i == G::RN - 2) {
         // every operand of this stage has been read; the next stage is here
         wait_lds<0>();
         wait_vm<0>();
         wg_barrier();
-        load(s + 2, slot);
+        load_scales((s + 1) / G::kSc + 1, (s + 1) % G::kSc / (G::kSc / G::NS));
+      }
+      // loads of the stage after next, from the barrier into the next stage
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) {
+        if (i >= G::RN - 2) load(s + 2, slot, (i - (G::RN - 2)) * kPer + q);
+        else if (i + 2 < kOver) load(s + 1, slot ^ 1, (i + 2) * kPer + q);
       }
       if (i < G::RN - 2) wf[i & 1] = read_w(slot, i + 2);
       else wf[i & 1] = read_w(slot ^ 1, i + 2 - G::RN);
-      if (i == G::RN - 1) read_scales(slot ^ 1);
+      if (i == G::RN - 1) read_scales(s + 1);
     }
+  }
   }
 #pragma unroll
   for (int j = 0; j < G::RM; ++j) add(G::RN - 1, j, (G::RN - 1) & 1);
+  // Through LDS (the wave's own part of it) to rows: a store then covers whole
+  // cache lines of a few tokens in place of 32 bytes of each of 16.
   wait_vm<0>();
-
+  wg_barrier();
+  const auto rows_out = [&](auto esz_tag, auto&& put) {
+    constexpr int kE = decltype(esz_tag)::value;          // bytes of an element
+    constexpr int kRow = G::RN * 16 * kE, kPitch = kRow + 16, kLanes = kRow / 16;
+    static_assert(16 * kPitch <= G::kLds / G::kWaves, "a wave's part of LDS");
+    lds_u8_t w = lds + wave * (G::kLds / G::kWaves / 16 * 16);
 #pragma unroll
-  for (int j = 0; j < G::RM; ++j) {
-    const int m = m0 + (wm * G::RM + j) * 16 + c;
-    if (m >= a.M) continue;
+    for (int j = 0; j < G::RM; ++j) {
 #pragma unroll
-    for (int i = 0; i < G::RN; ++i) store4(a, m, n0 + (wn * G::RN + i) * 16 + 4 * lg, acc[i][j]);
-  }
+      for (int i = 0; i < G::RN; ++i) put(w + c * kPitch + (i * 16 + 4 * lg) * kE, acc[i][j]);
+#pragma unroll
+      for (int k = 0; k < 16 * kLanes; k += 64) {
+        const int row = (k + lane) / kLanes, p = (k + lane) % kLanes;
+        const u32x4 v = lds16(w + row * kPitch + 16 * p);
+        const int m = m0 + (wm * G::RM + j) * 16 + row;
+        if (m < a.M) store_piece<kE>(a, m, n0 + wn * G::RN * 16 + p * (16 / kE), v);
+      }
+    }
+  };
+  if (a.y_type == PW_F32)
+    rows_out(std::integral_constant<int, 4>{}, [](lds_u8_t p, f32x4 v) { *reinterpret_cast<PW_LDS f32x4*>(p) = v; });
+  else if (a.y_type == PW_BF16)
+    rows_out(std::integral_constant<int, 2>{}, [](lds_u8_t p, f32x4 v) {
+      *reinterpret_cast<PW_LDS u32x2*>(p) = u32x2{pack16<PW_BF16>(v[0], v[1]), pack16<PW_BF16>(v[2], v[3])};
+    });
+  else
+    rows_out(std::integral_constant<int, 2>{}, [](lds_u8_t p, f32x4 v) {
+      *reinterpret_cast<PW_LDS u32x2*>(p) = u32x2{pack16<PW_F16>(v[0], v[1]), pack16<PW_F16>(v[2], v[3])};
+    });
 }
 
 template <int TN, int TM, int WN, int WM>
