@@ -13,7 +13,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import pw
-from .layer import PagedLayer, _stream
+from .layer import PagedLayer
 
 _TYPE = {torch.float16: pw.PW_F16, torch.bfloat16: pw.PW_BF16, torch.float32: pw.PW_F32}
 _F8 = torch.float8_e4m3fn
@@ -28,22 +28,37 @@ def _ptr(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.data_ptr()
 
 
+def _on(t: torch.Tensor, stream) -> int:
+    """The given stream, or the current one of the tensor's device. (Its raw
+    handle: 0.1 us, a Stream object 3 us, as long as a launch.)"""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
+
+
 def _packed(t: Optional[torch.Tensor], shape, dtype, name: str):
-    _need(t is None or (t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.is_cuda),
-          "%s must be a contiguous device tensor of %s, %s" % (name, tuple(shape), dtype))
+    if t is not None and not (t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous device tensor of %s, %s" % (name, shape, dtype))
 
 
 class _Workspace:
     """A device buffer that grows to what the calls of one handle need."""
 
     def __init__(self, device):
-        self.device, self.t, self.bytes = device, None, 0
+        self.device, self.t, self.ptr, self.bytes = device, None, 0, 0
 
-    def ptr(self, need: int) -> int:
-        if need > self.bytes:
-            self.t = torch.empty(need, dtype=torch.uint8, device=self.device)
-            self.bytes = need
-        return _ptr(self.t)
+    def call(self, fn, need, *args):
+        """fn(*args, ws_ptr, ws_bytes, stream) with the last of args the stream;
+        where the buffer is too small (PW_ENOMEM, nothing launched), again with
+        one of need() bytes."""
+        *args, stream = args
+        try:
+            fn(*args, self.ptr, self.bytes, stream)
+        except pw.PWError as e:
+            if e.status != pw.PW_ENOMEM:
+                raise
+            self.bytes = need()
+            self.t = torch.empty(self.bytes, dtype=torch.uint8, device=self.device)
+            self.ptr = self.t.data_ptr()
+            fn(*args, self.ptr, self.bytes, stream)
 
 
 # ---------------------------------------------------------------------------
@@ -68,9 +83,15 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: O
     wanted ones of them or those that ``out`` holds (pw_rms_norm)."""
     T, H = x.shape
     act = x.dtype
-    _need(act in (torch.float16, torch.bfloat16) and x.is_cuda and x.stride(1) == 1, "x must be 16-bit rows on the device")
-    _need(residual is None or (residual.shape == x.shape and residual.dtype == act and residual.stride(1) == 1),
-          "residual must have x's shape and type")
+    ldx, inner = x.stride()
+    _need((act is torch.bfloat16 or act is torch.float16) and x.is_cuda and inner == 1, "x must be 16-bit rows on the device")
+    ldr = H
+    if residual is not None:
+        ldr, inner = residual.stride()
+        _need(residual.shape == x.shape and residual.dtype is act and residual.is_cuda and inner == 1,
+              "residual must have x's shape and type")
+    if T <= 1:                         # a single row may have any stride
+        ldx = ldr = H
     _packed(weight, (H,), act, "weight")
     if out is None:
         out = norm_buffers(T, H, act, residual is not None, y16, y8, x.device)
@@ -79,10 +100,8 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: O
     _packed(y, (T, H), act, "y16")
     _packed(q, (T, H), _F8, "y8")
     _packed(qs, (T, H // 128), torch.float32, "y8_scale")
-    # (a single row may have any stride)
-    pw.pw_rms_norm(x.data_ptr(), x.stride(0) if T > 1 else H, _ptr(residual),
-                   residual.stride(0) if residual is not None and T > 1 else H, _ptr(weight), T, H, eps, _TYPE[act], _ptr(s),
-                   _ptr(y), _ptr(q), _ptr(qs), _stream(stream))
+    pw.pw_rms_norm(x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), T, H, eps, _TYPE[act], _ptr(s), _ptr(y), _ptr(q),
+                   _ptr(qs), _on(x, stream))
     return out
 
 
@@ -100,6 +119,7 @@ class Linear8:
         _need(self.K % 128 == 0, "K must be a multiple of 128")
         _packed(w_scale, (-(-self.N // 128), self.K // 128), torch.float32, "w_scale")
         self.w8, self.w_scale = w8, w_scale
+        self.ldw = w8.stride(0) if self.N > 1 else self.K
         self._ws = _Workspace(w8.device)
 
     def forward(self, x8: torch.Tensor, x_scale: torch.Tensor, out: torch.Tensor = None, dtype=torch.bfloat16,
@@ -107,15 +127,15 @@ class Linear8:
         """x8 [M, K] e4m3 rows with x_scale [M, K / 128] (as rms_norm gives
         them) -> [M, N] (pw_gemm_fp8)."""
         M, N, K = x8.shape[0], self.N, self.K
-        _need(x8.dtype == _F8 and x8.dim() == 2 and x8.shape[1] == K and x8.stride(1) == 1, "x8 must be [M, K] e4m3 rows")
+        _need(x8.dtype is _F8 and x8.shape == (M, K) and x8.is_cuda and x8.stride(1) == 1, "x8 must be [M, K] e4m3 rows")
         _packed(x_scale, (M, K // 128), torch.float32, "x_scale")
         if out is None:
             out = torch.empty((M, N), dtype=dtype, device=x8.device)
-        _need(out.shape == (M, N) and out.dtype in _TYPE and (N == 1 or out.stride(1) == 1), "out must be [M, N] rows")
-        need = pw.pw_gemm_fp8_workspace(M, N, K)
-        pw.pw_gemm_fp8(x8.data_ptr(), x8.stride(0) if M > 1 else K, x_scale.data_ptr(), self.w8.data_ptr(),
-                       self.w8.stride(0) if N > 1 else K, self.w_scale.data_ptr(), M, N, K, out.data_ptr(),
-                       out.stride(0) if M > 1 else N, _TYPE[out.dtype], self._ws.ptr(need), need, _stream(stream))
+        _need(out.shape == (M, N) and out.dtype in _TYPE and out.is_cuda and (N == 1 or out.stride(1) == 1),
+              "out must be [M, N] rows")
+        self._ws.call(pw.pw_gemm_fp8, lambda: pw.pw_gemm_fp8_workspace(M, N, K), x8.data_ptr(), x8.stride(0) if M > 1 else K,
+                      x_scale.data_ptr(), self.w8.data_ptr(), self.ldw, self.w_scale.data_ptr(), M, N, K, out.data_ptr(),
+                      out.stride(0) if M > 1 else N, _TYPE[out.dtype], _on(x8, stream))
         return out
 
 
@@ -149,10 +169,11 @@ class KVCache:
         block_tokens + position in it; negative: nothing) (pw_kv_append)."""
         T = k.shape[0]
         _need(k.shape == (T, self.kv_heads, self.head_dim) and v.shape == k.shape, "k and v must be [T, kv_heads, head_dim]")
-        _need(k.dtype == self.act and v.dtype == self.act and k.stride() == v.stride() and k.stride(2) == 1,
-              "k and v must be of the cache's type, with equal strides and contiguous channels")
+        ld, ldh, inner = k.stride()
+        _need(k.dtype is self.act and v.dtype is self.act and k.is_cuda and v.is_cuda and v.stride() == (ld, ldh, inner)
+              and inner == 1, "k and v must be of the cache's type, with equal strides and contiguous channels")
         _packed(slots, (T,), torch.int64, "slots")
-        pw.pw_kv_append(self.desc, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), slots.data_ptr(), T, _stream(stream))
+        pw.pw_kv_append(self.desc, k.data_ptr(), v.data_ptr(), ld, ldh, slots.data_ptr(), T, _on(k, stream))
 
     def attend(self, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, max_len: int, scale: float = None,
                window: int = 0, out: torch.Tensor = None, lse: torch.Tensor = None, stream=None) -> torch.Tensor:
@@ -160,20 +181,21 @@ class KVCache:
         first lens[b] cached tokens of the blocks block_table[b] (the last
         ``window`` of them) -> [B, heads, head_dim] (pw_attn_decode)."""
         B, heads, D = q.shape
-        _need(q.dtype == self.act and D == self.head_dim and q.stride(2) == 1, "q must be [B, heads, head_dim] of the cache's type")
-        _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.shape[0] == B
-              and (block_table.stride(1) == 1 or block_table.shape[1] == 1), "block_table must be [B, blocks] int32")
+        ldq, ldqh, inner = q.stride()
+        _need(q.dtype is self.act and D == self.head_dim and q.is_cuda and inner == 1,
+              "q must be [B, heads, head_dim] of the cache's type")
+        rows, blocks = block_table.shape
+        _need(block_table.dtype is torch.int32 and rows == B and block_table.is_cuda
+              and (block_table.stride(1) == 1 or blocks <= 1), "block_table must be [B, blocks] int32")
         _packed(lens, (B,), torch.int32, "lens")
-        _need(block_table.shape[1] * self.desc.block_tokens >= max_len, "the block table is shorter than max_len")
+        _need(blocks * self.desc.block_tokens >= max_len, "the block table is shorter than max_len")
         if out is None:
             out = torch.empty((B, heads, D), dtype=self.act, device=q.device)
         _packed(out, (B, heads, D), self.act, "out")
         _packed(lse, (B, heads), torch.float32, "lse")
-        need = pw.pw_attn_workspace(self.desc, B, heads, max_len, window)
-        pw.pw_attn_decode(self.desc, q.data_ptr(), q.stride(0), q.stride(1), heads, block_table.data_ptr(),
-                          block_table.stride(0) if B > 1 else block_table.shape[1],
-                          lens.data_ptr(), B, max_len, D ** -0.5 if scale is None else scale, window, out.data_ptr(),
-                          _ptr(lse), self._ws.ptr(need), need, _stream(stream))
+        args = (self.desc, q.data_ptr(), ldq, ldqh, heads, block_table.data_ptr(), block_table.stride(0) if B > 1 else blocks,
+                lens.data_ptr(), B, max_len, D ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse))
+        self._ws.call(pw.pw_attn_decode, lambda: pw.pw_attn_workspace(self.desc, B, heads, max_len, window), *args, _on(q, stream))
         return out
 
 
@@ -191,14 +213,15 @@ def route_grouped(logits: torch.Tensor, K: int, score: str = "softmax", bias: to
     sorted_slot, slot_pos), n_shared shared-expert columns after the K routed
     ones (pw_route_grouped)."""
     T, E = logits.shape
-    _packed(logits, (T, E), logits.dtype, "logits")
-    _need(logits.dtype in _TYPE, "logits must be fp32, fp16 or bf16")
+    _need(logits.dtype in _TYPE and logits.is_cuda and logits.is_contiguous(), "logits must be packed fp32, fp16 or bf16 rows")
     _need(score in _SCORE, "score must be softmax or sigmoid")
     _packed(bias, (E,), torch.float32, "bias")
     _packed(gate, (T, n_shared), torch.float32, "gate")
     Kt = K + n_shared
     ids, w, offsets, ss, sp = out if out is not None else PagedLayer.routing_buffers(T, E + n_shared, Kt, logits.device)
+    _need(ids.shape == (T, Kt) and w.shape == (T, Kt) and offsets.numel() == E + n_shared + 1
+          and min(ss.numel(), sp.numel()) >= T * Kt, "the routing buffers are of another size (PagedLayer.routing_buffers)")
     pw.pw_route_grouped(logits.data_ptr(), _TYPE[logits.dtype], _ptr(bias), T, E, K, _SCORE[score], groups, top_groups,
                         group_top, int(renorm), scale, n_shared, _ptr(gate), ids.data_ptr(), w.data_ptr(),
-                        offsets.data_ptr(), ss.data_ptr(), sp.data_ptr(), _stream(stream))
+                        offsets.data_ptr(), ss.data_ptr(), sp.data_ptr(), _on(logits, stream))
     return ids, w, offsets, ss, sp
