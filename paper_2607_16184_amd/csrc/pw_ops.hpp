@@ -78,6 +78,9 @@ struct RouteArgs {
   const float* gate;
   int32_t* ids;
   float* w;
+  int32_t* offsets;
+  int32_t* sorted_slot;
+  int32_t* slot_pos;
   int T, E, K;
   int logit_type, score, n_groups, top_groups, group_top, renorm, n_shared;
   float w_scale;

@@ -192,13 +192,15 @@ pw_status pw_route_grouped(const void* logits, int logit_type, const float* bias
   const int Kt = K + n_shared;
   if (static_cast<int64_t>(T) * Kt >= (int64_t(1) << 31)) return set_error(PW_EINVAL, "T*K too large");
   if (!offsets || (T > 0 && (!logits || !ids || !w || !sorted_slot || !slot_pos))) return set_error(PW_EINVAL, "null argument");
-  const hipStream_t st = static_cast<hipStream_t>(stream);
   pw::RouteArgs a{};
   a.logits = logits;
   a.bias = bias;
   a.gate = shared_gate;
   a.ids = ids;
   a.w = w;
+  a.offsets = offsets;
+  a.sorted_slot = sorted_slot;
+  a.slot_pos = slot_pos;
   a.T = T;
   a.E = E;
   a.K = K;
@@ -210,9 +212,7 @@ pw_status pw_route_grouped(const void* logits, int logit_type, const float* bias
   a.renorm = renorm;
   a.n_shared = n_shared;
   a.w_scale = w_scale;
-  const pw_status s = launched(pw::launch_route_grouped(a, st), "router launch");
-  if (s != PW_OK) return s;
-  return launched(pw::launch_permute(ids, T, Kt, E + n_shared, offsets, sorted_slot, slot_pos, st), "permute launch");
+  return launched(pw::launch_route_grouped(a, static_cast<hipStream_t>(stream)), "router launch");
 }
 
 }  // extern "C"

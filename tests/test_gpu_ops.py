@@ -510,6 +510,19 @@ def test_route_near_ties_follow_64_bits():
     _check_route(-x, 8, score="sigmoid", groups=8, top_groups=4, group_top=2)
 
 
+@pytest.mark.parametrize("T,E,K,n_shared", [(2048, 64, 8, 0), (2731, 250, 5, 1), (4099, 256, 8, 0), (40000, 16, 7, 0)])
+def test_route_many_slots(T, E, K, n_shared):
+    """Permutations of many slots, in parts of 512 and more; the choice is checked
+    by the other tests (few experts tie here)."""
+    logits = torch.randn(T, E, generator=_gen(T)).cuda()
+    ids, w, off, ss, sp = _ops().route_grouped(logits, K, n_shared=n_shared)
+    top = torch.sort(logits.double(), dim=1, descending=True, stable=True).indices[:, :K]
+    assert torch.equal(ids[:, :K].long(), top)
+    o, order, pos = R.permute(ids.cpu().numpy(), E + n_shared)
+    assert np.array_equal(off.cpu().numpy(), o)
+    assert np.array_equal(ss.cpu().numpy(), order) and np.array_equal(sp.cpu().numpy(), pos)
+
+
 def test_route_no_tokens():
     ids, w, off, _, _ = _ops().route_grouped(torch.empty(0, 16, device="cuda"), 4)
     assert ids.shape == (0, 4) and (off.cpu() == 0).all()
