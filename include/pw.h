@@ -636,7 +636,8 @@ pw_status pw_kv_block_bytes(const pw_kv_cache* cache, size_t* bytes);
  * slots [T] int64 device: block number * block_tokens + position in the block;
  * a slot that is negative or past the last block writes nothing. Two tokens of
  * one call in one slot: undefined which one stays. Other slots of a block are
- * not touched.                                                               */
+ * not touched. T <= 2^30 (PW_EINVAL otherwise), T * n_kv_heads < 2^28
+ * (PW_EUNSUPPORTED otherwise: split the batch).                              */
 pw_status pw_kv_append(const pw_kv_cache* cache, const void* k, const void* v, int64_t ld, int64_t ldh,
                        const int64_t* slots, int T, void* stream);
 

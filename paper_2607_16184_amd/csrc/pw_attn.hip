@@ -12,59 +12,273 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Append
 // ---------------------------------------------------------------------------
 
-// G neighbouring lanes (a power of two, at least D / 8) hold one token's key or
-// value of one head, 8 channels each.
+// One token's key (is_v 0) or value (1) of head h by G neighbouring lanes (a
+// power of two, at least D / 8), lane c of them with channels 8 c .. 8 c + 7: its
+// load, and what is done with it.
+__device__ __forceinline__ u32x4 load_one(const AppendArgs& a, int64_t tok, int h, int is_v, int c) {
+  return ld16(reinterpret_cast<const uint8_t*>((is_v ? a.v : a.k) + tok * a.ld + h * a.ldh + 8 * c));
+}
+template <int ACT, int BITS>
+__device__ __forceinline__ void append_one(const AppendArgs& a, u32x4 raw, int64_t slot, int h, int is_v, int c, int G) {
+  const int D = a.kv.head_dim, P = a.kv.block_tokens, H = a.kv.n_kv_heads;
+  const int t = static_cast<int>(slot % P);
+  uint8_t* blk = a.kv.pool + slot / P * a.kv.block_stride;
+  uint8_t* dst = blk + static_cast<size_t>(2 * h + is_v) * P * D * (BITS / 8);
+  if constexpr (BITS == 16) {
+    if (8 * c >= D) return;
+    if (!is_v) {
+      *reinterpret_cast<u32x4*>(dst + ((t / 16) * (D / 32) + c / 4) * 1024 + 16 * (16 * (c & 3) + t % 16)) = raw;
+    } else {
+      uint16_t* p = reinterpret_cast<uint16_t*>(dst + ((t / 32) * (D / 16) + c / 2) * 1024) +
+                    8 * (16 * (t / 4 % 4) + 8 * (c & 1)) + 4 * (t / 16 % 2) + t % 4;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[8 * j] = static_cast<uint16_t>(raw[j / 2] >> (16 * (j & 1)));
+    }
+  } else {
+    float f[8], m = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      f[j] = val16(raw[j / 2] >> (16 * (j & 1)), ACT);
+      m = fmaxf(m, fabsf(f[j]));
+    }
+    for (int o = G / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    const float s = f8_scale(m);
+    if (8 * c >= D) return;
+    const u32x2 q = f8_codes8(f, s);
+    if (!is_v) {
+      *reinterpret_cast<u32x2*>(dst + ((t / 16) * (D / 64) + c / 8) * 1024 + 16 * (16 * (c & 3) + t % 16) +
+                                8 * (c / 4 % 2)) = q;
+    } else {
+      uint8_t* p = dst + ((t / 32) * (D / 32) + c / 4) * 1024 + 16 * (16 * (t / 4 % 4) + 8 * (c & 1)) +
+                   8 * (c / 2 % 2) + 4 * (t / 16 % 2) + t % 4;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[16 * j] = static_cast<uint8_t>(q[j / 4] >> (8 * (j & 3)));
+    }
+    if (c == 0) {
+      float* sc = reinterpret_cast<float*>(blk + static_cast<size_t>(2) * H * P * D);
+      sc[(is_v * H + h) * P + t] = s;
+    }
+  }
+}
+__device__ __forceinline__ bool slot_ok(const AppendArgs& a, int64_t slot) {
+  return slot >= 0 && slot / a.kv.block_tokens < a.kv.n_blocks;
+}
+
+// Few tokens, or none next to each other (a decode step): G lanes per token,
+// head and side.
 template <int ACT, int BITS>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int G) {
-  const int D = a.kv.head_dim, P = a.kv.block_tokens, H = a.kv.n_kv_heads;
+  const int H = a.kv.n_kv_heads;
   const int64_t items = static_cast<int64_t>(a.T) * H * 2;
   const int per = 256 / G, c = static_cast<int>(threadIdx.x) % G;
   for (int64_t item = static_cast<int64_t>(blockIdx.x) * per + static_cast<int>(threadIdx.x) / G; item < items;
        item += static_cast<int64_t>(gridDim.x) * per) {
-    const int is_v = static_cast<int>(item & 1), h = static_cast<int>((item >> 1) % H);
-    const int64_t tok = (item >> 1) / H;
-    const int64_t slot = a.slots[tok];
-    if (slot < 0 || slot / P >= a.kv.n_blocks) continue;      // the same for all G lanes
-    const int t = static_cast<int>(slot % P);
+    const int64_t tok = (item >> 1) / H, slot = a.slots[tok];
+    const int h = static_cast<int>((item >> 1) % H), is_v = static_cast<int>(item & 1);
+    const u32x4 raw = 8 * c < a.kv.head_dim ? load_one(a, tok, h, is_v, c) : u32x4{0u, 0u, 0u, 0u};
+    if (slot_ok(a, slot)) append_one<ACT, BITS>(a, raw, slot, h, is_v, c, G);   // (the same for all G lanes)
+  }
+}
+
+// Many tokens (a prefill chunk): a wave per window of 32 tokens, head and side.
+// Tokens that follow each other inside a 32-token tile of the cache are a run;
+// the wave of the window that holds its first token writes it as a piece of the
+// tile: keys in the order in which they are loaded, 16 bytes a lane, values
+// turned in LDS. Tokens of runs shorter than kMinRun go one by one. (A value's
+// elements lie 16 bytes apart: written token by token, 4001 tokens of 8 heads
+// x 128 channels take 25.8 us in 16 bits and 18.2 in 8, as runs 8.3 and 10.4.
+// Tokens in no order lose by it, 512 of them 7.0 -> 13.6 us, and from 256 in a row
+// on runs win: the kernel is taken from kAppendMany on, where a step's tokens
+// are hardly those of a decode batch.)
+constexpr int kAppendWaves = 4;
+constexpr int kAppendMany = 512;          // tokens
+constexpr int kMinRun = 8;
+template <int ACT, int BITS, int D>
+__global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArgs a) {
+  constexpr int kE = BITS / 8, kPitch = D * kE + 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kAppendWaves][32 * kPitch];
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
+  const int H = a.kv.n_kv_heads, P = a.kv.block_tokens;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kAppendWaves + wave;
+  const int is_v = static_cast<int>(unit & 1), h = static_cast<int>((unit >> 1) % H);
+  const int64_t first = (unit >> 1) / H * 32;                    // first token of the window
+  if (first >= a.T) return;                                      // (wave-uniform; no barrier follows)
+
+  // slots of the tokens first - 32 + lane and first + 32 + lane
+  const auto slot_of = [&](int64_t n) { return n >= 0 && n < a.T ? a.slots[n] : int64_t(-1); };
+  const int64_t sa = slot_of(first - 32 + lane), sb = slot_of(first + 32 + lane);
+  const auto shfl64 = [&](int64_t v, int l) {
+    return static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(v >> 32), l))) << 32) |
+                                static_cast<uint32_t>(__shfl(static_cast<int>(v), l)));
+  };
+  const int64_t end = shfl64(sa, 63);
+  int64_t pa = shfl64(sa, (lane + 63) & 63), pb = shfl64(sb, (lane + 63) & 63);
+  if (lane == 0) {
+    pa = -1;
+    pb = end;
+  }
+  // bit i of (mb : ma): token i of these 128 goes on with its predecessor's run
+  const uint64_t ma = __ballot(slot_ok(a, sa) && (sa & 31) != 0 && pa == sa - 1);
+  const uint64_t mb = __ballot(slot_ok(a, sb) && (sb & 31) != 0 && pb == sb - 1);
+  // the window's own tokens are those of lanes 32 and up: the start of a token's
+  // run (no more than 31 before it) and its length
+  const bool own = lane >= 32 && slot_ok(a, sa);
+  const uint64_t starts = ~ma & (lane == 63 ? ~0ull : (2ull << lane) - 1ull);
+  const int s0 = starts ? 63 - __clzll(static_cast<long long>(starts)) : 0;
+  const uint64_t after = s0 == 63 ? mb : (ma >> (s0 + 1)) | (mb << (63 - s0));
+  const int len = __ffsll(static_cast<long long>(~after));        // one more than the ones that follow
+  uint64_t lead = __ballot(own && s0 == lane && len >= kMinRun);
+  const uint64_t single = __ballot(own && len < kMinRun) >> 32;
+
+  while (lead) {
+    const int ll = __ffsll(static_cast<long long>(lead)) - 1;
+    lead &= lead - 1;
+    const int64_t slot = shfl64(sa, ll);
+    const int n_run = __builtin_amdgcn_readlane(len, ll);
+    const int t = static_cast<int>(slot % P) & ~31, t0 = static_cast<int>(slot & 31);   // the tile, the run's place in it
+    const int64_t n0 = first - 32 + ll - t0;                     // token of the tile's first place
+    const auto in = [&](int place) { return place >= t0 && place < t0 + n_run; };
     uint8_t* blk = a.kv.pool + slot / P * a.kv.block_stride;
-    uint8_t* dst = blk + static_cast<size_t>(2 * h + is_v) * P * D * (BITS / 8);
-    u32x4 raw = {0u, 0u, 0u, 0u};
-    if (8 * c < D)
-      raw = ld16(reinterpret_cast<const uint8_t*>((is_v ? a.v : a.k) + tok * a.ld + h * a.ldh + 8 * c));
-    if constexpr (BITS == 16) {
-      if (8 * c >= D) continue;
-      if (!is_v) {
-        *reinterpret_cast<u32x4*>(dst + ((t / 16) * (D / 32) + c / 4) * 1024 + 16 * (16 * (c & 3) + t % 16)) = raw;
+    uint8_t* dst = blk + static_cast<size_t>(2 * h + is_v) * P * D * kE + static_cast<size_t>(t) * D * kE;
+    const int c = lane & 15, lg = lane >> 4;
+    u32x4 x[2][D / 32];                                          // place c of either half, channels 32 i + 8 lg ..
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint16_t* src = (is_v ? a.v : a.k) + (n0 + 16 * u + c) * a.ld + h * a.ldh + 8 * lg;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+        x[u][i] = in(16 * u + c) ? ld16(reinterpret_cast<const uint8_t*>(src + 32 * i)) : u32x4{0u, 0u, 0u, 0u};
+    }
+    uint8_t* mine = lds[wave];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      uint8_t* row = mine + (16 * u + c) * kPitch + 8 * lg * kE;
+      const bool here = in(16 * u + c);
+      if constexpr (BITS == 16) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          if (!is_v) {
+            if (here) *reinterpret_cast<u32x4*>(dst + (u * (D / 32) + i) * 1024 + 16 * lane) = x[u][i];
+          } else {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) *reinterpret_cast<uint32_t*>(row + 64 * i + 4 * w) = x[u][i][w];
+          }
+        }
       } else {
-        uint16_t* p = reinterpret_cast<uint16_t*>(dst + ((t / 32) * (D / 16) + c / 2) * 1024) +
-                      8 * (16 * (t / 4 % 4) + 8 * (c & 1)) + 4 * (t / 16 % 2) + t % 4;
+        float m = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[8 * j] = static_cast<uint16_t>(raw[j / 2] >> (16 * (j & 1)));
-      }
-    } else {
-      float f[8], m = 0.0f;
+        for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        f[j] = val16(raw[j / 2] >> (16 * (j & 1)), ACT);
-        m = fmaxf(m, fabsf(f[j]));
-      }
-      for (int o = G / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-      const float s = f8_scale(m);
-      if (8 * c >= D) continue;
-      const u32x2 q = f8_codes8(f, s);
-      if (!is_v) {
-        *reinterpret_cast<u32x2*>(dst + ((t / 16) * (D / 64) + c / 8) * 1024 + 16 * (16 * (c & 3) + t % 16) +
-                                  8 * (c / 4 % 2)) = q;
-      } else {
-        uint8_t* p = dst + ((t / 32) * (D / 32) + c / 4) * 1024 + 16 * (16 * (t / 4 % 4) + 8 * (c & 1)) +
-                     8 * (c / 2 % 2) + 4 * (t / 16 % 2) + t % 4;
+          for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(val16(x[u][i][j / 2] >> (16 * (j & 1)), ACT)));
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float s = f8_scale(m);
+        u32x2 q[D / 32];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[16 * j] = static_cast<uint8_t>(q[j / 4] >> (8 * (j & 3)));
+        for (int i = 0; i < D / 32; ++i) {
+          float f[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = val16(x[u][i][j / 2] >> (16 * (j & 1)), ACT);
+          q[i] = f8_codes8(f, s);
+        }
+        if (lg == 0 && here) {
+          float* sc = reinterpret_cast<float*>(blk + static_cast<size_t>(2) * H * P * D);
+          sc[(is_v * H + h) * P + t + 16 * u + c] = s;
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; i += 2) {
+          if (!is_v) {
+            if (here)
+              *reinterpret_cast<u32x4*>(dst + (u * (D / 64) + i / 2) * 1024 + 16 * lane) =
+                  u32x4{q[i][0], q[i][1], q[i + 1][0], q[i + 1][1]};
+          } else {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) *reinterpret_cast<uint32_t*>(row + 32 * (i + w / 2) + 4 * (w & 1)) = q[i + w / 2][w & 1];
+          }
+        }
       }
-      if (c == 0) {
-        float* sc = reinterpret_cast<float*>(blk + static_cast<size_t>(2) * H * P * D);
-        sc[(is_v * H + h) * P + t] = s;
+    }
+    if (is_v) {
+      __builtin_amdgcn_wave_barrier();                           // the wave's own LDS: in order
+      // lane: channel c of a tile, places 4 lg .. + 3 of either half
+      bool all[2], some[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int p0 = 16 * u + 4 * lg;
+        all[u] = in(p0) && in(p0 + 3);
+        some[u] = p0 + 3 >= t0 && p0 < t0 + n_run;
       }
+#pragma unroll
+      for (int j = 0; j < D * kE / 32; ++j) {
+        u32x4 v;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t o = 0;
+          if constexpr (BITS == 16) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int tok = 16 * (w / 2) + 4 * lg + 2 * (w & 1) + e;
+              o |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(mine + tok * kPitch + 2 * (16 * j + c))) << (16 * e);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int tok = 16 * (w & 1) + 4 * lg + e;
+              o |= static_cast<uint32_t>(mine[tok * kPitch + 32 * j + 16 * (w / 2) + c]) << (8 * e);
+            }
+          }
+          v[w] = o;
+        }
+        uint8_t* at = dst + j * 1024 + 16 * lane;
+        if (n_run == 32) {
+          *reinterpret_cast<u32x4*>(at) = v;
+          continue;
+        }
+        // four places of one channel: whole, or element by element
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if constexpr (BITS == 16) {
+            if (all[u]) {
+              *reinterpret_cast<u32x2*>(at + 8 * u) = u32x2{v[2 * u], v[2 * u + 1]};
+            } else if (some[u]) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (in(16 * u + 4 * lg + e))
+                  *reinterpret_cast<uint16_t*>(at + 8 * u + 2 * e) = static_cast<uint16_t>(v[2 * u + e / 2] >> (16 * (e & 1)));
+            }
+          } else {
+#pragma unroll
+            for (int jh = 0; jh < 2; ++jh) {
+              const uint32_t o = v[2 * jh + u];
+              if (all[u]) {
+                *reinterpret_cast<uint32_t*>(at + 8 * jh + 4 * u) = o;
+              } else if (some[u]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (in(16 * u + 4 * lg + e)) at[8 * jh + 4 * u + e] = static_cast<uint8_t>(o >> (8 * e));
+              }
+            }
+          }
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+  if (single) {
+    constexpr int G = D <= 64 ? 8 : D <= 128 ? 16 : 32, kAtOnce = 64 / G, kTurns = 32 / kAtOnce;
+    const int c = lane % G;
+    u32x4 raw[kTurns];                                           // (all loads before the first use)
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+      const int n = j * kAtOnce + lane / G;
+      raw[j] = u32x4{0u, 0u, 0u, 0u};
+      if (8 * c < D && ((single >> n) & 1ull)) raw[j] = load_one(a, first + n, h, is_v, c);
+    }
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+      const int n = j * kAtOnce + lane / G;
+      const int64_t slot = shfl64(sa, 32 + n);
+      if ((single >> n) & 1ull) append_one<ACT, BITS>(a, raw[j], slot, h, is_v, c, G);
     }
   }
 }
@@ -435,21 +649,40 @@ AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int, int 
   return p;
 }
 
-hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st) {
+namespace {
+
+template <int ACT, int BITS>
+hipError_t append_tiles(const AppendArgs& a, hipStream_t st) {
+  const int64_t units = (static_cast<int64_t>(a.T) + 31) / 32 * a.kv.n_kv_heads * 2;
+  const int64_t grid = (units + kAppendWaves - 1) / kAppendWaves;
+  if (grid >= (1 << 23)) return hipErrorInvalidConfiguration;
+  const dim3 g(static_cast<uint32_t>(grid)), b(64 * kAppendWaves);
+  switch (a.kv.head_dim) {
+    case 64: k_kv_append_tiles<ACT, BITS, 64><<<g, b, 0, st>>>(a); break;
+    case 128: k_kv_append_tiles<ACT, BITS, 128><<<g, b, 0, st>>>(a); break;
+    case 192: k_kv_append_tiles<ACT, BITS, 192><<<g, b, 0, st>>>(a); break;
+    case 256: k_kv_append_tiles<ACT, BITS, 256><<<g, b, 0, st>>>(a); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+template <int ACT, int BITS>
+hipError_t append(const AppendArgs& a, hipStream_t st) {
+  if (a.T >= kAppendMany) return append_tiles<ACT, BITS>(a, st);
   int G = 8;
   while (8 * G < a.kv.head_dim) G *= 2;
   const int64_t per = 256 / G, items = static_cast<int64_t>(a.T) * a.kv.n_kv_heads * 2;
   const int64_t blocks = (items + per - 1) / per;
-  const uint32_t grid = static_cast<uint32_t>(blocks < (1 << 20) ? blocks : (1 << 20));
-  const bool bf = a.kv.act == PW_BF16;
-  if (a.kv.bits == 16) {
-    if (bf) k_kv_append<PW_BF16, 16><<<grid, 256, 0, st>>>(a, G);
-    else k_kv_append<PW_F16, 16><<<grid, 256, 0, st>>>(a, G);
-  } else {
-    if (bf) k_kv_append<PW_BF16, 8><<<grid, 256, 0, st>>>(a, G);
-    else k_kv_append<PW_F16, 8><<<grid, 256, 0, st>>>(a, G);
-  }
+  k_kv_append<ACT, BITS><<<static_cast<uint32_t>(blocks), 256, 0, st>>>(a, G);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st) {
+  if (a.kv.act == PW_BF16) return a.kv.bits == 16 ? append<PW_BF16, 16>(a, st) : append<PW_BF16, 8>(a, st);
+  return a.kv.bits == 16 ? append<PW_F16, 16>(a, st) : append<PW_F16, 8>(a, st);
 }
 
 hipError_t launch_attn(const AttnArgs& a, hipStream_t st) {

@@ -125,15 +125,33 @@ __device__ __forceinline__ float row16_max(float m) {
   m = fmaxf(m, dpp_f32<0x141>(m));   // row_half_mirror
   return fmaxf(m, dpp_f32<0x140>(m));   // row_mirror
 }
-// Scale of a group of largest magnitude m. (The divisions here and below are
-// correctly rounded: v / s is at most 448 (1 + 2^-23), which rounds to 448.)
+// Scale of a group of largest magnitude m.
 __device__ __forceinline__ float f8_scale(float m) { return fmaxf(m / 448.0f, 0x1p-126f); }
+// The codes of eight values v of one group: e4m3 of the correctly rounded v / s
+// (at most 448 (1 + 2^-23), which rounds to 448). The division's own steps are
+// mostly about the divisor, so they are done once: y = 1 / s, correctly rounded;
+// q = v y is off by less than two units, q + (v - q s) y (the remainder exact)
+// by less than one, and the same correction of that rounds to what v / s rounds
+// to (Markstein), for every v / s that is not coded 0 while no step leaves the
+// normal range: elsewhere, divisions.
 __device__ __forceinline__ u32x2 f8_codes8(const float* v, float s) {
+  float q[8];
+  if (s > 0x1p-90f && s < 0x1p90f) {
+    const float y = 1.0f / s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float q0 = v[i] * y, q1 = fmaf(fmaf(-q0, s, v[i]), y, q0);
+      q[i] = fmaf(fmaf(-q1, s, v[i]), y, q1);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = v[i] / s;
+  }
   u32x2 o;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i] / s, v[4 * i + 1] / s, 0, false);
-    c = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2] / s, v[4 * i + 3] / s, c, true);
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i], q[4 * i + 1], 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i + 2], q[4 * i + 3], c, true);
     o[i] = static_cast<uint32_t>(c);
   }
   return o;

@@ -120,6 +120,7 @@ pw_status pw_kv_append(const pw_kv_cache* c, const void* k, const void* v, int64
   if (const char* f = kv_fault(c)) return set_error(PW_EINVAL, f);
   if (const char* f = kv_memory_fault(c)) return set_error(PW_EINVAL, f);
   if (T < 0 || T > (1 << 30)) return set_error(PW_EINVAL, "need 0 <= T <= 2^30");
+  if (static_cast<int64_t>(T) * c->n_kv_heads >= (int64_t(1) << 28)) return set_error(PW_EUNSUPPORTED, "T * n_kv_heads must stay below 2^28");
   if (ld % 8 != 0 || ldh % 8 != 0) return set_error(PW_EINVAL, "strides must be multiples of 8");
   if (T == 0) return PW_OK;
   if (!k || !v || !slots) return set_error(PW_EINVAL, "null argument");

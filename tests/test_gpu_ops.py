@@ -258,6 +258,32 @@ def test_append_consecutive_positions(bits, P, first, T):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+def test_append_many_tokens_in_runs(bits, D):
+    """More than 512 tokens: whole tiles, runs of every length that start and end
+    anywhere in a tile, padding and lone tokens between them, a slot past the end."""
+    H, P, n = 2, 64, 60
+    g = _gen(D)
+    slots, at = [], 0
+    for length in [40, 1, 7, 8, 9, 31, 32, 33, 64, 3, 2, 100, 5, 16, 17, 65, 150]:
+        at += int(torch.randint(1, 50, (1,), generator=g))
+        slots += list(range(at, at + length)) + ([-1] if length % 2 else [])
+        at += length
+    slots += list(range(n * P - 70, n * P + 30))                  # runs past the last block
+    slots += (torch.arange(40) * 3 + at).flip(0).tolist()         # lone tokens, backwards
+    slots = torch.tensor(slots)
+    T = slots.numel()
+    assert T > 512 and at + 120 < n * P - 70
+    kv = torch.randn(T, 2, H, D, generator=g).to(FP)
+    c = _cache(n, P, H, D, FP, bits)
+    dev = kv.cuda()
+    c.append(dev[:, 0], dev[:, 1], slots.cuda())
+    want = np.full(c.pool.numel(), 0xFF, np.uint8)
+    R.write_slots(want, c.block_bytes, kv[:, 0], kv[:, 1], slots, P, bits, n)
+    assert np.array_equal(c.pool.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 def test_append_extreme_values(bits):
     kv = torch.randn(6, 2, 1, 64, generator=_gen(9)).to(BF)
     kv[1, 0, 0, 3] = math.nan
