@@ -659,8 +659,8 @@ pw_status pw_kv_append(const pw_kv_cache* cache, const void* k, const void* v, i
  * the cache outside the attended positions is not used, NaN and infinities
  * included. Scores, softmax and sums are in fp32.
  * Constraints: B >= 0; n_q_heads a multiple of n_kv_heads; max_len >= 0, below
- * 2^31 - 256; window >= 0; scale finite (PW_EINVAL otherwise); B *
- * n_q_heads < 2^23 (PW_EUNSUPPORTED: split the batch).
+ * 2^31 - 256; window >= 0; scale finite (PW_EINVAL otherwise); B and
+ * n_q_heads < 65536, their product < 2^23 (PW_EUNSUPPORTED: split the batch).
  * ws: device workspace of at least pw_attn_workspace bytes, 16-byte aligned
  * (PW_ENOMEM below; may be NULL where that is 0), in use until `stream` passes
  * the call. Deterministic: the split of a sequence and the order of the joins

@@ -311,18 +311,51 @@ constexpr int kAttnWaves = 4;
 constexpr float kNoMax = -1e30f;      // below every score, and exp2(-inf - it) = 0
 constexpr float kSlack = 8.0f;
 
-// Attended positions [lo, hi) of sequence b, and their tiles.
+// Attended positions [lo, hi) of a sequence of n cached tokens, and their tiles.
 struct Span {
   int lo, hi, t0, tiles;
 };
-__device__ __forceinline__ Span span_of(const AttnArgs& a, int b) {
+__device__ __forceinline__ Span span_of(const AttnArgs& a, int n) {
   Span s;
-  const int n = a.lens[b];
   s.hi = n < 0 ? 0 : (n > a.max_len ? a.max_len : n);
   s.lo = a.window > 0 && s.hi > a.window ? s.hi - a.window : 0;
   s.t0 = s.lo / kTile;
   s.tiles = (s.hi + kTile - 1) / kTile - s.t0;
   return s;
+}
+
+// How the work is cut. An item is one sequence, key head and tile of 16 query
+// heads; its tiles go to one or more workgroups, whose partial results lie in
+// consecutive slots.
+//   split (a.n_splits > 0): workgroup (split, item) takes split_tiles tiles.
+//   shares (a.n_splits = 0): all items' tiles form one line, cut into equal
+//     shares, one per workgroup, wherever the items end: sequences of unlike
+//     lengths leave no workgroup with more than another. Workgroup w's part of
+//     item i lies in slot w + i (one of the two grows from part to part).
+// Sequence lengths are read on the device in both, and nothing else decides.
+constexpr int kShareBatch = 1024;     // sequences that the shares' sums take
+
+// Tiles of the sequences before b and of all of them, in every lane (B <=
+// kShareBatch).
+__device__ __forceinline__ void tiles_before(const AttnArgs& a, int b, int lane, int* before, int* all) {
+  int x = 0, y = 0;
+  for (int i = lane; i < a.B; i += 64) {
+    const int n = span_of(a, a.lens[i]).tiles;
+    y += n;
+    x += i < b ? n : 0;
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    x += __shfl_xor(x, o);
+    y += __shfl_xor(y, o);
+  }
+  *before = x;
+  *all = y;
+}
+// Tiles of a share: a multiple of the waves, all of them equally loaded.
+__device__ __forceinline__ int share_of(const AttnArgs& a, int tiles, int items_per_seq) {
+  const int total = tiles * items_per_seq, r = (total + a.n_shares - 1) / a.n_shares;
+  return (r + kAttnWaves - 1) / kAttnWaves * kAttnWaves;
 }
 
 // Two e4m3 codes (the low or high half of a word) as two 16-bit values.
@@ -338,28 +371,37 @@ __device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi) {
   return u32x4{widen2<ACT, false>(lo), widen2<ACT, true>(lo), widen2<ACT, false>(hi), widen2<ACT, true>(hi)};
 }
 
+// Block number of a tile of sequence b (counted from position 0); -1 past max_len.
+__device__ __forceinline__ int block_at(const AttnArgs& a, int b, int tile) {
+  const int most = (a.max_len + kTile - 1) / kTile;
+  if (tile >= most) return -1;
+  return a.table[b * a.ld_table + (static_cast<int64_t>(tile) * kTile >> __builtin_ctz(a.kv.block_tokens))];   // (a power of two)
+}
+
+template <int D>
+struct AttnLds {
+  float o[kAttnWaves][16][D + 4];
+  float m[kAttnWaves][16], l[kAttnWaves][16];
+};
+
+// Tiles [begin, end) of a sequence's span for one key head h and its query
+// heads 16 qt and up, by the workgroup. ids: block numbers of the wave's first
+// 64 tiles, one per lane. whole: no other workgroup has tiles of the item, the
+// result goes to the output; else to slot `slot`.
 template <int ACT, int BITS, int D>
-__global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(AttnArgs a, int q_tiles) {
+__device__ __forceinline__ void attend(const AttnArgs& a, AttnLds<D>& lds, int b, int h, int qt, const Span& sp, int begin,
+                                       int end, int ids, bool whole, int64_t slot) {
   constexpr int kPv = BITS == 8 ? PW_BF16 : ACT;      // 16-bit type of the second product
   constexpr int kLoads = D * BITS / 8 * 16 / 1024;    // 1 KB loads of 16 tokens' keys
-  constexpr int kPad = D + 4;
-  __shared__ float lds_o[kAttnWaves][16][kPad];
-  __shared__ float lds_m[kAttnWaves][16], lds_l[kAttnWaves][16];
-
-  const int split = static_cast<int>(blockIdx.x) % a.n_splits, item = static_cast<int>(blockIdx.x) / a.n_splits;
-  const int qt = item % q_tiles, h = item / q_tiles % a.kv.n_kv_heads;
-  const int b = item / q_tiles / a.kv.n_kv_heads;
-  const Span sp = span_of(a, b);
-  const int n_act = (sp.tiles + a.split_tiles - 1) / a.split_tiles;
-  if (split > 0 && split >= n_act) return;
-
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
   const int col = lane & 15, lg = lane >> 4;
+  const int P = a.kv.block_tokens;
+  const int first = begin + wave;                                // the wave's tiles: first, first + 4, ...
+  const int n_my = first < end ? (end - first + kAttnWaves - 1) / kAttnWaves : 0;
+
   const int g = a.n_q_heads / a.kv.n_kv_heads;
   const int n_col = g - 16 * qt < 16 ? g - 16 * qt : 16;
   const int hq0 = h * g + 16 * qt;
-  const int P = a.kv.block_tokens, p_shift = __builtin_ctz(P);   // a power of two
-
   u32x4 q[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
@@ -368,31 +410,36 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
       q[i] = ld16(reinterpret_cast<const uint8_t*>(a.q + b * a.ldq + (hq0 + col) * a.ldqh + 32 * i + 8 * lg));
   }
 
-  const int first = split * a.split_tiles + wave;                 // the wave's tiles: first, first + 4, ...
-  int end = (split + 1) * a.split_tiles;
-  end = end < sp.tiles ? end : sp.tiles;
-  const int n_my = first < end ? (end - first + kAttnWaves - 1) / kAttnWaves : 0;
-  const int32_t* table = a.table + b * a.ld_table;
+  // The tiles in blocks of the pool, one after the other (tiles in other blocks
+  // are left out): bits of the 64 numbers at hand, then the next 64.
+  int chunk = 0;
+  uint64_t todo = __ballot(lane < n_my && ids >= 0 && ids < a.kv.n_blocks);
+  int next_t = -1, next_id = 0;                                  // first token of the next tile (-1: none), its block
+  const auto advance = [&] {
+    while (todo == 0 && chunk + 64 < n_my) {
+      chunk += 64;
+      ids = chunk + lane < n_my ? block_at(a, b, sp.t0 + first + kAttnWaves * (chunk + lane)) : -1;
+      todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
+    }
+    next_t = -1;
+    if (todo) {
+      const int l = __ffsll(static_cast<long long>(todo)) - 1;
+      todo &= todo - 1;
+      next_id = __builtin_amdgcn_readlane(ids, l);
+      next_t = (sp.t0 + first + kAttnWaves * (chunk + l)) * kTile;
+    }
+  };
   const size_t head_off = static_cast<size_t>(2 * h) * P * D * (BITS / 8);
   const size_t v_off = static_cast<size_t>(P) * D * (BITS / 8);
-  const size_t sc_off = static_cast<size_t>(2) * a.kv.n_kv_heads * P * D + (static_cast<size_t>(h) * P + 4 * lg) * 4;
+  const size_t sc_off = static_cast<size_t>(2) * a.kv.n_kv_heads * P * D + static_cast<size_t>(h) * P * 4;
+  const size_t vs_off = static_cast<size_t>(a.kv.n_kv_heads) * P * 4;
   const float scale2 = a.scale * kLog2e;
 
   u32x4 k[2][kLoads], v[2 * kLoads];
   f32x4 ks[2], vs[2];
-  const auto tile_of = [&](int i) { return sp.t0 + first + kAttnWaves * i; };
-  // block numbers of the wave's next 64 tiles, one per lane
-  int ids = 0;
-  const auto fetch_ids = [&](int i) {
-    const int j = i + lane;
-    ids = j < n_my ? table[tile_of(j) * kTile >> p_shift] : -1;
-  };
-  const auto block_of = [&](int i) { return __builtin_amdgcn_readlane(ids, i & 63); };
-  const auto ok = [&](int id) { return id >= 0 && id < a.kv.n_blocks; };
-  const auto load_k = [&](int i, int id) {
-    if (!ok(id)) return;
-    const int t = tile_of(i) * kTile & (P - 1);                         // first token in the block
-    const uint8_t* blk = a.kv.pool + static_cast<int64_t>(id) * a.kv.block_stride;
+  const auto load_k = [&] {
+    const int t = next_t & (P - 1);                              // in the block
+    const uint8_t* blk = a.kv.pool + static_cast<int64_t>(next_id) * a.kv.block_stride;
     const uint8_t* p = blk + head_off + static_cast<size_t>(t) * D * (BITS / 8) + 16 * lane;
 #pragma unroll
     for (int r = 0; r < 2; ++r)
@@ -400,21 +447,18 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
       for (int j = 0; j < kLoads; ++j) k[r][j] = ld16_nt(p + (r * kLoads + j) * 1024);
     if constexpr (BITS == 8) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
-        ks[r] = *reinterpret_cast<const f32x4*>(blk + sc_off + 4 * t + 64 * r);
+      for (int r = 0; r < 2; ++r) ks[r] = *reinterpret_cast<const f32x4*>(blk + sc_off + 4 * t + 16 * lg + 64 * r);
     }
   };
-  const auto load_v = [&](int i, int id) {
-    if (!ok(id)) return;
-    const int t = tile_of(i) * kTile & (P - 1);
-    const uint8_t* blk = a.kv.pool + static_cast<int64_t>(id) * a.kv.block_stride;
+  const auto load_v = [&] {
+    const int t = next_t & (P - 1);
+    const uint8_t* blk = a.kv.pool + static_cast<int64_t>(next_id) * a.kv.block_stride;
     const uint8_t* p = blk + head_off + v_off + static_cast<size_t>(t) * D * (BITS / 8) + 16 * lane;
 #pragma unroll
     for (int j = 0; j < 2 * kLoads; ++j) v[j] = ld16_nt(p + j * 1024);
     if constexpr (BITS == 8) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
-        vs[r] = *reinterpret_cast<const f32x4*>(blk + sc_off + static_cast<size_t>(a.kv.n_kv_heads) * P * 4 + 4 * t + 64 * r);
+      for (int r = 0; r < 2; ++r) vs[r] = *reinterpret_cast<const f32x4*>(blk + sc_off + vs_off + 4 * t + 16 * lg + 64 * r);
     }
   };
 
@@ -423,14 +467,13 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
   for (int j = 0; j < D / 16; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = kNoMax, l = 0.0f;
 
-  int id = -1;
-  if (n_my > 0) {
-    fetch_ids(0);
-    id = block_of(0);
-    load_k(0, id);
-    load_v(0, id);
+  advance();
+  if (next_t >= 0) {
+    load_k();
+    load_v();
   }
-  for (int i = 0; i < n_my; ++i) {
+  while (next_t >= 0) {
+    const int t = next_t;
     f32x4 s[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -447,33 +490,33 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
     for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[r][e] *= BITS == 8 ? scale2 * ks[r][e] : scale2;
-    f32x4 vsc[2];
-    if constexpr (BITS == 8) {
-      vsc[0] = vs[0];
-      vsc[1] = vs[1];
-    }
-    // a tile at either end of the span, or in a missing block: what lies
-    // outside is left out, whatever its bits
-    const int t = tile_of(i) * kTile;
-    const bool edge = t < sp.lo || t + kTile > sp.hi || !ok(id);
-    if (edge) {
+    // the tile at either end of the span: what lies outside is left out,
+    // whatever its bits
+    if (t < sp.lo || t + kTile > sp.hi) {
+      uint32_t keep[2][2];                                       // of four tokens' 8 or 16 bits
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
+        keep[r][0] = keep[r][1] = 0u;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int tok = t + 16 * r + 4 * lg + e;
-          const bool in = tok >= sp.lo && tok < sp.hi && ok(id);
+          const bool in = tok >= sp.lo && tok < sp.hi;
           s[r][e] = in ? s[r][e] : -INFINITY;
-          if constexpr (BITS == 8) vsc[r][e] = in ? vsc[r][e] : 0.0f;
+          if constexpr (BITS == 8) {
+            vs[r][e] = in ? vs[r][e] : 0.0f;
+            keep[r][0] |= in ? 0xFFu << (8 * e) : 0u;
+          } else {
+            keep[r][e / 2] |= in ? 0xFFFFu << (16 * (e & 1)) : 0u;
+          }
         }
       }
+#pragma unroll
+      for (int j = 0; j < 2 * kLoads; ++j)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[j][w] &= BITS == 8 ? keep[w & 1][0] : keep[w / 2][w & 1];
     }
-    int next = -1;
-    if (i + 1 < n_my) {
-      if (((i + 1) & 63) == 0) fetch_ids(i + 1);
-      next = block_of(i + 1);
-      load_k(i + 1, next);
-    }
+    advance();
+    if (next_t >= 0) load_k();
     float top = s[0][0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e / 4][e & 3]);
@@ -481,7 +524,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float m_new = fmaxf(m, top);
-      const float f = exp2f(m - m_new);
+      const float f = __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
       l *= f;
 #pragma unroll
@@ -496,9 +539,9 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int r = w / 2, x = 2 * (w & 1) + e;
-        p[e] = exp2f(s[r][x] - m);
+        p[e] = __builtin_amdgcn_exp2f(s[r][x] - m);
         l += p[e];
-        if constexpr (BITS == 8) p[e] *= vsc[r][x];
+        if constexpr (BITS == 8) p[e] *= vs[r][x];
       }
       p_hi[w] = pack16<kPv>(p[0], p[1]);
       p_lo[w] = pack16<kPv>(p[0] - val16(p_hi[w] & 0xFFFFu, kPv), p[1] - val16(p_hi[w] >> 16, kPv));
@@ -510,23 +553,10 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
         x = v[j];
       else
         x = widen8<kPv>(v[j / 2][2 * (j & 1)], v[j / 2][2 * (j & 1) + 1]);
-      if (edge) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          uint32_t keep = 0u;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int tok = t + 16 * (w / 2) + 4 * lg + 2 * (w & 1) + e;
-            if (tok >= sp.lo && tok < sp.hi && ok(id)) keep |= 0xFFFFu << (16 * e);
-          }
-          x[w] &= keep;
-        }
-      }
       o[j] = mma<kPv>(x, p_hi, o[j]);
       o[j] = mma<kPv>(x, p_lo, o[j]);
     }
-    if (i + 1 < n_my) load_v(i + 1, next);
-    id = next;
+    if (next_t >= 0) load_v();
   }
 
   // join the four waves
@@ -534,36 +564,37 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
   l += __shfl_xor(l, 32);
   if (col < n_col) {
     if (lg == 0) {
-      lds_m[wave][col] = m;
-      lds_l[wave][col] = l;
+      lds.m[wave][col] = m;
+      lds.l[wave][col] = l;
     }
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) *reinterpret_cast<f32x4*>(&lds_o[wave][col][16 * j + 4 * lg]) = o[j];
+    for (int j = 0; j < D / 16; ++j) *reinterpret_cast<f32x4*>(&lds.o[wave][col][16 * j + 4 * lg]) = o[j];
   }
   __syncthreads();
+  const int n_part = g < 16 ? g : 16;                            // rows of a slot
   for (int e = threadIdx.x; e < n_col * (D / 4); e += 64 * kAttnWaves) {
     const int c = e / (D / 4), d = 4 * (e % (D / 4));
-    float mx = lds_m[0][c];
+    float mx = lds.m[0][c];
 #pragma unroll
-    for (int w = 1; w < kAttnWaves; ++w) mx = fmaxf(mx, lds_m[w][c]);
+    for (int w = 1; w < kAttnWaves; ++w) mx = fmaxf(mx, lds.m[w][c]);
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     float sum = 0.0f;
 #pragma unroll
     for (int w = 0; w < kAttnWaves; ++w) {
-      const float f = exp2f(lds_m[w][c] - mx);
-      sum = fmaf(f, lds_l[w][c], sum);
-      const f32x4 x = *reinterpret_cast<const f32x4*>(&lds_o[w][c][d]);
+      const float f = __builtin_amdgcn_exp2f(lds.m[w][c] - mx);
+      sum = fmaf(f, lds.l[w][c], sum);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(&lds.o[w][c][d]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[j] = fmaf(f, x[j], acc[j]);
     }
-    const size_t row = static_cast<size_t>(b) * a.n_q_heads + hq0 + c;
-    if (n_act <= 1) {
+    if (whole) {
+      const size_t row = static_cast<size_t>(b) * a.n_q_heads + hq0 + c;
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       *reinterpret_cast<u32x2*>(a.out + row * D + d) =
           u32x2{pack16<ACT>(acc[0] * inv, acc[1] * inv), pack16<ACT>(acc[2] * inv, acc[3] * inv)};
       if (a.lse && d == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
     } else {
-      const size_t at = row * a.n_splits + split;
+      const size_t at = static_cast<size_t>(slot) * n_part + c;
       *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = acc;
       if (d == 0) {
         a.part_ml[2 * at] = mx;
@@ -573,43 +604,141 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(Attn
   }
 }
 
-// Joins the splits of one row (sequence and query head) per wave, in the
-// order of the splits.
+template <int ACT, int BITS, int D>
+__global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(AttnArgs a, int q_tiles) {
+  __shared__ AttnLds<D> lds;
+  const int split = blockIdx.x, b = blockIdx.z;
+  const int h = q_tiles == 1 ? blockIdx.y : blockIdx.y / q_tiles, qt = q_tiles == 1 ? 0 : blockIdx.y % q_tiles;
+  const int wave = static_cast<int>(threadIdx.x) >> 6, lane = lane_id();
+  const int begin = split * a.split_tiles;
+  // Without a window the block numbers do not hang on the sequence's length, so
+  // they come along with it (what lies past the length is dropped later).
+  int ids = a.window == 0 ? block_at(a, b, begin + wave + kAttnWaves * lane) : -1;
+  const Span sp = span_of(a, a.lens[b]);
+  const int n_act = (sp.tiles + a.split_tiles - 1) / a.split_tiles;
+  if (split > 0 && split >= n_act) return;
+  if (a.window > 0) ids = block_at(a, b, sp.t0 + begin + wave + kAttnWaves * lane);
+  const int end = begin + a.split_tiles < sp.tiles ? begin + a.split_tiles : sp.tiles;
+  const int64_t item = static_cast<int64_t>(b) * gridDim.y + blockIdx.y;
+  attend<ACT, BITS, D>(a, lds, b, h, qt, sp, begin, end, ids, n_act <= 1, item * a.n_splits + split);
+}
+
+// The workgroup's share, an item's part after the other.
+template <int ACT, int BITS, int D>
+__global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn_shares(AttnArgs a, int q_tiles) {
+  __shared__ AttnLds<D> lds;
+  const int w = blockIdx.x, wave = static_cast<int>(threadIdx.x) >> 6, lane = lane_id();
+  const int per_seq = a.kv.n_kv_heads * q_tiles;                 // items of a sequence
+  // lane l sums sequences l per .. (l + 1) per - 1, then the lanes' sums
+  const int per = (a.B + 63) / 64;
+  int sum = 0;
+  for (int i = lane * per; i < (lane + 1) * per && i < a.B; ++i) sum += span_of(a, a.lens[i]).tiles;
+  int upto = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+  }
+  const int r = share_of(a, __builtin_amdgcn_readlane(upto, 63), per_seq);
+  const int total = __builtin_amdgcn_readlane(upto, 63) * per_seq;
+  // (the products below stay below 2^31: checked on the host for max_len)
+  int pos = w * r < total && r > 0 ? w * r : total;
+  const int stop = total - pos < r ? total : pos + r;
+  if (pos >= stop) return;
+  // the sequence at `pos`: the first lane whose sums reach past it, then its sequences
+  const int l = __ffsll(static_cast<long long>(__ballot(upto * per_seq > pos))) - 1;
+  int b = l * per;
+  int start = (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(sum, l)) * per_seq;   // of sequence b
+  Span sp = span_of(a, a.lens[b]);
+  while (start + sp.tiles * per_seq <= pos) {
+    start += sp.tiles * per_seq;
+    sp = span_of(a, a.lens[++b]);
+  }
+  while (true) {
+    const int item = (pos - start) / sp.tiles, begin = pos - start - item * sp.tiles;
+    const int n = min(sp.tiles - begin, stop - pos);
+    const int h = item / q_tiles, qt = item % q_tiles;
+    const int ids = block_at(a, b, sp.t0 + begin + wave + kAttnWaves * lane);
+    attend<ACT, BITS, D>(a, lds, b, h, qt, sp, begin, begin + n, ids, n == sp.tiles,
+                         w + static_cast<int64_t>(b) * per_seq + item);
+    pos += n;
+    if (pos >= stop) return;
+    __syncthreads();                                             // the joins above read LDS
+    while (start + sp.tiles * per_seq <= pos) {
+      start += sp.tiles * per_seq;
+      sp = span_of(a, a.lens[++b]);
+    }
+  }
+}
+
+// Joins the parts of one row (sequence and query head), and writes the rows of
+// empty sequences where no workgroup has them. Four waves take every fourth part
+// and join in a fixed order.
 template <int ACT, int D>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  const int lane = lane_id();
-  const int row = static_cast<int>(blockIdx.x) * 4 + (static_cast<int>(threadIdx.x) >> 6);
-  if (row >= a.B * a.n_q_heads) return;
-  const Span sp = span_of(a, row / a.n_q_heads);
-  const int n = (sp.tiles + a.split_tiles - 1) / a.split_tiles;
-  if (n <= 1) return;
-  const size_t at = static_cast<size_t>(row) * a.n_splits;
+  constexpr int kC = D / 64;
+  __shared__ float lds_o[4][D], lds_l[4];
+  const int wave = static_cast<int>(threadIdx.x) >> 6, lane = lane_id();
+  const int b = blockIdx.y, hq = blockIdx.x, g = a.n_q_heads / a.kv.n_kv_heads;
+  const int q_tiles = (g + 15) / 16, n_part = g < 16 ? g : 16, per_seq = a.kv.n_kv_heads * q_tiles;
+  const int item = hq / g * q_tiles + hq % g / 16;               // of the sequence
+  const Span sp = span_of(a, a.lens[b]);
+  int64_t slot;
+  int n;
+  if (a.n_splits > 0) {
+    slot = (static_cast<int64_t>(b) * per_seq + item) * a.n_splits;
+    n = (sp.tiles + a.split_tiles - 1) / a.split_tiles;
+    if (n <= 1) return;
+  } else {
+    int before, all;
+    tiles_before(a, b, lane, &before, &all);
+    const int r = share_of(a, all, per_seq), start = before * per_seq + item * sp.tiles;
+    if (sp.tiles > 0) {
+      n = (start + sp.tiles - 1) / r - start / r + 1;
+      slot = start / r + static_cast<int64_t>(b) * per_seq + item;
+      if (n == 1) return;
+    } else {
+      n = 0;
+      slot = 0;
+    }
+  }
+  const size_t row = static_cast<size_t>(b) * a.n_q_heads + hq;
+  const size_t at = static_cast<size_t>(slot) * n_part + hq % g % 16;
   float mx = kNoMax;
-  for (int s = lane; s < n; s += 64) mx = fmaxf(mx, a.part_ml[2 * (at + s)]);
+  for (int s = lane; s < n; s += 64) mx = fmaxf(mx, a.part_ml[2 * (at + static_cast<size_t>(s) * n_part)]);
 #pragma unroll
   for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-  float acc[D / 64] = {}, sum = 0.0f;
+  float acc[kC] = {}, sum = 0.0f;
 #pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const float f = exp2f(a.part_ml[2 * (at + s)] - mx);
-    sum = fmaf(f, a.part_ml[2 * (at + s) + 1], sum);
+  for (int s = wave; s < n; s += 4) {
+    const size_t x = at + static_cast<size_t>(s) * n_part;
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * x] - mx);
+    sum = fmaf(f, a.part_ml[2 * x + 1], sum);
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) acc[j] = fmaf(f, a.part_o[(at + s) * D + 64 * j + lane], acc[j]);
+    for (int j = 0; j < kC; ++j) acc[j] = fmaf(f, a.part_o[x * D + 64 * j + lane], acc[j]);
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-  for (int j = 0; j < D / 64; ++j)
-    a.out[static_cast<size_t>(row) * D + 64 * j + lane] = static_cast<uint16_t>(pack16<ACT>(acc[j] * inv, 0.0f));
-  if (a.lse && lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
+  for (int j = 0; j < kC; ++j) lds_o[wave][64 * j + lane] = acc[j];
+  if (lane == 0) lds_l[wave] = sum;
+  __syncthreads();
+  sum = (lds_l[0] + lds_l[1]) + (lds_l[2] + lds_l[3]);
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  for (int d = threadIdx.x; d < D; d += 256)
+    a.out[row * D + d] =
+        static_cast<uint16_t>(pack16<ACT>(((lds_o[0][d] + lds_o[1][d]) + (lds_o[2][d] + lds_o[3][d])) * inv, 0.0f));
+  if (a.lse && threadIdx.x == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
 }
 
 template <int ACT, int BITS, int D>
 hipError_t launch_attn_d(const AttnArgs& a, hipStream_t st) {
   const int g = a.n_q_heads / a.kv.n_kv_heads, q_tiles = (g + 15) / 16;
-  k_attn<ACT, BITS, D><<<a.B * a.kv.n_kv_heads * q_tiles * a.n_splits, 64 * kAttnWaves, 0, st>>>(a, q_tiles);
+  if (a.n_splits > 0)
+    k_attn<ACT, BITS, D><<<dim3(a.n_splits, a.kv.n_kv_heads * q_tiles, a.B), 64 * kAttnWaves, 0, st>>>(a, q_tiles);
+  else
+    k_attn_shares<ACT, BITS, D><<<a.n_shares, 64 * kAttnWaves, 0, st>>>(a, q_tiles);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_splits == 1) return e;
-  k_attn_join<ACT, D><<<(a.B * a.n_q_heads + 3) / 4, 256, 0, st>>>(a);
+  k_attn_join<ACT, D><<<dim3(a.n_q_heads, a.B), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -626,26 +755,41 @@ hipError_t launch_attn_bits(const AttnArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// How far a sequence is split: enough workgroups for every CU to hold a few,
-// and at least eight tiles (two per wave) to a split.
+// How the work is cut (see above).
 AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int, int max_len, int window) {
-  AttnPlan p{1, 4, 0};
+  AttnPlan p{1, 4, 0, 0};
   int64_t tiles = (static_cast<int64_t>(max_len) + kTile - 1) / kTile;
   if (window > 0) {
     const int64_t w = (static_cast<int64_t>(window) + 2 * kTile - 2) / kTile;   // a window that starts inside a tile
     tiles = w < tiles ? w : tiles;
   }
-  const int64_t q_tiles = (n_q_heads / n_kv_heads + 15) / 16;
+  const int64_t g = n_q_heads / n_kv_heads, q_tiles = (g + 15) / 16, rows = g < 16 ? g : 16;
   const int64_t items = static_cast<int64_t>(B) * n_kv_heads * q_tiles;
   if (items == 0 || tiles == 0) return p;
-  int64_t n = (1024 + items - 1) / items;
-  const int64_t most = (tiles + 7) / 8;
+  const size_t slot = static_cast<size_t>(rows) * (head_dim + 2) * sizeof(float);
+  // as many workgroups as the chip holds at once, by the kernels' registers
+  const int64_t resident = 256 * (head_dim <= 64 ? 4 : head_dim <= 128 ? 3 : head_dim <= 192 ? 2 : 1);
+  // Equal shares cost each workgroup the sums over the lengths and, where an item
+  // ends inside its share, a second start, and they need the join; splits leave
+  // unlike lengths unbalanced. 16 bits, 8 key heads of 128 channels, ragged (us,
+  // shares / splits): 64 sequences up to 8192 tokens 166 / 206, up to 4096 92.6 /
+  // 108, up to 2048 56 / 58 (in 8 bits 42 / 36); 16 up to 8192 51 / 61, up to 4096
+  // 31 / 35; 256 up to 2048, more items than workgroups, 207 / 171.
+  if (B > 1 && B <= kShareBatch && items <= resident && tiles >= 96 && items * tiles >= 16 * resident &&
+      items * tiles < (int64_t(1) << 31) - (1 << 20)) {
+    p.n_splits = 0;
+    p.n_shares = static_cast<int>(resident);
+    p.ws_bytes = static_cast<size_t>(resident + items) * slot;
+    return p;
+  }
+  int64_t n = (resident + items - 1) / items;
+  const int64_t most = (tiles + 15) / 16;
   n = n < most ? n : most;
   const int64_t per = ((tiles + n - 1) / n + kAttnWaves - 1) / kAttnWaves * kAttnWaves;
   n = (tiles + per - 1) / per;
   p.split_tiles = static_cast<int>(per);
   p.n_splits = static_cast<int>(n);
-  if (n > 1) p.ws_bytes = static_cast<size_t>(B) * n_q_heads * n * (head_dim + 2) * sizeof(float);
+  if (n > 1) p.ws_bytes = static_cast<size_t>(items * n) * slot;
   return p;
 }
 

@@ -53,8 +53,8 @@ struct AppendArgs {
   int T;
 };
 
-// A sequence's attended positions are cut into tiles of 32 tokens (cut at
-// multiples of 32), split_tiles tiles to a split.
+// A sequence's attended positions are cut into tiles of 32 tokens, at multiples
+// of 32.
 struct AttnArgs {
   KvArgs kv;
   const uint16_t* q;
@@ -67,9 +67,9 @@ struct AttnArgs {
   float scale;
   uint16_t* out;
   float* lse;
-  int n_splits, split_tiles;
-  float* part_o;           // [B n_q_heads][n_splits][D], not normalised
-  float* part_ml;          // [B n_q_heads][n_splits][2]: maximum (base 2), sum
+  int n_splits, split_tiles, n_shares;
+  float* part_o;           // [slots][min(16, query heads per key head)][D], not normalised
+  float* part_ml;          // [slots][the same][2]: maximum (base 2), sum
 };
 
 struct RouteArgs {
@@ -87,8 +87,9 @@ struct RouteArgs {
 };
 
 struct AttnPlan {
-  int n_splits, split_tiles;
-  size_t ws_bytes;
+  int n_splits, split_tiles;  // n_splits 0: equal shares of all tiles
+  int n_shares;
+  size_t ws_bytes;            // a slot's rows of head_dim + 2 floats each
 };
 AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int bits, int max_len, int window);
 

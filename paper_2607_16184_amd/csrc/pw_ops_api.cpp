@@ -49,7 +49,7 @@ const char* attn_fault(const pw_kv_cache* c, int B, int n_q_heads, int max_len, 
   if (max_len < 0 || max_len > INT32_MAX - 256 || window < 0) return "need 0 <= max_len < 2^31 - 256 and window >= 0";
   return nullptr;
 }
-bool attn_too_wide(int B, int n_q_heads) { return static_cast<int64_t>(B) * n_q_heads >= (int64_t(1) << 23); }
+bool attn_too_wide(int B, int n_q_heads) { return B > 65535 || n_q_heads > 65535 || static_cast<int64_t>(B) * n_q_heads >= (int64_t(1) << 23); }
 
 }  // namespace
 
@@ -132,7 +132,7 @@ pw_status pw_kv_append(const pw_kv_cache* c, const void* k, const void* v, int64
 pw_status pw_attn_workspace(const pw_kv_cache* c, int B, int n_q_heads, int max_len, int window, size_t* ws_bytes) {
   if (const char* f = attn_fault(c, B, n_q_heads, max_len, window)) return set_error(PW_EINVAL, f);
   if (!ws_bytes) return set_error(PW_EINVAL, "null argument");
-  if (attn_too_wide(B, n_q_heads)) return set_error(PW_EUNSUPPORTED, "B * n_q_heads must stay below 2^23");
+  if (attn_too_wide(B, n_q_heads)) return set_error(PW_EUNSUPPORTED, "B and n_q_heads must stay below 65536, their product below 2^23");
   *ws_bytes = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window).ws_bytes;
   return PW_OK;
 }
@@ -142,7 +142,7 @@ pw_status pw_attn_decode(const pw_kv_cache* c, const void* q, int64_t ldq, int64
                          float scale, int window, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
   if (const char* f = attn_fault(c, B, n_q_heads, max_len, window)) return set_error(PW_EINVAL, f);
   if (const char* f = kv_memory_fault(c)) return set_error(PW_EINVAL, f);
-  if (attn_too_wide(B, n_q_heads)) return set_error(PW_EUNSUPPORTED, "B * n_q_heads must stay below 2^23");
+  if (attn_too_wide(B, n_q_heads)) return set_error(PW_EUNSUPPORTED, "B and n_q_heads must stay below 65536, their product below 2^23");
   if (ldq % 8 != 0 || ldqh % 8 != 0) return set_error(PW_EINVAL, "strides must be multiples of 8");
   if (!std::isfinite(scale)) return set_error(PW_EINVAL, "scale must be finite");
   const int64_t blocks = (static_cast<int64_t>(max_len) + c->block_tokens - 1) / c->block_tokens;
@@ -171,8 +171,9 @@ pw_status pw_attn_decode(const pw_kv_cache* c, const void* q, int64_t ldq, int64
   a.lse = lse;
   a.n_splits = p.n_splits;
   a.split_tiles = p.split_tiles;
+  a.n_shares = p.n_shares;
   a.part_o = static_cast<float*>(ws);
-  a.part_ml = a.part_o + static_cast<size_t>(B) * n_q_heads * p.n_splits * c->head_dim;
+  a.part_ml = a.part_o + p.ws_bytes / sizeof(float) / (c->head_dim + 2) * c->head_dim;
   return launched(pw::launch_attn(a, static_cast<hipStream_t>(stream)), "attention launch");
 }
 

@@ -445,6 +445,25 @@ def test_attend_many_sequences(bits):
     _attend_case([(37 * i) % 90 for i in range(300)], 32, 1, 2, 64, BF, bits, seed=11)
 
 
+@pytest.mark.parametrize("D,bits,act", [(64, 16, BF), (64, 8, FP), (128, 16, FP), (128, 8, BF), (192, 8, BF), (256, 16, BF), (256, 8, FP)])
+@pytest.mark.parametrize("g", [1, 5, 20])
+def test_attend_equal_shares(D, bits, act, g):
+    """A large bound on the lengths: all tiles cut into equal shares, with
+    workgroups that hold several short sequences and sequences over several."""
+    lens = [0, 1, 33, 700, 64, 0, 0, 2, 1500, 31, 32, 5, 97, 0]
+    H = 2 if g < 20 else 1
+    _attend_case(lens, 64, H, g, D, act, bits, seed=g, max_len=40000)
+
+
+@pytest.mark.parametrize("window", [0, 900])
+def test_attend_equal_shares_of_many_sequences(window):
+    """More sequences than lanes, most of them empty or short."""
+    lens = [(37 * i) % 97 * (i % 3) for i in range(150)]
+    lens[70], lens[149] = 4000, 2000
+    _attend_case(lens, 32, 2, 2, 64, BF, 16, window=window, seed=7, max_len=5000)
+    _attend_case([0] * 150, 32, 2, 2, 64, BF, 16, window=window, seed=7, max_len=5000)
+
+
 def test_attend_runs_twice_the_same_and_on_other_streams():
     side = torch.cuda.Stream()
     _, a = _attend_case([3000, 50], 64, 2, 4, 128, BF, 8, seed=4)
