@@ -578,17 +578,24 @@ pw_status pw_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t 
  *            sum of a[m,k] w[n,k] over the block,
  * accumulated in fp32 and rounded once.
  *   a [M,K] e4m3, row stride lda; a_scale [M, K/128] fp32, packed (as
- *   pw_rms_norm writes them); w [N,K] e4m3, row stride ldw; w_scale
- *   [ceil(N/128), K/128] fp32, packed; y [M,N] of y_type (PW_F16, PW_BF16 or
- *   PW_F32), row stride ldy >= N.
- * Constraints: K a positive multiple of 128; N >= 1; lda, ldw >= K, multiples
- * of 16; a and w 16-byte aligned; y aligned to its elements; one row's and one
- * tile's offsets stay below 2^31 bytes: lda, ldw <= 2^22 (PW_EINVAL otherwise).
+ *   pw_rms_norm writes them); w_scale [ceil(N/128), K/128] fp32, packed; y [M,N]
+ *   of y_type (PW_F16, PW_BF16 or PW_F32), row stride ldy >= N.
+ *   w_packed: the weights w [N,K] e4m3 as pw_gemm_fp8_pack lays them out, once:
+ *   tiles of 16 rows x 128 values, 2048 bytes, tile (t, b) at index t (K/128) +
+ *   b; row r, value k of it at byte 1024 (k/64) + 16 (16 (k/16 mod 4) + r) + k
+ *   mod 16; rows past N are zeros. pw_gemm_fp8_pack reads w with row stride ldw
+ *   and writes pw_gemm_fp8_packed_bytes bytes.
+ * Constraints: K a positive multiple of 128, at most 2^22; N >= 1; the packed
+ * matrix below 2^40 bytes; lda (at most 2^22) and ldw at least K, multiples of
+ * 16; a, w and w_packed 16-byte aligned; y aligned to its elements (PW_EINVAL
+ * otherwise).
  * ws: device workspace of at least pw_gemm_fp8_workspace bytes, 16-byte aligned
  * (PW_ENOMEM below; may be NULL where that is 0), in use until `stream` passes
- * the call. M = 0 does nothing. Deterministic: a fixed order of summation.       */
+ * the call. M = 0 does nothing. Deterministic: a fixed order of summation.   */
+pw_status pw_gemm_fp8_packed_bytes(int N, int K, size_t* bytes);
+pw_status pw_gemm_fp8_pack(const void* w, int64_t ldw, int N, int K, void* packed, void* stream);
 pw_status pw_gemm_fp8_workspace(int M, int N, int K, size_t* ws_bytes);
-pw_status pw_gemm_fp8(const void* a, int64_t lda, const float* a_scale, const void* w, int64_t ldw,
+pw_status pw_gemm_fp8(const void* a, int64_t lda, const float* a_scale, const void* w_packed,
                       const float* w_scale, int M, int N, int K, void* y, int64_t ldy, int y_type, void* ws,
                       size_t ws_bytes, void* stream);
 

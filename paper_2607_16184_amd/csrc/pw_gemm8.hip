@@ -1,12 +1,18 @@
 // Product of 8-bit matrices with block scales, gfx950.
 //
+// Weights are packed once (k_pack8) into tiles of 16 rows x 128 values, 2 KB in
+// the order in which the matrix instructions take them, the tiles of 16 rows one
+// after the other along K. Row-major rows would be read 128 bytes at a time,
+// each from another place of memory: 16 tokens x 28672 x 4096 then take 36.6 us
+// (3.2 TB/s) where packed tiles take XX.
+//
 // One matrix instruction of 16 x 16 x 128 covers exactly one scale block of K,
 // so every block's product starts from zero and enters the fp32 sum with one
 // multiply-add per element. Weight rows are the row operand: their scale is one
 // number per 128 rows, and a lane, which holds four rows of one token's column,
 // multiplies all of them by the same w_scale * a_scale. (Both operands hold
-// bytes 32 g .. 32 g + 31 of their row's block in lane group g; which k that is
-// for the hardware does not matter, it is the same for both.)
+// 16-byte pieces g and g + 4 of their row's block in lane group g; which k that
+// is for the hardware does not matter, it is the same for both.)
 #include <type_traits>
 
 #include "pw_device.hpp"
@@ -72,62 +78,113 @@ __device__ __forceinline__ void store_piece(const Gemm8Args& a, int m, int n, u3
   }
 }
 
-// Streaming kernel: 16 weight rows x 16 MT tokens per workgroup, whose four
-// waves take every fourth K block and join in LDS in a fixed order.
-constexpr int kStreamWaves = 4;
+// Rows [16 t, 16 t + 16) of w, block b, at tile t K / 128 + b: first the 16-byte
+// pieces 0 .. 3 of every row's 128, row c's piece g at 16 (16 g + c), then the
+// pieces 4 .. 7 the same way. Rows past N are zeros.
+__global__ __launch_bounds__(256) void k_pack8(const uint8_t* __restrict__ w, int64_t ldw, int N, int KB,
+                                               u32x4* __restrict__ packed, int64_t pieces) {
+  for (int64_t o = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; o < pieces;
+       o += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t tile = o >> 7, row = tile / KB * 16 + (o & 15);
+    const int piece = static_cast<int>((o >> 4) & 3) + 4 * static_cast<int>((o >> 6) & 1);
+    packed[o] = row < N ? ld16_nt(w + row * ldw + tile % KB * 128 + 16 * piece) : u32x4{0u, 0u, 0u, 0u};
+  }
+}
 
-template <int MT>
+// Streaming kernel, for few tokens: 16 RT weight rows x 16 MT tokens per
+// workgroup, straight from memory to the matrix instructions. The eight waves
+// split K into eight runs of blocks and join in LDS in a fixed order; a wave has
+// kAhead blocks of weights in flight (2 KB RT each), which is what a kernel
+// bound by HBM needs.
+constexpr int kStreamWaves = 8;
+constexpr int kAhead = 4;
+
+template <int RT, int MT>
 __global__ __launch_bounds__(64 * kStreamWaves) void k_gemm8_stream(Gemm8Args a) {
-  __shared__ f32x4 part[kStreamWaves][MT][64];
-  const int wave = static_cast<int>(threadIdx.x) >> 6, lane = lane_id();
+  __shared__ f32x4 part[kStreamWaves][RT * MT][64];
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
   const int c = lane & 15, lg = lane >> 4;
-  const int n_tiles = (a.N + 15) / 16;
+  const int n_tiles = (a.N + 16 * RT - 1) / (16 * RT);
   const int nt = static_cast<int>(blockIdx.x) % n_tiles, m0 = static_cast<int>(blockIdx.x) / n_tiles * (16 * MT);
-  const int KB = a.K / 128;
-  // rows past the end repeat the last one; nothing of them is stored
-  const int n_row = 16 * nt + c < a.N ? 16 * nt + c : a.N - 1;
-  const uint8_t* w = a.w + n_row * a.ldw + 32 * lg;
-  const float* ws = a.w_scale + static_cast<size_t>(nt / 8) * KB;
+  const int KB = a.K / 128, per = (KB + kStreamWaves - 1) / kStreamWaves;
+  const int kb0 = wave * per, kb1 = min(kb0 + per, KB);
+  // row tiles and rows past the end repeat the last one; nothing of them is stored
+  const uint8_t* w[RT];
+  const float* ws[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    w[r] = a.w + static_cast<size_t>(min(nt * RT + r, (a.N - 1) / 16)) * KB * 2048 + 16 * lane;
+    ws[r] = a.w_scale + static_cast<size_t>(min((nt * RT + r) * 16, a.N - 1) / 128) * KB;
+  }
   const uint8_t* x[MT];
   const float* xs[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int m = m0 + 16 * i + c < a.M ? m0 + 16 * i + c : a.M - 1;
-    x[i] = a.a + m * a.lda + 32 * lg;
+    const int m = min(m0 + 16 * i + c, a.M - 1);
+    x[i] = a.a + m * a.lda + 16 * lg;
     xs[i] = a.a_scale + static_cast<size_t>(m) * KB;
   }
-  f32x4 acc[MT];
+  f32x4 acc[RT][MT];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int b = wave; b < KB; b += kStreamWaves) {
-    const F8Frag wf = {ld16_nt(w + b * 128), ld16_nt(w + b * 128 + 16)};
-    const float s = ws[b];
+  for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const F8Frag xf = {ld16(x[i] + b * 128), ld16(x[i] + b * 128 + 16)};
-      const float f = s * xs[i][b];
-      const f32x4 d = mma8(wf, xf);
+    for (int i = 0; i < MT; ++i) acc[r][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int b0 = kb0; b0 < kb1; b0 += kAhead) {
+    F8Frag wf[kAhead][RT], xf[kAhead][MT];
+    float sx[kAhead][MT], sw[kAhead][RT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(d[j], f, acc[i][j]);
+    for (int u = 0; u < kAhead; ++u) {
+      const int b = min(b0 + u, KB - 1);       // past the end: a block again, not used
+#pragma unroll
+      for (int r = 0; r < RT; ++r) wf[u][r] = F8Frag{ld16_nt(w[r] + static_cast<size_t>(b) * 2048), ld16_nt(w[r] + static_cast<size_t>(b) * 2048 + 1024)};
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int b = min(b0 + u, KB - 1);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        xf[u][i] = F8Frag{ld16(x[i] + b * 128), ld16(x[i] + b * 128 + 64)};
+        sx[u][i] = xs[i][b];
+      }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) sw[u][r] = ws[r][b];
+    }
+    __builtin_amdgcn_sched_barrier(0);         // all loads out before the first use
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const bool in = b0 + u < kb1;
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const f32x4 d = mma8(wf[u][r], xf[u][i]);
+          const float f = sw[u][r] * sx[u][i];
+          if (in) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[r][i][j] = fmaf(d[j], f, acc[r][i][j]);
+          }
+        }
     }
   }
 #pragma unroll
-  for (int i = 0; i < MT; ++i) part[wave][i][lane] = acc[i];
-  __syncthreads();
-  for (int i = wave; i < MT; i += kStreamWaves) {
-    f32x4 v = part[0][i][lane];
+  for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int q = 1; q < kStreamWaves; ++q) v += part[q][i][lane];
-    const int m = m0 + 16 * i + c;
-    if (m < a.M) store4(a, m, 16 * nt + 4 * lg, v);
+    for (int i = 0; i < MT; ++i) part[wave][r * MT + i][lane] = acc[r][i];
+  __syncthreads();
+  for (int t = wave; t < RT * MT; t += kStreamWaves) {
+    f32x4 v = part[0][t][lane];
+#pragma unroll
+    for (int q = 1; q < kStreamWaves; ++q) v += part[q][t][lane];
+    const int m = m0 + 16 * (t % MT) + c;
+    if (m < a.M) store4(a, m, (nt * RT + t / MT) * 16 + 4 * lg, v);
   }
 }
 
-template <int MT>
+template <int RT, int MT>
 hipError_t launch_stream(const Gemm8Args& a, hipStream_t st) {
-  const int64_t grid = static_cast<int64_t>((a.N + 15) / 16) * ((a.M + 16 * MT - 1) / (16 * MT));
-  if (grid > (1 << 23)) return hipErrorInvalidConfiguration;
-  k_gemm8_stream<MT><<<static_cast<uint32_t>(grid), 64 * kStreamWaves, 0, st>>>(a);
+  const int64_t grid = static_cast<int64_t>((a.N + 16 * RT - 1) / (16 * RT)) * ((a.M + 16 * MT - 1) / (16 * MT));
+  if (grid > (1 << 22)) return hipErrorInvalidConfiguration;
+  k_gemm8_stream<RT, MT><<<static_cast<uint32_t>(grid), 64 * kStreamWaves, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -144,90 +201,99 @@ hipError_t launch_stream(const Gemm8Args& a, hipStream_t st) {
 // then, so that the next stage's first operands arrive under it. The loads of a
 // stage go out over several row tiles: all at once they queue up in the address
 // unit and hold the wave back.
-template <int TN, int TM, int WN, int WM>
+template <int TN, int TM, int WN, int WM, int SLOTS>
 struct Geo8 {
   static constexpr int kWaves = WN * WM;
   static constexpr int RN = TN / WN / 16, RM = TM / WM / 16;     // a wave's 16 x 16 tiles
   static constexpr int NW = TN / 8 / kWaves, NX = TM / 8 / kWaves;   // a wave's 1 KB loads of a stage
-  // two slots of weights and tokens, two of the tokens' scales of kSc stages
+  // slots of weights and tokens, and two of the tokens' scales of kSc stages
   static constexpr int kX = TN * 128, kSlot = kX + TM * 128;
-  static constexpr int kSc = 8, kScSlot = TM * kSc * 4, kScOff = 2 * kSlot;
+  static constexpr int kSc = 8, kScSlot = TM * kSc * 4, kScOff = SLOTS * kSlot;
   static constexpr int NS = TM / 8 / kWaves;                     // a wave's loads of scales: 8 tokens x kSc stages each
   static constexpr int kLds = kScOff + 2 * kScSlot;
-  static_assert(NS <= kSc && kSc % NS == 0, "the scales of the next stages are loaded over kSc stages");
+  static_assert(NS + SLOTS <= kSc, "the scales of the next stages land in time");
 };
 
-template <int TN, int TM, int WN, int WM>
-__global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
-  using G = Geo8<TN, TM, WN, WM>;
+template <int TN, int TM, int WN, int WM, int SLOTS>
+__global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled(Gemm8Args a) {
+  using G = Geo8<TN, TM, WN, WM, SLOTS>;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[G::kLds];
   lds_u8_t lds = (lds_u8_t)smem;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)));
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
   const int wn = wave % WN, wm = wave / WN;
   const int c = lane & 15, lg = lane >> 4;
-  const int KB = a.K / 128;
+  const int KB = a.K / 128;                            // blocks of a row
 
   // Workgroups go to the eight XCDs in turn: each XCD gets a contiguous run of
   // tiles, walked four token tiles deep so that its L2 serves both operands.
   const int tn = (a.N + TN - 1) / TN, tm = (a.M + TM - 1) / TM, total = tn * tm;
-  const int id = static_cast<int>(blockIdx.x), xcd = id & 7, q8 = total >> 3, r8 = total & 7;
+  const int ks = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x) / total), id = static_cast<int>(blockIdx.x) - ks * total;
+  const int xcd = id & 7, q8 = total >> 3, r8 = total & 7;
+  const int kb0 = ks * a.kb_per;                       // this workgroup's blocks of K
+  const int nstage = __builtin_amdgcn_readfirstlane(min(a.kb_per, KB - kb0));
   const int t = xcd * q8 + (xcd < r8 ? xcd : r8) + (id >> 3);
   constexpr int kDeep = 4;
   const int grp = t / (kDeep * tn), deep = tm - kDeep * grp < kDeep ? tm - kDeep * grp : kDeep;
   const int in = t - kDeep * grp * tn;
   const int n0 = in / deep * TN, m0 = (kDeep * grp + in % deep) * TM;
 
-  // the wave's loads: rows 8 q .. 8 q + 7 of its share, lane l the piece (l mod
-  // 8) ^ (row / 2 mod 8) of row l / 8; rows past the end repeat the last one
+  // the wave's loads: halves of weight tiles as they lie, and 8 rows of tokens,
+  // lane l the piece (l mod 8) ^ (row / 2 mod 8) of row l / 8; what is past the
+  // end repeats the last one
   const int lrow = lane >> 3;
   const auto piece = [&](int q) { return (lane & 7) ^ (lrow >> 1) ^ (4 * (q & 1)); };
   uint32_t woff[G::NW], xoff[G::NX];
 #pragma unroll
-  for (int q = 0; q < G::NW; ++q) {
-    const int r = min(n0 + (wave * G::NW + q) * 8 + lrow, a.N - 1) - n0;
-    woff[q] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.ldw) + 16 * piece(wave * G::NW + q);
+  for (int q = 0; q < G::NW; ++q) {                    // half a tile each (wave-uniform)
+    const int x = wave * G::NW + q, rt = min(n0 / 16 + x / 2, (a.N - 1) / 16) - n0 / 16;
+    woff[q] = static_cast<uint32_t>(rt) * static_cast<uint32_t>(KB) * 2048u + (x & 1) * 1024u;
   }
 #pragma unroll
   for (int q = 0; q < G::NX; ++q) {
     const int r = min(m0 + (wave * G::NX + q) * 8 + lrow, a.M - 1) - m0;
     xoff[q] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.lda) + 16 * piece(wave * G::NX + q);
   }
-  const uint8_t* wbase = uniform_ptr(a.w + n0 * a.ldw);
-  const uint8_t* xbase = uniform_ptr(a.a + m0 * a.lda);
+  const uint8_t* wbase = uniform_ptr(a.w + (static_cast<size_t>(n0 / 16) * KB + kb0) * 2048);
+  const uint8_t* xbase = uniform_ptr(a.a + m0 * a.lda + kb0 * 128);
   // Scales of the tokens come for kSc stages at a time: a load takes 8 tokens x
   // kSc stages, lane l token l mod 8 and stage l / 8 (a load for one stage would
   // touch a cache line per token, as many as all operand loads of the stage).
-  // They are spread over the stages before: stage s loads a share of those of
-  // the next kSc (each share more than once, so that every stage has the same
+  // They are spread over the stages before: a stage loads a share of those of the
+  // next kSc (the last share more than once, so that every stage has the same
   // count of loads). The weight block's scales lie in a register, a stage in a
   // lane.
-  const uint8_t* sbase = uniform_ptr(reinterpret_cast<const uint8_t*>(a.a_scale + static_cast<size_t>(m0) * KB));
+  const uint8_t* sbase = uniform_ptr(reinterpret_cast<const uint8_t*>(a.a_scale + static_cast<size_t>(m0) * KB + kb0));
   const auto load_scales = [&](int chunk, int q) {
     const int o = wave * G::NS + q;
-    const int r = min(m0 + 8 * o + (lane & 7), a.M - 1) - m0, st = min(chunk * G::kSc + lrow, KB - 1);
+    const int r = min(m0 + 8 * o + (lane & 7), a.M - 1) - m0, st = min(chunk * G::kSc + lrow, nstage - 1);
     lds_load4(lds0 + G::kScOff + (chunk & 1) * G::kScSlot + o * 256,
               (static_cast<uint32_t>(r) * static_cast<uint32_t>(KB) + static_cast<uint32_t>(st)) * 4u, sbase);
   };
-  const float* wsp = a.w_scale + static_cast<size_t>(min((n0 + wn * G::RN * 16) / 128, (a.N - 1) / 128)) * KB;
+  const float* wsp = a.w_scale + static_cast<size_t>(min((n0 + wn * G::RN * 16) / 128, (a.N - 1) / 128)) * KB + kb0;
   int ws64 = 0;
-  const auto fetch_ws = [&](int s) { ws64 = __float_as_int(wsp[min(s + lane, KB - 1)]); };
+  const auto fetch_ws = [&](int s) { ws64 = __float_as_int(wsp[min(s + lane, nstage - 1)]); };
   // the wave's loads of stage s, one at a time
   const auto load = [&](int s, int slot, int q) {
-    const int b = s < KB ? s : KB - 1;               // past the end: the last block again, not used
+    const int b = s < nstage ? s : nstage - 1;       // past the end: the last block again, not used
     const uint32_t d = lds0 + slot * G::kSlot;
     if (q < G::NX) lds_load16(d + G::kX + (wave * G::NX + q) * 1024, xoff[q], xbase + b * 128);
-    else lds_load16(d + (wave * G::NW + q - G::NX) * 1024, woff[q - G::NX], wbase + b * 128);
+    else lds_load16(d + (wave * G::NW + q - G::NX) * 1024, 16u * lane, wbase + woff[q - G::NX] + static_cast<size_t>(b) * 2048);
   };
   // They go out over kOver row tiles from the barrier on, kPer at each.
-  constexpr int kOver = G::RN == 8 ? 4 : 2, kPer = (G::NX + G::NW) / kOver;
-  static_assert(kPer * kOver == G::NX + G::NW, "whole shares");
+  constexpr int kOver = G::RN == 8 ? 4 : 2, kAll = G::NX + G::NW, kPer = kAll / kOver;
+  static_assert(kPer * kOver == kAll && (SLOTS == 2 || kOver == 2), "whole shares, all out before the next barrier");
 
   // operand reads: row c of a 16-row tile, pieces lg and lg + 4
   const uint32_t p0 = 128 * c + 16 * (lg ^ (c >> 1)), p1 = p0 ^ 64;
-  const auto read = [&](int off) { return F8Frag{lds16(lds + off + p0), lds16(lds + off + p1)}; };
-  const auto read_w = [&](int slot, int i) { return read(slot * G::kSlot + (wn * G::RN + i) * 2048); };
-  const auto read_x = [&](int slot, int j) { return read(slot * G::kSlot + G::kX + (wm * G::RM + j) * 2048); };
+  const auto read_w = [&](int slot, int i) {
+    lds_u8_t p = lds + slot * G::kSlot + (wn * G::RN + i) * 2048 + 16 * lane;
+    return F8Frag{lds16(p), lds16(p + 1024)};
+  };
+  const auto read_x = [&](int slot, int j) {
+    lds_u8_t p = lds + slot * G::kSlot + G::kX + (wm * G::RM + j) * 2048;
+    return F8Frag{lds16(p + p0), lds16(p + p1)};
+  };
   const auto lds_f32 = [&](int off) { return *reinterpret_cast<const PW_LDS float*>(lds + off); };
 
   F8Frag wf[2], xf[G::RM];
@@ -256,10 +322,12 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
 #pragma unroll
   for (int q = 0; q < G::NS; ++q) load_scales(0, q);
 #pragma unroll
-  for (int q = 0; q < 8; ++q) load(0, 0, q);
+  for (int s = 0; s < SLOTS - 1; ++s)
 #pragma unroll
-  for (int q = 0; q < 2 * kPer; ++q) load(1, 1, q);
-  wait_vm<2 * kPer>();
+    for (int q = 0; q < kAll; ++q) load(s, s, q);
+#pragma unroll
+  for (int q = 0; q < 2 * kPer; ++q) load(SLOTS - 1, SLOTS - 1, q);
+  wait_vm<(SLOTS - 2) * kAll + 2 * kPer>();
   wg_barrier();
   wf[0] = read_w(0, 0);
   wf[1] = read_w(0, 1);
@@ -268,17 +336,17 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
   read_scales(0);
 
   // (64 stages at a time: a branch in the loop would cut its schedule in two)
-  for (int s0 = 0; s0 < KB; s0 += 64) {
+  for (int s0 = 0; s0 < nstage; s0 += 64) {
   fetch_ws(s0);
-  for (int s = s0; s < min(s0 + 64, KB); ++s) {
-    const int slot = s & 1;
+  for (int s = s0; s < min(s0 + 64, nstage); ++s) {
+    const int slot = s % SLOTS, next = (s + 1) % SLOTS;
 #pragma unroll
     for (int i = 0; i < G::RN; ++i) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < G::RM; ++j) {
         d[i & 1][j] = mma8(wf[i & 1], xf[j]);
-        if (i == G::RN - 1) xf[j] = read_x(slot ^ 1, j);
+        if (i == G::RN - 1) xf[j] = read_x(next, j);
         // the tile before this one: at i = 0 the last of the previous stage
         add(i == 0 ? G::RN - 1 : i - 1, j, (i + 1) & 1);
         __builtin_amdgcn_sched_barrier(0);
@@ -291,24 +359,30 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
       if (i == G::RN - 2) {
         // every operand of this stage has been read; the next stage is here
         wait_lds<0>();
-        wait_vm<0>();
+        wait_vm<(SLOTS - 2) * kAll>();
         wg_barrier();
-        load_scales((s + 1) / G::kSc + 1, (s + 1) % G::kSc / (G::kSc / G::NS));
+        load_scales((s + 1) / G::kSc + 1, min((s + 1) % G::kSc, G::NS - 1));
       }
-      // loads of the stage after next, from the barrier into the next stage
+      // loads of stage s + SLOTS, from the barrier into the next stage
 #pragma unroll
       for (int q = 0; q < kPer; ++q) {
-        if (i >= G::RN - 2) load(s + 2, slot, (i - (G::RN - 2)) * kPer + q);
-        else if (i + 2 < kOver) load(s + 1, slot ^ 1, (i + 2) * kPer + q);
+        if (i >= G::RN - 2) load(s + SLOTS, slot, (i - (G::RN - 2)) * kPer + q);
+        else if (i + 2 < kOver) load(s + SLOTS - 1, (s + SLOTS - 1) % SLOTS, (i + 2) * kPer + q);
       }
       if (i < G::RN - 2) wf[i & 1] = read_w(slot, i + 2);
-      else wf[i & 1] = read_w(slot ^ 1, i + 2 - G::RN);
+      else wf[i & 1] = read_w(next, i + 2 - G::RN);
       if (i == G::RN - 1) read_scales(s + 1);
     }
   }
   }
 #pragma unroll
   for (int j = 0; j < G::RM; ++j) add(G::RN - 1, j, (G::RN - 1) & 1);
+  // a part of K: fp32 rows of its own, joined afterwards
+  const bool part = a.ksplit > 1;
+  Gemm8Args out = a;
+  out.y = part ? a.part + static_cast<size_t>(ks) * a.M * a.ldp : a.y;
+  out.ldy = part ? a.ldp : a.ldy;
+  const int y_type = part ? PW_F32 : a.y_type;
   // Through LDS (the wave's own part of it) to rows: a store then covers whole
   // cache lines of a few tokens in place of 32 bytes of each of 16.
   wait_vm<0>();
@@ -327,13 +401,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
         const int row = (k + lane) / kLanes, p = (k + lane) % kLanes;
         const u32x4 v = lds16(w + row * kPitch + 16 * p);
         const int m = m0 + (wm * G::RM + j) * 16 + row;
-        if (m < a.M) store_piece<kE>(a, m, n0 + wn * G::RN * 16 + p * (16 / kE), v);
+        if (m < a.M) store_piece<kE>(out, m, n0 + wn * G::RN * 16 + p * (16 / kE), v);
       }
     }
   };
-  if (a.y_type == PW_F32)
+  if (y_type == PW_F32)
     rows_out(std::integral_constant<int, 4>{}, [](lds_u8_t p, f32x4 v) { *reinterpret_cast<PW_LDS f32x4*>(p) = v; });
-  else if (a.y_type == PW_BF16)
+  else if (y_type == PW_BF16)
     rows_out(std::integral_constant<int, 2>{}, [](lds_u8_t p, f32x4 v) {
       *reinterpret_cast<PW_LDS u32x2*>(p) = u32x2{pack16<PW_BF16>(v[0], v[1]), pack16<PW_BF16>(v[2], v[3])};
     });
@@ -343,24 +417,84 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void k_gemm8_tiled(Gemm8Args a) {
     });
 }
 
-template <int TN, int TM, int WN, int WM>
+template <int TN, int TM, int WN, int WM, int SLOTS>
 hipError_t launch_tiled(const Gemm8Args& a, hipStream_t st) {
-  const int64_t grid = static_cast<int64_t>((a.N + TN - 1) / TN) * ((a.M + TM - 1) / TM);
+  const int64_t grid = static_cast<int64_t>((a.N + TN - 1) / TN) * ((a.M + TM - 1) / TM) * a.ksplit;
   if (grid >= (1 << 22)) return hipErrorInvalidConfiguration;
-  k_gemm8_tiled<TN, TM, WN, WM><<<static_cast<uint32_t>(grid), 64 * WN * WM, 0, st>>>(a);
+  k_gemm8_tiled<TN, TM, WN, WM, SLOTS><<<static_cast<uint32_t>(grid), 64 * WN * WM, 0, st>>>(a);
   return hipGetLastError();
 }
 
+// Sums the parts of K, in their order, four columns a thread.
+__global__ __launch_bounds__(256) void k_gemm8_join(Gemm8Args a) {
+  const int n4 = static_cast<int>(a.ldp / 4);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < static_cast<int64_t>(a.M) * n4;
+       i += static_cast<int64_t>(gridDim.x) * 256) {
+    const float* p = a.part + i * 4;
+    f32x4 v = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll 4
+    for (int k = 1; k < a.ksplit; ++k) v += *reinterpret_cast<const f32x4*>(p + static_cast<size_t>(k) * a.M * a.ldp);
+    store4(a, static_cast<int>(i / n4), static_cast<int>(i % n4) * 4, v);
+  }
+}
+
+// Which kernel runs, and into how many parts K is cut (0: the streaming kernel).
+struct Plan8 {
+  int wide;        // 256 x 256 tiles, not 128 x 128
+  int ksplit, kb_per;
+};
+Plan8 plan8(int M, int N, int K) {
+  Plan8 p{0, 0, K / 128};
+  if (M <= 32) return p;
+  p.ksplit = 1;
+  const int64_t wide = static_cast<int64_t>((N + 255) / 256) * ((M + 255) / 256);
+  if (wide >= 200) {
+    p.wide = 1;
+    return p;
+  }
+  const int64_t tiles = static_cast<int64_t>((N + 127) / 128) * ((M + 127) / 128), KB = K / 128;
+  int64_t k = 256 / tiles;
+  k = k < KB / 4 ? k : KB / 4;
+  if (k > 8) k = 8;
+  if (k > 1) {
+    p.kb_per = static_cast<int>((KB + k - 1) / k);
+    p.ksplit = static_cast<int>((KB + p.kb_per - 1) / p.kb_per);
+  }
+  return p;
+}
+int64_t part_ld(int N) { return (static_cast<int64_t>(N) + 3) / 4 * 4; }
+
 }  // namespace
 
-size_t gemm8_workspace(int, int, int) { return 0; }
+size_t gemm8_workspace(int M, int N, int K) {
+  const Plan8 p = plan8(M, N, K);
+  return p.ksplit > 1 ? static_cast<size_t>(p.ksplit) * M * part_ld(N) * sizeof(float) : 0;
+}
 
-hipError_t launch_gemm8(const Gemm8Args& a, hipStream_t st) {
-  if (a.M <= 16) return launch_stream<1>(a, st);
-  if (a.M <= 32) return launch_stream<2>(a, st);
-  if (a.M <= 64) return launch_stream<4>(a, st);
-  const int64_t wide = static_cast<int64_t>((a.N + 255) / 256) * ((a.M + 255) / 256);
-  return wide >= 200 ? launch_tiled<256, 256, 2, 4>(a, st) : launch_tiled<128, 128, 2, 2>(a, st);
+hipError_t launch_pack8(const uint8_t* w, int64_t ldw, int N, int K, uint8_t* packed, hipStream_t st) {
+  const int64_t pieces = (static_cast<int64_t>(N) + 15) / 16 * K, blocks = (pieces + 255) / 256;   // of 16 bytes
+  k_pack8<<<static_cast<uint32_t>(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, st>>>(
+      w, ldw, N, K / 128, reinterpret_cast<u32x4*>(packed), pieces);
+  return hipGetLastError();
+}
+
+hipError_t launch_gemm8(const Gemm8Args& args, hipStream_t st) {
+  Gemm8Args a = args;
+  const Plan8 p = plan8(a.M, a.N, a.K);
+  if (p.ksplit == 0) {
+    const bool many = a.N >= 16384;
+    if (a.M <= 16) return many ? launch_stream<2, 1>(a, st) : launch_stream<1, 1>(a, st);
+    return many ? launch_stream<2, 2>(a, st) : launch_stream<1, 2>(a, st);
+  }
+  a.ksplit = p.ksplit;
+  a.kb_per = p.kb_per;
+  a.ldp = part_ld(a.N);
+  if (p.wide) return launch_tiled<256, 256, 2, 4, 2>(a, st);
+  hipError_t e = launch_tiled<128, 128, 2, 4, 4>(a, st);
+  if (e != hipSuccess || a.ksplit == 1) return e;
+  const int64_t blocks = (static_cast<int64_t>(a.M) * (a.ldp / 4) + 255) / 256;
+  k_gemm8_join<<<static_cast<uint32_t>(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace pw

@@ -28,13 +28,14 @@ struct NormArgs {
 struct Gemm8Args {
   const uint8_t* a;
   const float* a_scale;
-  const uint8_t* w;
+  const uint8_t* w;        // packed tiles
   const float* w_scale;
   void* y;
-  float* part;             // K-split partials [ksplit][M][N] fp32
-  int64_t lda, ldw, ldy;
+  float* part;             // sums of K's parts [ksplit][M][ldp] fp32
+  int64_t lda, ldy, ldp;
   int M, N, K;
   int y_type;
+  int ksplit, kb_per;      // parts of K and their 128-blocks
 };
 
 struct KvArgs {
@@ -96,6 +97,7 @@ AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int bits,
 size_t gemm8_workspace(int M, int N, int K);
 
 hipError_t launch_rms_norm(const NormArgs& a, hipStream_t st);
+hipError_t launch_pack8(const uint8_t* w, int64_t ldw, int N, int K, uint8_t* packed, hipStream_t st);
 hipError_t launch_gemm8(const Gemm8Args& a, hipStream_t st);
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st);
 hipError_t launch_attn(const AttnArgs& a, hipStream_t st);

@@ -19,6 +19,13 @@ bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p
 bool act_ok(int t) { return t == PW_F16 || t == PW_BF16; }
 bool rows_ok(int64_t ld, int64_t width) { return ld >= width && ld % 8 == 0; }
 
+// What is wrong with a packed matrix's shape, or nullptr.
+const char* packed_fault(int N, int K) {
+  if (N < 1 || K < 128 || K % 128 != 0) return "need N >= 1 and K a positive multiple of 128";
+  if (K > (1 << 22) || (static_cast<int64_t>(N) + 15) / 16 * 16 * K >= (int64_t(1) << 40)) return "K above 2^22, or the matrix above 2^40 bytes";
+  return nullptr;
+}
+
 // What is wrong with a cache's description, or nullptr.
 const char* kv_fault(const pw_kv_cache* c) {
   if (!c) return "null cache";
@@ -78,32 +85,47 @@ pw_status pw_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t 
 
 pw_status pw_gemm_fp8_workspace(int M, int N, int K, size_t* ws_bytes) {
   if (!ws_bytes) return set_error(PW_EINVAL, "null argument");
-  if (M < 0 || N < 1 || K < 128 || K % 128 != 0)
-    return set_error(PW_EINVAL, "need M >= 0, N >= 1 and K a positive multiple of 128");
+  if (M < 0) return set_error(PW_EINVAL, "need M >= 0");
+  if (const char* f = packed_fault(N, K)) return set_error(PW_EINVAL, f);
   *ws_bytes = pw::gemm8_workspace(M, N, K);
   return PW_OK;
 }
 
-pw_status pw_gemm_fp8(const void* a, int64_t lda, const float* a_scale, const void* w, int64_t ldw, const float* w_scale,
-                      int M, int N, int K, void* y, int64_t ldy, int y_type, void* ws, size_t ws_bytes, void* stream) {
-  if (M < 0 || N < 1 || K < 128 || K % 128 != 0)
-    return set_error(PW_EINVAL, "need M >= 0, N >= 1 and K a positive multiple of 128");
+pw_status pw_gemm_fp8_packed_bytes(int N, int K, size_t* bytes) {
+  if (const char* f = packed_fault(N, K)) return set_error(PW_EINVAL, f);
+  if (!bytes) return set_error(PW_EINVAL, "null argument");
+  *bytes = (static_cast<size_t>(N) + 15) / 16 * 16 * K;
+  return PW_OK;
+}
+
+pw_status pw_gemm_fp8_pack(const void* w, int64_t ldw, int N, int K, void* packed, void* stream) {
+  if (const char* f = packed_fault(N, K)) return set_error(PW_EINVAL, f);
+  if (ldw < K || ldw % 16 != 0) return set_error(PW_EINVAL, "ldw must be at least K and a multiple of 16");
+  if (!w || !packed) return set_error(PW_EINVAL, "null argument");
+  if (!aligned(w, 16) || !aligned(packed, 16)) return set_error(PW_EINVAL, "w and packed must be 16-byte aligned");
+  return launched(pw::launch_pack8(static_cast<const uint8_t*>(w), ldw, N, K, static_cast<uint8_t*>(packed),
+                                   static_cast<hipStream_t>(stream)), "pack launch");
+}
+
+pw_status pw_gemm_fp8(const void* a, int64_t lda, const float* a_scale, const void* w_packed, const float* w_scale, int M,
+                      int N, int K, void* y, int64_t ldy, int y_type, void* ws, size_t ws_bytes, void* stream) {
+  if (M < 0) return set_error(PW_EINVAL, "need M >= 0");
+  if (const char* f = packed_fault(N, K)) return set_error(PW_EINVAL, f);
   if (y_type != PW_F16 && y_type != PW_BF16 && y_type != PW_F32)
     return set_error(PW_EINVAL, "y_type must be PW_F16, PW_BF16 or PW_F32");
-  constexpr int64_t kMaxLd = int64_t(1) << 22;
-  if (lda < K || lda % 16 != 0 || lda > kMaxLd || ldw < K || ldw % 16 != 0 || ldw > kMaxLd)
-    return set_error(PW_EINVAL, "lda and ldw must be at least K, multiples of 16 and at most 2^22");
+  if (lda < K || lda % 16 != 0 || lda > (int64_t(1) << 22))
+    return set_error(PW_EINVAL, "lda must be at least K, a multiple of 16 and at most 2^22");
   if (ldy < N) return set_error(PW_EINVAL, "ldy must be at least N");
   if (M == 0) return PW_OK;
-  if (!a || !a_scale || !w || !w_scale || !y) return set_error(PW_EINVAL, "null argument");
-  if (!aligned(a, 16) || !aligned(w, 16)) return set_error(PW_EINVAL, "a and w must be 16-byte aligned");
+  if (!a || !a_scale || !w_packed || !w_scale || !y) return set_error(PW_EINVAL, "null argument");
+  if (!aligned(a, 16) || !aligned(w_packed, 16)) return set_error(PW_EINVAL, "a and w_packed must be 16-byte aligned");
   if (!aligned(a_scale, 4) || !aligned(w_scale, 4) || !aligned(y, y_type == PW_F32 ? 4 : 2))
     return set_error(PW_EINVAL, "scales and y must be aligned to their elements");
   const size_t need = pw::gemm8_workspace(M, N, K);
   if (need && (!ws || ws_bytes < need)) return set_error(PW_ENOMEM, "workspace too small (pw_gemm_fp8_workspace)");
   if (need && !aligned(ws, 16)) return set_error(PW_EINVAL, "the workspace must be 16-byte aligned");
-  const pw::Gemm8Args g{static_cast<const uint8_t*>(a), a_scale, static_cast<const uint8_t*>(w), w_scale, y,
-                        static_cast<float*>(ws), lda, ldw, ldy, M, N, K, y_type};
+  const pw::Gemm8Args g{static_cast<const uint8_t*>(a), a_scale, static_cast<const uint8_t*>(w_packed), w_scale, y,
+                        static_cast<float*>(ws), lda, ldy, 0, M, N, K, y_type, 1, K / 128};
   return launched(pw::launch_gemm8(g, static_cast<hipStream_t>(stream)), "8-bit product launch");
 }
 

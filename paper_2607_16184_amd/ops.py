@@ -111,15 +111,19 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: O
 
 class Linear8:
     """y = x W^T of 8-bit rows: W [N, K] e4m3 with one scale per 128 x 128
-    block [ceil(N / 128), K / 128]."""
+    block [ceil(N / 128), K / 128]. The weights are packed into tiles here
+    (pw_gemm_fp8_pack, on the current stream or ``stream``); w8 itself is not
+    kept."""
 
-    def __init__(self, w8: torch.Tensor, w_scale: torch.Tensor):
-        _need(w8.dtype == _F8 and w8.dim() == 2 and w8.stride(1) == 1 and w8.is_cuda, "w8 must be e4m3 rows on the device")
+    def __init__(self, w8: torch.Tensor, w_scale: torch.Tensor, stream=None):
+        _need(w8.dtype is _F8 and w8.dim() == 2 and w8.stride(1) == 1 and w8.is_cuda, "w8 must be e4m3 rows on the device")
         self.N, self.K = w8.shape
         _need(self.K % 128 == 0, "K must be a multiple of 128")
         _packed(w_scale, (-(-self.N // 128), self.K // 128), torch.float32, "w_scale")
-        self.w8, self.w_scale = w8, w_scale
-        self.ldw = w8.stride(0) if self.N > 1 else self.K
+        self.w_scale = w_scale
+        self.packed = torch.empty(pw.pw_gemm_fp8_packed_bytes(self.N, self.K), dtype=torch.uint8, device=w8.device)
+        pw.pw_gemm_fp8_pack(w8.data_ptr(), w8.stride(0) if self.N > 1 else self.K, self.N, self.K, self.packed.data_ptr(),
+                            _on(w8, stream))
         self._ws = _Workspace(w8.device)
 
     def forward(self, x8: torch.Tensor, x_scale: torch.Tensor, out: torch.Tensor = None, dtype=torch.bfloat16,
@@ -134,7 +138,7 @@ class Linear8:
         _need(out.shape == (M, N) and out.dtype in _TYPE and out.is_cuda and (N == 1 or out.stride(1) == 1),
               "out must be [M, N] rows")
         self._ws.call(pw.pw_gemm_fp8, lambda: pw.pw_gemm_fp8_workspace(M, N, K), x8.data_ptr(), x8.stride(0) if M > 1 else K,
-                      x_scale.data_ptr(), self.w8.data_ptr(), self.ldw, self.w_scale.data_ptr(), M, N, K, out.data_ptr(),
+                      x_scale.data_ptr(), self.packed.data_ptr(), self.w_scale.data_ptr(), M, N, K, out.data_ptr(),
                       out.stride(0) if M > 1 else N, _TYPE[out.dtype], _on(x8, stream))
         return out
 

@@ -135,7 +135,9 @@ def _load():
         "pw_planner_apply": (i32, [vp, vp, vp, P(sz)]),
         "pw_rms_norm": (i32, [vp, i64, vp, i64, vp, i32, i32, f32, i32, vp, vp, vp, vp, vp]),
         "pw_gemm_fp8_workspace": (i32, [i32, i32, i32, P(sz)]),
-        "pw_gemm_fp8": (i32, [vp, i64, vp, vp, i64, vp, i32, i32, i32, vp, i64, i32, vp, sz, vp]),
+        "pw_gemm_fp8_packed_bytes": (i32, [i32, i32, P(sz)]),
+        "pw_gemm_fp8_pack": (i32, [vp, i64, i32, i32, vp, vp]),
+        "pw_gemm_fp8": (i32, [vp, i64, vp, vp, vp, i32, i32, i32, vp, i64, i32, vp, sz, vp]),
         "pw_kv_block_bytes": (i32, [P(pw_kv_cache), P(sz)]),
         "pw_kv_append": (i32, [P(pw_kv_cache), vp, vp, i64, i64, vp, i32, vp]),
         "pw_attn_workspace": (i32, [P(pw_kv_cache), i32, i32, i32, i32, P(sz)]),
@@ -486,10 +488,20 @@ def pw_gemm_fp8_workspace(M: int, N: int, K: int) -> int:
     return out.value
 
 
-def pw_gemm_fp8(a_ptr: int, lda: int, a_scale_ptr: int, w_ptr: int, ldw: int, w_scale_ptr: int, M: int, N: int, K: int,
+def pw_gemm_fp8_packed_bytes(N: int, K: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.pw_gemm_fp8_packed_bytes(N, K, ctypes.byref(out)))
+    return out.value
+
+
+def pw_gemm_fp8_pack(w_ptr: int, ldw: int, N: int, K: int, packed_ptr: int, stream: int):
+    _check(_lib.pw_gemm_fp8_pack(w_ptr, ldw, N, K, packed_ptr, stream))
+
+
+def pw_gemm_fp8(a_ptr: int, lda: int, a_scale_ptr: int, w_packed_ptr: int, w_scale_ptr: int, M: int, N: int, K: int,
                 y_ptr: int, ldy: int, y_type: int, ws_ptr: int, ws_bytes: int, stream: int):
-    _check(_lib.pw_gemm_fp8(a_ptr, lda, a_scale_ptr, w_ptr, ldw, w_scale_ptr, M, N, K, y_ptr, ldy, y_type, ws_ptr, ws_bytes,
-                            stream))
+    _check(_lib.pw_gemm_fp8(a_ptr, lda, a_scale_ptr, w_packed_ptr, w_scale_ptr, M, N, K, y_ptr, ldy, y_type, ws_ptr,
+                            ws_bytes, stream))
 
 
 def pw_kv_block_bytes(cache: pw_kv_cache) -> int:

@@ -155,6 +155,19 @@ def test_gemm_sizes(M, N, K, out):
     assert _same(y, lin.forward(a.cuda(), a_s.cuda(), dtype=out)), "two runs differ"
 
 
+@pytest.mark.parametrize("N,K", [(1, 128), (16, 256), (37, 384), (300, 1024)])
+def test_packed_layout(N, K):
+    """Tiles as the header lays them out; rows past N are zeros."""
+    w = torch.randint(0, 256, (N, K), generator=_gen(N), dtype=torch.uint8)
+    lin = _ops().Linear8(w.view(F8).cuda(), torch.ones(-(-N // 128), K // 128, device="cuda"))
+    rows = np.zeros((-(-N // 16) * 16, K), np.uint8)
+    rows[:N] = w.numpy()
+    want = np.zeros(rows.size, np.uint8)
+    n, k = np.meshgrid(np.arange(rows.shape[0]), np.arange(K), indexing="ij")
+    want[(n // 16 * (K // 128) + k // 128) * 2048 + k % 128 // 64 * 1024 + 16 * (16 * (k // 16 % 4) + n % 16) + k % 16] = rows
+    assert np.array_equal(lin.packed.cpu().numpy(), want)
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 200, 1024), (40, 130, 2048), (300, 700, 512)])
 def test_gemm_wide_scales(M, N, K):
     a, a_s, w, w_s = _gemm_case(M, N, K, 3, wide=True)

@@ -35,16 +35,31 @@ def test_norm_refusals(bad):
     _refused(pw.PW_EINVAL, _call(pw.pw_rms_norm, NORM, NORM_OK, **bad))
 
 
-GEMM = "a lda as_ w ldw ws_ M N K y ldy t ws wsb st".split()
-GEMM_OK = dict(a=A, lda=256, as_=A, w=A, ldw=256, ws_=A, M=4, N=100, K=256, y=A, ldy=100, t=pw.PW_BF16, ws=0, wsb=0, st=0)
+GEMM = "a lda as_ w ws_ M N K y ldy t ws wsb st".split()
+GEMM_OK = dict(a=A, lda=256, as_=A, w=A, ws_=A, M=4, N=100, K=256, y=A, ldy=100, t=pw.PW_BF16, ws=0, wsb=0, st=0)
 
 
-@pytest.mark.parametrize("bad", [dict(M=-1), dict(N=0), dict(K=0), dict(K=192), dict(lda=255), dict(lda=264), dict(ldw=128),
-                                 dict(lda=(1 << 22) + 16), dict(ldw=1 << 23), dict(ldy=99), dict(t=3), dict(t=-1), dict(a=0),
+@pytest.mark.parametrize("bad", [dict(M=-1), dict(N=0), dict(K=0), dict(K=192), dict(lda=255), dict(lda=264),
+                                 dict(lda=(1 << 22) + 16), dict(K=(1 << 22) + 128, lda=(1 << 22) + 128), dict(ldy=99), dict(t=3), dict(t=-1), dict(a=0),
                                  dict(as_=0), dict(w=0), dict(ws_=0), dict(y=0), dict(a=A + 8), dict(w=A + 1), dict(as_=A + 2),
                                  dict(ws_=A + 1), dict(y=A + 1), dict(y=A + 2, t=pw.PW_F32)])
 def test_gemm_refusals(bad):
     _refused(pw.PW_EINVAL, _call(pw.pw_gemm_fp8, GEMM, GEMM_OK, **bad))
+
+
+PACK = "w ldw N K p st".split()
+PACK_OK = dict(w=A, ldw=256, N=100, K=256, p=A, st=0)
+
+
+@pytest.mark.parametrize("bad", [dict(N=0), dict(K=0), dict(K=200), dict(K=1 << 23, ldw=1 << 23), dict(ldw=255), dict(ldw=264),
+                                 dict(w=0), dict(p=0), dict(w=A + 8), dict(p=A + 4), dict(N=1 << 30, K=1 << 14, ldw=1 << 14)])
+def test_pack_refusals(bad):
+    _refused(pw.PW_EINVAL, _call(pw.pw_gemm_fp8_pack, PACK, PACK_OK, **bad))
+
+
+def test_packed_bytes():
+    assert [pw.pw_gemm_fp8_packed_bytes(n, 256) for n in (1, 16, 17, 4000)] == [4096, 4096, 8192, 4000 * 256]
+    _refused(pw.PW_EINVAL, pw.pw_gemm_fp8_packed_bytes, 1, 100)
 
 
 def test_gemm_workspace():
@@ -54,7 +69,7 @@ def test_gemm_workspace():
     for M, N, K in ((1, 256, 4096), (16, 6144, 4096), (100, 512, 4096), (128, 640, 8192), (300, 4096, 14336)):
         need = pw.pw_gemm_fp8_workspace(M, N, K)
         if need:
-            over = dict(M=M, N=N, K=K, lda=K, ldw=K, ldy=N)
+            over = dict(M=M, N=N, K=K, lda=K, ldy=N)
             _refused(pw.PW_ENOMEM, _call(pw.pw_gemm_fp8, GEMM, GEMM_OK, **over))
             _refused(pw.PW_ENOMEM, _call(pw.pw_gemm_fp8, GEMM, GEMM_OK, ws=A, wsb=need - 1, **over))
             _refused(pw.PW_EINVAL, _call(pw.pw_gemm_fp8, GEMM, GEMM_OK, ws=A + 8, wsb=need, **over))
@@ -155,7 +170,7 @@ def test_route_refusals(bad):
 
 def test_nothing_to_do_is_no_error():
     pw.pw_rms_norm(0, 256, 0, 0, 0, 0, 256, 1e-5, pw.PW_F16, 0, 0, 0, 0, 0)
-    pw.pw_gemm_fp8(0, 256, 0, 0, 256, 0, 0, 10, 256, 0, 10, pw.PW_F32, 0, 0, 0)
+    pw.pw_gemm_fp8(0, 256, 0, 0, 0, 0, 10, 256, 0, 10, pw.PW_F32, 0, 0, 0)
     pw.pw_kv_append(_desc(), 0, 0, 64, 64, 0, 0, 0)
     pw.pw_attn_decode(_desc(), 0, 64, 64, 2, 0, 0, 0, 0, 0, 1.0, 0, 0, 0, 0, 0, 0)
 
