@@ -97,10 +97,11 @@ __global__ __launch_bounds__(256) void k_pack8(const uint8_t* __restrict__ w, in
 // kAhead blocks of weights in flight (2 KB RT each), which is what a kernel
 // bound by HBM needs.
 constexpr int kStreamWaves = 8;
-constexpr int kAhead = 4;
+constexpr int kAhead = 2;
 
 template <int RT, int MT>
 __global__ __launch_bounds__(64 * kStreamWaves) void k_gemm8_stream(Gemm8Args a) {
+  constexpr int kAhead = MT == 1 ? 2 : 1;
   __shared__ f32x4 part[kStreamWaves][RT * MT][64];
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
   const int c = lane & 15, lg = lane >> 4;
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
         wait_lds<0>();
         wait_vm<(SLOTS - 2) * kAll>();
         wg_barrier();
-        load_scales((s + 1) / G::kSc + 1, min((s + 1) % G::kSc, G::NS - 1));
+        load_scales(s / G::kSc + 1, min(s % G::kSc, G::NS - 1));
       }
       // loads of stage s + SLOTS, from the barrier into the next stage
 #pragma unroll
@@ -438,28 +439,40 @@ __global__ __launch_bounds__(256) void k_gemm8_join(Gemm8Args a) {
   }
 }
 
-// Which kernel runs, and into how many parts K is cut (0: the streaming kernel).
+// Which kernel runs, and into how many parts K is cut. Measured (us):
+//   streaming / 128 x 128 tiles: 64 tokens x 1024 x 2048 5.8 / 11.8, x 4000 x
+//     2048 8.9 / 13.2, x 6144 x 4096 16.8 / 17.2, x 4096 x 14336 45 / 23.9, x
+//     28672 x 4096 52.6 / 34.0; 128 x 4000 x 2048 14.8 / 14.6;
+//   128 x 128 tiles whole / in parts of K: 128 x 6144 x 4096 24.1 / 18.0, 128 x
+//     4096 x 14336 109 / 27, 256 x 4000 x 2048 14.3 / 18.9;
+//   128 x 128 tiles four stages deep, one workgroup per CU / two deep, two per
+//     CU: 256 x 28672 x 4096 (448 tiles) 64 / 52; below 257 tiles there is but
+//     one workgroup per CU.
+enum { kStream8, kSmall8, kSmallPair8, kWide8 };
 struct Plan8 {
-  int wide;        // 256 x 256 tiles, not 128 x 128
-  int ksplit, kb_per;
+  int kernel, ksplit, kb_per;
 };
 Plan8 plan8(int M, int N, int K) {
-  Plan8 p{0, 0, K / 128};
-  if (M <= 32) return p;
-  p.ksplit = 1;
+  const int64_t KB = K / 128;
+  Plan8 p{kStream8, 1, static_cast<int>(KB)};
+  const int64_t streamed = static_cast<int64_t>(N) * K * ((static_cast<int64_t>(M) + 31) / 32);
+  if (M <= 32 || streamed <= (M <= 64 ? int64_t(52) << 20 : int64_t(32) << 20)) return p;
+  const auto split = [&](int64_t parts) {
+    p.kb_per = static_cast<int>((KB + parts - 1) / parts);
+    p.ksplit = static_cast<int>((KB + p.kb_per - 1) / p.kb_per);
+  };
   const int64_t wide = static_cast<int64_t>((N + 255) / 256) * ((M + 255) / 256);
-  if (wide >= 200) {
-    p.wide = 1;
+  const int64_t tiles = static_cast<int64_t>((N + 127) / 128) * ((M + 127) / 128);
+  p.kernel = kWide8;
+  if (wide >= 200) return p;
+  if (wide >= 48 && KB >= 28 * (256 / wide)) {       // long K: parts of it fill the chip
+    split(256 / wide);
     return p;
   }
-  const int64_t tiles = static_cast<int64_t>((N + 127) / 128) * ((M + 127) / 128), KB = K / 128;
-  int64_t k = 256 / tiles;
-  k = k < KB / 4 ? k : KB / 4;
-  if (k > 8) k = 8;
-  if (k > 1) {
-    p.kb_per = static_cast<int>((KB + k - 1) / k);
-    p.ksplit = static_cast<int>((KB + p.kb_per - 1) / p.kb_per);
-  }
+  p.kernel = tiles > 256 ? kSmallPair8 : kSmall8;
+  int64_t parts = 256 / tiles;
+  parts = parts < KB / 4 ? parts : KB / 4;
+  if (parts > 1 && KB >= 24) split(parts < 8 ? parts : 8);
   return p;
 }
 int64_t part_ld(int N) { return (static_cast<int64_t>(N) + 3) / 4 * 4; }
@@ -481,16 +494,22 @@ hipError_t launch_pack8(const uint8_t* w, int64_t ldw, int N, int K, uint8_t* pa
 hipError_t launch_gemm8(const Gemm8Args& args, hipStream_t st) {
   Gemm8Args a = args;
   const Plan8 p = plan8(a.M, a.N, a.K);
-  if (p.ksplit == 0) {
-    const bool many = a.N >= 16384;
-    if (a.M <= 16) return many ? launch_stream<2, 1>(a, st) : launch_stream<1, 1>(a, st);
-    return many ? launch_stream<2, 2>(a, st) : launch_stream<1, 2>(a, st);
-  }
   a.ksplit = p.ksplit;
   a.kb_per = p.kb_per;
   a.ldp = part_ld(a.N);
-  if (p.wide) return launch_tiled<256, 256, 2, 4, 2>(a, st);
-  hipError_t e = launch_tiled<128, 128, 2, 4, 4>(a, st);
+  hipError_t e;
+  switch (p.kernel) {
+    case kStream8: {
+      // two row tiles per workgroup share its loads of the tokens, where enough
+      // workgroups are left
+      const bool two = a.N >= 5120;
+      if (a.M <= 16) return two ? launch_stream<2, 1>(a, st) : launch_stream<1, 1>(a, st);
+      return two ? launch_stream<2, 2>(a, st) : launch_stream<1, 2>(a, st);
+    }
+    case kSmall8: e = launch_tiled<128, 128, 2, 4, 4>(a, st); break;
+    case kSmallPair8: e = launch_tiled<128, 128, 2, 2, 2>(a, st); break;
+    default: e = launch_tiled<256, 256, 2, 4, 2>(a, st);
+  }
   if (e != hipSuccess || a.ksplit == 1) return e;
   const int64_t blocks = (static_cast<int64_t>(a.M) * (a.ldp / 4) + 255) / 256;
   k_gemm8_join<<<static_cast<uint32_t>(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a);

@@ -131,13 +131,15 @@ def _gemm_case(M, N, K, seed, wide=False):
 
 def _check_gemm(y, a, a_s, w, w_s):
     N, K = w.shape
+    if y.shape[0] * N * K > 1 << 32:   # (the definition's products on the device)
+        y, a, a_s, w, w_s = (t.cuda() for t in (y, a, a_s, w, w_s))
     af = a.double() * a_s.double().repeat_interleave(128, 1)
     wf = w.double() * w_s.double().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)
     want, mass = af @ wf.T, af.abs() @ wf.abs().T
     # 128 products in one instruction, one multiply-add for each block, and the
     # joins of K's parts
     sums = (128 + K // 128 + 24) * 2.0 ** -23 * mass
-    _within(y, want, R.U[y.dtype] * (want.abs() + sums) + sums + R.TINY[y.dtype], "product")
+    _within(y, want.cpu(), (R.U[y.dtype] * (want.abs() + sums) + sums + R.TINY[y.dtype]).cpu(), "product")
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 1, 128), (1, 16, 128), (2, 129, 256), (15, 500, 384), (16, 4000, 512), (17, 127, 4096),
@@ -153,6 +155,24 @@ def test_gemm_sizes(M, N, K, out):
     y = lin.forward(a.cuda(), a_s.cuda(), dtype=out)
     _check_gemm(y, a, a_s, w, w_s)
     assert _same(y, lin.forward(a.cuda(), a_s.cuda(), dtype=out)), "two runs differ"
+
+
+@pytest.mark.parametrize("M,N,K", [
+    (3600, 3400, 1280), (2600, 5300, 2304), (4001, 3333, 8448),    # wide tiles; more than 64 blocks of K
+    (2100, 2200, 1408), (1700, 2700, 4224), (900, 4800, 8320),     # pairs of small tiles
+    (513, 2052, 1280), (777, 4000, 2048), (130, 700, 8448),        # small tiles, whole and in parts of K
+    (1250, 4300, 10752), (1000, 4000, 14336),                      # wide tiles in parts of a long K
+    (64, 6144, 4096), (40, 900, 16512), (250, 1000, 2048)])
+def test_gemm_kernels(M, N, K):
+    """Every kernel at sizes that it is chosen for, with odd ends."""
+    a, a_s, w, w_s = _gemm_case(M, N, K, N)
+    lin = _ops().Linear8(w.cuda(), w_s.cuda())
+    y = lin.forward(a.cuda(), a_s.cuda(), dtype=F32)
+    _check_gemm(y, a, a_s, w, w_s)
+    y16 = torch.full((M, N + 5), 3.0, dtype=BF, device="cuda")
+    lin.forward(a.cuda(), a_s.cuda(), out=y16[:, 1:N + 1])
+    _check_gemm(y16[:, 1:N + 1], a, a_s, w, w_s)
+    assert (y16[:, 0] == 3.0).all() and (y16[:, N + 1:] == 3.0).all()
 
 
 @pytest.mark.parametrize("N,K", [(1, 128), (16, 256), (37, 384), (300, 1024)])
