@@ -4,7 +4,7 @@
 // the order in which the matrix instructions take them, the tiles of 16 rows one
 // after the other along K. Row-major rows would be read 128 bytes at a time,
 // each from another place of memory: 16 tokens x 28672 x 4096 then take 36.6 us
-// (3.2 TB/s) where packed tiles take XX.
+// (3.2 TB/s) where packed tiles take 24 to 26.
 //
 // One matrix instruction of 16 x 16 x 128 covers exactly one scale block of K,
 // so every block's product starts from zero and enters the fp32 sum with one
@@ -97,7 +97,6 @@ __global__ __launch_bounds__(256) void k_pack8(const uint8_t* __restrict__ w, in
 // kAhead blocks of weights in flight (2 KB RT each), which is what a kernel
 // bound by HBM needs.
 constexpr int kStreamWaves = 8;
-constexpr int kAhead = 2;
 
 template <int RT, int MT>
 __global__ __launch_bounds__(64 * kStreamWaves) void k_gemm8_stream(Gemm8Args a) {
@@ -338,43 +337,43 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
 
   // (64 stages at a time: a branch in the loop would cut its schedule in two)
   for (int s0 = 0; s0 < nstage; s0 += 64) {
-  fetch_ws(s0);
-  for (int s = s0; s < min(s0 + 64, nstage); ++s) {
-    const int slot = s % SLOTS, next = (s + 1) % SLOTS;
+    fetch_ws(s0);
+    for (int s = s0; s < min(s0 + 64, nstage); ++s) {
+      const int slot = s % SLOTS, next = (s + 1) % SLOTS;
 #pragma unroll
-    for (int i = 0; i < G::RN; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int j = 0; j < G::RM; ++j) {
-        d[i & 1][j] = mma8(wf[i & 1], xf[j]);
-        if (i == G::RN - 1) xf[j] = read_x(next, j);
-        // the tile before this one: at i = 0 the last of the previous stage
-        add(i == 0 ? G::RN - 1 : i - 1, j, (i + 1) & 1);
+      for (int i = 0; i < G::RN; ++i) {
         __builtin_amdgcn_sched_barrier(0);
-      }
-      if (i == 0) {
-        const float ws = __int_as_float(__builtin_amdgcn_readlane(ws64, s & 63));
 #pragma unroll
-        for (int j = 0; j < G::RM; ++j) f[j] = fn[j] * ws;
-      }
-      if (i == G::RN - 2) {
-        // every operand of this stage has been read; the next stage is here
-        wait_lds<0>();
-        wait_vm<(SLOTS - 2) * kAll>();
-        wg_barrier();
-        load_scales(s / G::kSc + 1, min(s % G::kSc, G::NS - 1));
-      }
-      // loads of stage s + SLOTS, from the barrier into the next stage
+        for (int j = 0; j < G::RM; ++j) {
+          d[i & 1][j] = mma8(wf[i & 1], xf[j]);
+          if (i == G::RN - 1) xf[j] = read_x(next, j);
+          // the tile before this one: at i = 0 the last of the previous stage
+          add(i == 0 ? G::RN - 1 : i - 1, j, (i + 1) & 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (i == 0) {
+          const float ws = __int_as_float(__builtin_amdgcn_readlane(ws64, s & 63));
 #pragma unroll
-      for (int q = 0; q < kPer; ++q) {
-        if (i >= G::RN - 2) load(s + SLOTS, slot, (i - (G::RN - 2)) * kPer + q);
-        else if (i + 2 < kOver) load(s + SLOTS - 1, (s + SLOTS - 1) % SLOTS, (i + 2) * kPer + q);
+          for (int j = 0; j < G::RM; ++j) f[j] = fn[j] * ws;
+        }
+        if (i == G::RN - 2) {
+          // every operand of this stage has been read; the next stage is here
+          wait_lds<0>();
+          wait_vm<(SLOTS - 2) * kAll>();
+          wg_barrier();
+          load_scales(s / G::kSc + 1, min(s % G::kSc, G::NS - 1));
+        }
+        // loads of stage s + SLOTS, from the barrier into the next stage
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+          if (i >= G::RN - 2) load(s + SLOTS, slot, (i - (G::RN - 2)) * kPer + q);
+          else if (i + 2 < kOver) load(s + SLOTS - 1, (s + SLOTS - 1) % SLOTS, (i + 2) * kPer + q);
+        }
+        if (i < G::RN - 2) wf[i & 1] = read_w(slot, i + 2);
+        else wf[i & 1] = read_w(next, i + 2 - G::RN);
+        if (i == G::RN - 1) read_scales(s + 1);
       }
-      if (i < G::RN - 2) wf[i & 1] = read_w(slot, i + 2);
-      else wf[i & 1] = read_w(next, i + 2 - G::RN);
-      if (i == G::RN - 1) read_scales(s + 1);
     }
-  }
   }
 #pragma unroll
   for (int j = 0; j < G::RM; ++j) add(G::RN - 1, j, (G::RN - 1) & 1);
