@@ -5,6 +5,12 @@ into libpagedweight.so (see include/pw.h for the formulas and constraints).
 Outputs are written where ``out`` points, as a serving loop that keeps its
 buffers wants it, or into new tensors. Shapes, types and strides are checked
 here, sizes and alignment by the library (:class:`pw.PWError`).
+
+Work goes to the current stream, or to ``stream``: what this module allocates
+then belongs to that stream; the caller orders it after whatever wrote the
+inputs, and keeps them until it is done. A handle may be used on several
+streams; graphs that were captured on one stream share its workspace and are
+replayed one after the other.
 """
 from __future__ import annotations
 
@@ -39,26 +45,34 @@ def _packed(t: Optional[torch.Tensor], shape, dtype, name: str):
         raise ValueError("%s must be a contiguous device tensor of %s, %s" % (name, shape, dtype))
 
 
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A new tensor that belongs to the stream whose kernels write it."""
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class _Workspace:
-    """A device buffer that grows to what the calls of one handle need."""
+    """The device buffers of one handle, one for each stream that it is used on,
+    grown to what the calls need: a call is made with the buffer at hand, and
+    where that is too small (PW_ENOMEM, nothing launched) again with a larger
+    one. Sizes are powers of two and an outgrown buffer is kept, since a
+    captured graph may hold its address: together they are smaller than the
+    last one."""
 
     def __init__(self, device):
-        self.device, self.t, self.ptr, self.bytes = device, None, 0, 0
+        self.device, self.of, self.kept = device, {}, []
 
-    def call(self, fn, need, *args):
-        """fn(*args, ws_ptr, ws_bytes, stream) with the last of args the stream;
-        where the buffer is too small (PW_ENOMEM, nothing launched), again with
-        one of need() bytes."""
-        *args, stream = args
+    def run(self, st: int, stream, fn, args, need):
+        at = self.of.get(st, (0, 0))
         try:
-            fn(*args, self.ptr, self.bytes, stream)
+            fn(*args, *at, st)
         except pw.PWError as e:
             if e.status != pw.PW_ENOMEM:
                 raise
-            self.bytes = need()
-            self.t = torch.empty(self.bytes, dtype=torch.uint8, device=self.device)
-            self.ptr = self.t.data_ptr()
-            fn(*args, self.ptr, self.bytes, stream)
+            t = _empty(1 << (need() - 1).bit_length(), torch.uint8, self.device, stream)
+            self.kept.append(t)
+            at = self.of[st] = (t.data_ptr(), t.numel())
+            fn(*args, *at, st)
 
 
 # ---------------------------------------------------------------------------
@@ -94,7 +108,8 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: O
         ldx = ldr = H
     _packed(weight, (H,), act, "weight")
     if out is None:
-        out = norm_buffers(T, H, act, residual is not None, y16, y8, x.device)
+        with torch.cuda.stream(stream):
+            out = norm_buffers(T, H, act, residual is not None, y16, y8, x.device)
     s, y, q, qs = out
     _packed(s, (T, H), act, "the sum")
     _packed(y, (T, H), act, "y16")
@@ -121,9 +136,11 @@ class Linear8:
         _need(self.K % 128 == 0, "K must be a multiple of 128")
         _packed(w_scale, (-(-self.N // 128), self.K // 128), torch.float32, "w_scale")
         self.w_scale = w_scale
-        self.packed = torch.empty(pw.pw_gemm_fp8_packed_bytes(self.N, self.K), dtype=torch.uint8, device=w8.device)
+        self.packed = _empty(pw.pw_gemm_fp8_packed_bytes(self.N, self.K), torch.uint8, w8.device, stream)
         pw.pw_gemm_fp8_pack(w8.data_ptr(), w8.stride(0) if self.N > 1 else self.K, self.N, self.K, self.packed.data_ptr(),
                             _on(w8, stream))
+        if stream is not None:
+            w8.record_stream(stream)       # the caller may drop it before the packing has run
         self._ws = _Workspace(w8.device)
 
     def forward(self, x8: torch.Tensor, x_scale: torch.Tensor, out: torch.Tensor = None, dtype=torch.bfloat16,
@@ -134,12 +151,12 @@ class Linear8:
         _need(x8.dtype is _F8 and x8.shape == (M, K) and x8.is_cuda and x8.stride(1) == 1, "x8 must be [M, K] e4m3 rows")
         _packed(x_scale, (M, K // 128), torch.float32, "x_scale")
         if out is None:
-            out = torch.empty((M, N), dtype=dtype, device=x8.device)
+            out = _empty((M, N), dtype, x8.device, stream)
         _need(out.shape == (M, N) and out.dtype in _TYPE and out.is_cuda and (N == 1 or out.stride(1) == 1),
               "out must be [M, N] rows")
-        self._ws.call(pw.pw_gemm_fp8, lambda: pw.pw_gemm_fp8_workspace(M, N, K), x8.data_ptr(), x8.stride(0) if M > 1 else K,
-                      x_scale.data_ptr(), self.packed.data_ptr(), self.w_scale.data_ptr(), M, N, K, out.data_ptr(),
-                      out.stride(0) if M > 1 else N, _TYPE[out.dtype], _on(x8, stream))
+        args = (x8.data_ptr(), x8.stride(0) if M > 1 else K, x_scale.data_ptr(), self.packed.data_ptr(),
+                self.w_scale.data_ptr(), M, N, K, out.data_ptr(), out.stride(0) if M > 1 else N, _TYPE[out.dtype])
+        self._ws.run(_on(x8, stream), stream, pw.pw_gemm_fp8, args, lambda: pw.pw_gemm_fp8_workspace(M, N, K))
         return out
 
 
@@ -156,14 +173,14 @@ class KVCache:
     def __init__(self, n_blocks: int, block_tokens: int, kv_heads: int, head_dim: int, act: torch.dtype, fp8: bool = False,
                  pool: torch.Tensor = None, block_stride: int = None, device="cuda"):
         _need(act in (torch.float16, torch.bfloat16), "act must be a 16-bit type")
-        self.act, self.head_dim, self.kv_heads = act, head_dim, kv_heads
+        self.act, self.head_dim, self.kv_heads, self.block_tokens = act, head_dim, kv_heads, block_tokens
         self.desc = pw.pw_kv_cache(None, 0, n_blocks, block_tokens, kv_heads, head_dim, _TYPE[act], 8 if fp8 else 16)
         self.block_bytes = pw.pw_kv_block_bytes(self.desc)
         self.desc.block_stride = block_stride or self.block_bytes
         if pool is None:
             pool = torch.empty(max(n_blocks - 1, 0) * self.desc.block_stride + self.block_bytes, dtype=torch.uint8, device=device)
         _need(pool.dtype == torch.uint8 and pool.is_contiguous() and pool.is_cuda, "the pool must be contiguous device bytes")
-        _need(block_stride is not None or pool.numel() >= n_blocks * self.block_bytes, "the pool is smaller than its blocks")
+        _need(pool.numel() >= (n_blocks - 1) * self.desc.block_stride + self.block_bytes, "the pool is smaller than its blocks")
         self.pool = pool
         self.desc.pool = pool.data_ptr()
         self._ws = _Workspace(pool.device)
@@ -192,14 +209,15 @@ class KVCache:
         _need(block_table.dtype is torch.int32 and rows == B and block_table.is_cuda
               and (block_table.stride(1) == 1 or blocks <= 1), "block_table must be [B, blocks] int32")
         _packed(lens, (B,), torch.int32, "lens")
-        _need(blocks * self.desc.block_tokens >= max_len, "the block table is shorter than max_len")
+        _need(blocks * self.block_tokens >= max_len, "the block table is shorter than max_len")
         if out is None:
-            out = torch.empty((B, heads, D), dtype=self.act, device=q.device)
+            out = _empty((B, heads, D), self.act, q.device, stream)
         _packed(out, (B, heads, D), self.act, "out")
         _packed(lse, (B, heads), torch.float32, "lse")
         args = (self.desc, q.data_ptr(), ldq, ldqh, heads, block_table.data_ptr(), block_table.stride(0) if B > 1 else blocks,
                 lens.data_ptr(), B, max_len, D ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse))
-        self._ws.call(pw.pw_attn_decode, lambda: pw.pw_attn_workspace(self.desc, B, heads, max_len, window), *args, _on(q, stream))
+        self._ws.run(_on(q, stream), stream, pw.pw_attn_decode, args,
+                     lambda: pw.pw_attn_workspace(self.desc, B, heads, max_len, window))
         return out
 
 
@@ -222,7 +240,10 @@ def route_grouped(logits: torch.Tensor, K: int, score: str = "softmax", bias: to
     _packed(bias, (E,), torch.float32, "bias")
     _packed(gate, (T, n_shared), torch.float32, "gate")
     Kt = K + n_shared
-    ids, w, offsets, ss, sp = out if out is not None else PagedLayer.routing_buffers(T, E + n_shared, Kt, logits.device)
+    if out is None:
+        with torch.cuda.stream(stream):
+            out = PagedLayer.routing_buffers(T, E + n_shared, Kt, logits.device)
+    ids, w, offsets, ss, sp = out
     _need(ids.shape == (T, Kt) and w.shape == (T, Kt) and offsets.numel() == E + n_shared + 1
           and min(ss.numel(), sp.numel()) >= T * Kt, "the routing buffers are of another size (PagedLayer.routing_buffers)")
     pw.pw_route_grouped(logits.data_ptr(), _TYPE[logits.dtype], _ptr(bias), T, E, K, _SCORE[score], groups, top_groups,

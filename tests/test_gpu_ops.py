@@ -671,3 +671,43 @@ def test_captured_calls_replay():
         torch.cuda.synchronize()
         for a, b in zip(first, want):
             assert torch.equal(a, b)
+
+
+def test_outgrown_workspace_stays_with_its_graph():
+    """A larger call after a capture: the graph's own buffer stays untouched by
+    others, and its replays give the first result."""
+    ops = _ops()
+    a, a_s, w, w_s = _gemm_case(200, 4000, 4096, 31)
+    lin = ops.Linear8(w.cuda(), w_s.cuda())
+    x, xs = a[:65].cuda(), a_s[:65].cuda()
+    want = lin.forward(x, xs).clone()
+    assert 2 * pw.pw_gemm_fp8_workspace(200, 4000, 4096) > 3 * pw.pw_gemm_fp8_workspace(65, 4000, 4096) > 0
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = lin.forward(x, xs)
+    held = {t.data_ptr() for t in lin._ws.kept}
+    a_d, as_d = a.cuda(), a_s.cuda()
+    side.wait_stream(torch.cuda.current_stream())
+    big, other = lin.forward(a_d, as_d, stream=side), lin.forward(x, xs, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    fill = [torch.full((1 << 20,), 255, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert _same(got, want) and _same(other, want)
+    assert held <= {t.data_ptr() for t in lin._ws.kept} and len({p for p, _ in lin._ws.of.values()}) == len(lin._ws.of) >= 2
+    assert sum(t.numel() for t in lin._ws.kept) <= 2 * sum(n for _, n in lin._ws.of.values())
+    assert all(bool((t == 255).all()) for t in fill)
+    _check_gemm(big, a, a_s, w, w_s)
+
+
+def test_cache_refuses_a_pool_smaller_than_its_blocks():
+    ops = _ops()
+    nb = R.block_bytes(2, 32, 64, 16)
+    pool = torch.zeros(4 * nb, dtype=torch.uint8, device="cuda")
+    ops.KVCache(4, 32, 2, 64, BF, pool=pool)
+    ops.KVCache(2, 32, 2, 64, BF, pool=pool, block_stride=3 * nb)
+    for n, stride in [(5, None), (3, 2 * nb), (2, 4 * nb)]:
+        with pytest.raises(ValueError):
+            ops.KVCache(n, 32, 2, 64, BF, pool=pool, block_stride=stride)
