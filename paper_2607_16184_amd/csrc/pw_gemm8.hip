@@ -210,7 +210,7 @@ struct Geo8 {
   static constexpr int kX = TN * 128, kSlot = kX + TM * 128;
   static constexpr int kSc = 8, kScSlot = TM * kSc * 4, kScOff = SLOTS * kSlot;
   static constexpr int NS = TM / 8 / kWaves;                     // a wave's loads of scales: 8 tokens x kSc stages each
-  static constexpr int kLds = kScOff + 2 * kScSlot;
+  static constexpr int kSpare = kScOff + 2 * kScSlot, kLds = kSpare + 256;
   static_assert(NS + SLOTS <= kSc, "the scales of the next stages land in time");
 };
 
@@ -260,15 +260,17 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
   // kSc stages, lane l token l mod 8 and stage l / 8 (a load for one stage would
   // touch a cache line per token, as many as all operand loads of the stage).
   // They are spread over the stages before: a stage loads a share of those of the
-  // next kSc (the last share more than once, so that every stage has the same
-  // count of loads). The weight block's scales lie in a register, a stage in a
-  // lane.
+  // next kSc. Every stage has the same count of loads, which the waits rely on;
+  // those past the last share read one address into spare bytes of LDS (777 tokens
+  // x 4000 x 4096: 27.4 us, with the last share's eight lines again 29.1). The
+  // weight block's scales lie in a register, a stage in a lane.
   const uint8_t* sbase = uniform_ptr(reinterpret_cast<const uint8_t*>(a.a_scale + static_cast<size_t>(m0) * KB + kb0));
   const auto load_scales = [&](int chunk, int q) {
+    const bool live = q < G::NS;                     // (wave-uniform)
     const int o = wave * G::NS + q;
     const int r = min(m0 + 8 * o + (lane & 7), a.M - 1) - m0, st = min(chunk * G::kSc + lrow, nstage - 1);
-    lds_load4(lds0 + G::kScOff + (chunk & 1) * G::kScSlot + o * 256,
-              (static_cast<uint32_t>(r) * static_cast<uint32_t>(KB) + static_cast<uint32_t>(st)) * 4u, sbase);
+    const uint32_t off = (static_cast<uint32_t>(r) * static_cast<uint32_t>(KB) + static_cast<uint32_t>(st)) * 4u;
+    lds_load4(lds0 + (live ? G::kScOff + (chunk & 1) * G::kScSlot + o * 256 : G::kSpare), off & (live ? ~0u : 0u), sbase);
   };
   const float* wsp = a.w_scale + static_cast<size_t>(min((n0 + wn * G::RN * 16) / 128, (a.N - 1) / 128)) * KB + kb0;
   int ws64 = 0;
@@ -361,7 +363,7 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
           wait_lds<0>();
           wait_vm<(SLOTS - 2) * kAll>();
           wg_barrier();
-          load_scales(s / G::kSc + 1, min(s % G::kSc, G::NS - 1));
+          load_scales(s / G::kSc + 1, s % G::kSc);
         }
         // loads of stage s + SLOTS, from the barrier into the next stage
 #pragma unroll
