@@ -13,6 +13,13 @@
 // multiplies all of them by the same w_scale * a_scale. (Both operands hold
 // 16-byte pieces g and g + 4 of their row's block in lane group g; which k that
 // is for the hardware does not matter, it is the same for both.)
+//
+// The 8-bit instruction aligns its products to the largest of them and drops
+// what lies below: sums come out 1.4e-5 off in norm, 2^-16, for K = 384 as for
+// 4096. Outputs of 16 bits, rounded to 2^-9 or 2^-12, do not show it. For fp32
+// outputs the codes are widened, exactly, to bf16 and go through four 16-bit
+// instructions, whose sums are off by 5e-8 (K = 384) to 1.1e-7 (4096).
+#include <algorithm>
 #include <type_traits>
 
 #include "pw_device.hpp"
@@ -35,6 +42,37 @@ __device__ __forceinline__ i32x8 frag(const F8Frag& f) {
 __device__ __forceinline__ f32x4 mma8(const F8Frag& a, const F8Frag& b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag(a), frag(b), f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0,
                                                           0, 0);
+}
+// The same operand in 16 bits.
+struct WideFrag {
+  bf16x8 v[4];
+};
+__device__ __forceinline__ WideFrag widen(const F8Frag& f) {
+  WideFrag r;
+#pragma unroll
+  for (int p = 0; p < 4; ++p)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t x = p < 2 ? f.lo[2 * p + k] : f.hi[2 * p + k - 4];
+      const auto lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false);
+      const auto hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true);
+      r.v[p][4 * k] = lo[0];
+      r.v[p][4 * k + 1] = lo[1];
+      r.v[p][4 * k + 2] = hi[0];
+      r.v[p][4 * k + 3] = hi[1];
+    }
+  return r;
+}
+__device__ __forceinline__ f32x4 mma8(const WideFrag& a, const WideFrag& b) {
+  f32x4 d{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int p = 0; p < 4; ++p) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[p], b.v[p], d, 0, 0, 0);
+  return d;
+}
+template <bool WIDE>
+__device__ __forceinline__ auto operand(const F8Frag& f) {
+  if constexpr (WIDE) return widen(f);
+  else return f;
 }
 
 __device__ __forceinline__ void store_y(const Gemm8Args& a, int m, int n, float v) {
@@ -98,7 +136,7 @@ __global__ __launch_bounds__(256) void k_pack8(const uint8_t* __restrict__ w, in
 // bound by HBM needs.
 constexpr int kStreamWaves = 8;
 
-template <int RT, int MT>
+template <int RT, int MT, bool WIDE>
 __global__ __launch_bounds__(64 * kStreamWaves) void k_gemm8_stream(Gemm8Args a) {
   constexpr int kAhead = MT == 1 ? 2 : 1;
   __shared__ f32x4 part[kStreamWaves][RT * MT][64];
@@ -157,7 +195,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_gemm8_stream(Gemm8Args a)
       for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          const f32x4 d = mma8(wf[u][r], xf[u][i]);
+          const f32x4 d = mma8(operand<WIDE>(wf[u][r]), operand<WIDE>(xf[u][i]));
           const float f = sw[u][r] * sx[u][i];
           if (in) {
 #pragma unroll
@@ -180,12 +218,21 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_gemm8_stream(Gemm8Args a)
   }
 }
 
-template <int RT, int MT>
+template <int RT, int MT, bool WIDE>
 hipError_t launch_stream(const Gemm8Args& a, hipStream_t st) {
   const int64_t grid = static_cast<int64_t>((a.N + 16 * RT - 1) / (16 * RT)) * ((a.M + 16 * MT - 1) / (16 * MT));
   if (grid > (1 << 22)) return hipErrorInvalidConfiguration;
-  k_gemm8_stream<RT, MT><<<static_cast<uint32_t>(grid), 64 * kStreamWaves, 0, st>>>(a);
+  k_gemm8_stream<RT, MT, WIDE><<<static_cast<uint32_t>(grid), 64 * kStreamWaves, 0, st>>>(a);
   return hipGetLastError();
+}
+
+// Two row tiles per workgroup share its loads of the tokens, where enough
+// workgroups are left.
+template <bool WIDE>
+hipError_t launch_stream_of(const Gemm8Args& a, hipStream_t st) {
+  const bool two = a.N >= 5120;
+  if (a.M <= 16) return two ? launch_stream<2, 1, WIDE>(a, st) : launch_stream<1, 1, WIDE>(a, st);
+  return two ? launch_stream<2, 2, WIDE>(a, st) : launch_stream<1, 2, WIDE>(a, st);
 }
 
 // Tiled kernel: TN weight rows x TM tokens per workgroup, WN x WM waves. K
@@ -214,7 +261,7 @@ struct Geo8 {
   static_assert(NS + SLOTS <= kSc, "the scales of the next stages land in time");
 };
 
-template <int TN, int TM, int WN, int WM, int SLOTS>
+template <int TN, int TM, int WN, int WM, int SLOTS, bool WIDE = false>
 __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled(Gemm8Args a) {
   using G = Geo8<TN, TM, WN, WM, SLOTS>;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[G::kLds];
@@ -299,6 +346,7 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
   const auto lds_f32 = [&](int off) { return *reinterpret_cast<const PW_LDS float*>(lds + off); };
 
   F8Frag wf[2], xf[G::RM];
+  WideFrag ww, xw[G::RM];                              // (WIDE alone)
   f32x4 acc[G::RN][G::RM], d[2][G::RM];
   float f[G::RM], fn[G::RM];
 #pragma unroll
@@ -347,7 +395,13 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < G::RM; ++j) {
-          d[i & 1][j] = mma8(wf[i & 1], xf[j]);
+          if constexpr (WIDE) {
+            if (i == 0) xw[j] = widen(xf[j]);
+            if (j == 0) ww = widen(wf[i & 1]);
+            d[i & 1][j] = mma8(ww, xw[j]);
+          } else {
+            d[i & 1][j] = mma8(wf[i & 1], xf[j]);
+          }
           if (i == G::RN - 1) xf[j] = read_x(next, j);
           // the tile before this one: at i = 0 the last of the previous stage
           add(i == 0 ? G::RN - 1 : i - 1, j, (i + 1) & 1);
@@ -419,11 +473,11 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
     });
 }
 
-template <int TN, int TM, int WN, int WM, int SLOTS>
+template <int TN, int TM, int WN, int WM, int SLOTS, bool WIDE = false>
 hipError_t launch_tiled(const Gemm8Args& a, hipStream_t st) {
   const int64_t grid = static_cast<int64_t>((a.N + TN - 1) / TN) * ((a.M + TM - 1) / TM) * a.ksplit;
   if (grid >= (1 << 22)) return hipErrorInvalidConfiguration;
-  k_gemm8_tiled<TN, TM, WN, WM, SLOTS><<<static_cast<uint32_t>(grid), 64 * WN * WM, 0, st>>>(a);
+  k_gemm8_tiled<TN, TM, WN, WM, SLOTS, WIDE><<<static_cast<uint32_t>(grid), 64 * WN * WM, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -449,11 +503,14 @@ __global__ __launch_bounds__(256) void k_gemm8_join(Gemm8Args a) {
 //   128 x 128 tiles four stages deep, one workgroup per CU / two deep, two per
 //     CU: 256 x 28672 x 4096 (448 tiles) 64 / 52; below 257 tiles there is but
 //     one workgroup per CU.
+// Widened operands do not fit the registers of a 256 x 256 tile; 128 x 128, two
+// stages deep in pairs / four deep alone: 825 x 5795 x 3456 (322 tiles) 56 / 66,
+// 4096 x 14336 x 4096 447 / 533 (8-bit instructions and wide tiles: 265).
 enum { kStream8, kSmall8, kSmallPair8, kWide8 };
 struct Plan8 {
   int kernel, ksplit, kb_per;
 };
-Plan8 plan8(int M, int N, int K) {
+Plan8 plan8(int M, int N, int K, bool widened) {
   const int64_t KB = K / 128;
   Plan8 p{kStream8, 1, static_cast<int>(KB)};
   const int64_t streamed = static_cast<int64_t>(N) * K * ((static_cast<int64_t>(M) + 31) / 32);
@@ -465,8 +522,8 @@ Plan8 plan8(int M, int N, int K) {
   const int64_t wide = static_cast<int64_t>((N + 255) / 256) * ((M + 255) / 256);
   const int64_t tiles = static_cast<int64_t>((N + 127) / 128) * ((M + 127) / 128);
   p.kernel = kWide8;
-  if (wide >= 200) return p;
-  if (wide >= 48 && KB >= 28 * (256 / wide)) {       // long K: parts of it fill the chip
+  if (!widened && wide >= 200) return p;
+  if (!widened && wide >= 48 && KB >= 28 * (256 / wide)) {       // long K: parts of it fill the chip
     split(256 / wide);
     return p;
   }
@@ -480,9 +537,10 @@ int64_t part_ld(int N) { return (static_cast<int64_t>(N) + 3) / 4 * 4; }
 
 }  // namespace
 
+// (for any type of y)
 size_t gemm8_workspace(int M, int N, int K) {
-  const Plan8 p = plan8(M, N, K);
-  return p.ksplit > 1 ? static_cast<size_t>(p.ksplit) * M * part_ld(N) * sizeof(float) : 0;
+  const int parts = std::max(plan8(M, N, K, false).ksplit, plan8(M, N, K, true).ksplit);
+  return parts > 1 ? static_cast<size_t>(parts) * M * part_ld(N) * sizeof(float) : 0;
 }
 
 hipError_t launch_pack8(const uint8_t* w, int64_t ldw, int N, int K, uint8_t* packed, hipStream_t st) {
@@ -494,21 +552,17 @@ hipError_t launch_pack8(const uint8_t* w, int64_t ldw, int N, int K, uint8_t* pa
 
 hipError_t launch_gemm8(const Gemm8Args& args, hipStream_t st) {
   Gemm8Args a = args;
-  const Plan8 p = plan8(a.M, a.N, a.K);
+  const bool widened = a.y_type == PW_F32;
+  const Plan8 p = plan8(a.M, a.N, a.K, widened);
   a.ksplit = p.ksplit;
   a.kb_per = p.kb_per;
   a.ldp = part_ld(a.N);
   hipError_t e;
   switch (p.kernel) {
-    case kStream8: {
-      // two row tiles per workgroup share its loads of the tokens, where enough
-      // workgroups are left
-      const bool two = a.N >= 5120;
-      if (a.M <= 16) return two ? launch_stream<2, 1>(a, st) : launch_stream<1, 1>(a, st);
-      return two ? launch_stream<2, 2>(a, st) : launch_stream<1, 2>(a, st);
-    }
-    case kSmall8: e = launch_tiled<128, 128, 2, 4, 4>(a, st); break;
-    case kSmallPair8: e = launch_tiled<128, 128, 2, 2, 2>(a, st); break;
+    case kStream8:
+      return widened ? launch_stream_of<true>(a, st) : launch_stream_of<false>(a, st);
+    case kSmall8: e = widened ? launch_tiled<128, 128, 2, 4, 4, true>(a, st) : launch_tiled<128, 128, 2, 4, 4>(a, st); break;
+    case kSmallPair8: e = widened ? launch_tiled<128, 128, 2, 2, 2, true>(a, st) : launch_tiled<128, 128, 2, 2, 2>(a, st); break;
     default: e = launch_tiled<256, 256, 2, 4, 2>(a, st);
   }
   if (e != hipSuccess || a.ksplit == 1) return e;

@@ -711,3 +711,20 @@ def test_cache_refuses_a_pool_smaller_than_its_blocks():
     for n, stride in [(5, None), (3, 2 * nb), (2, 4 * nb)]:
         with pytest.raises(ValueError):
             ops.KVCache(n, 32, 2, 64, BF, pool=pool, block_stride=stride)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1000, 3456), (4, 5236, 384), (20, 300, 2048), (60, 6000, 1024), (200, 1000, 1024), (300, 4000, 2048),
+                                   (130, 6144, 4096), (1000, 4100, 640)])
+def test_gemm_fp32_sums_are_fp32(M, N, K):
+    """fp32 outputs hold fp32 sums. Exact products, added 32 at a time to a
+    running sum, and one multiply-add per block: a random walk of K / 32 + K /
+    128 roundings of 2^-24 each; four times that is allowed, in norm."""
+    g = _gen(M)
+    a, a_s = R.quant(torch.randn(M, K, generator=g), 128)
+    w = (torch.randn(N, K, generator=g) * 100).clamp(-448, 448).to(F8)
+    w_s = torch.rand(-(-N // 128), K // 128, generator=g) + 0.1
+    y = _ops().Linear8(w.cuda(), w_s.cuda()).forward(a.cuda(), a_s.cuda(), dtype=F32).cpu().double()
+    af = a.double() * a_s.double().repeat_interleave(128, 1)
+    want = af @ (w.double() * w_s.double().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)).T
+    off = float((y - want).norm() / want.norm())
+    assert off <= (K / 32 + K / 128) ** 0.5 * 2.0 ** -22, off
