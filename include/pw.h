@@ -588,10 +588,10 @@ pw_status pw_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t 
  *   b; row r, value k of it at byte 1024 (k/64) + 16 (16 (k/16 mod 4) + r) + k
  *   mod 16; rows past N are zeros. pw_gemm_fp8_pack reads w with row stride ldw
  *   and writes pw_gemm_fp8_packed_bytes bytes.
- * Constraints: K a positive multiple of 128, at most 2^22; N >= 1; the packed
- * matrix below 2^40 bytes; lda (at most 2^22) and ldw at least K, multiples of
- * 16; a, w and w_packed 16-byte aligned; y aligned to its elements (PW_EINVAL
- * otherwise).
+ * Constraints: K a positive multiple of 128, at most 2^22; 1 <= N <= 2^30, 0 <=
+ * M <= 2^30; the packed matrix below 2^40 bytes; lda (at most 2^22) and ldw at
+ * least K, multiples of 16; a, w and w_packed 16-byte aligned; y aligned to its
+ * elements (PW_EINVAL otherwise).
  * ws: device workspace of at least pw_gemm_fp8_workspace bytes, 16-byte aligned
  * (PW_ENOMEM below; may be NULL where that is 0), in use until `stream` passes
  * the call. M = 0 does nothing. Deterministic: a fixed order of summation.   */
@@ -698,8 +698,8 @@ pw_status pw_attn_decode(const pw_kv_cache* cache, const void* q, int64_t ldq, i
  *   logits [T,E] of logit_type (PW_F32, PW_F16, PW_BF16), packed; bias [E]
  *   fp32; shared-expert columns, their gates and the outputs as in
  *   pw_route_topk_shared.
- * Constraints: those of pw_route_topk_shared; n_groups >= 1 divides E, n_groups
- * <= 64, 1 <= top_groups <= n_groups, K <= top_groups * (E / n_groups); w_scale
+ * Constraints: those of pw_route_topk_shared; T <= 2^30; n_groups >= 1 divides E,
+ * n_groups <= 64, 1 <= top_groups <= n_groups, K <= top_groups * (E / n_groups); w_scale
  * finite (PW_EINVAL otherwise). T = 0 writes offsets only.                   */
 enum { PW_SCORE_SOFTMAX = 0, PW_SCORE_SIGMOID = 1 };
 pw_status pw_route_grouped(const void* logits, int logit_type, const float* bias, int T, int E, int K, int score,

@@ -756,7 +756,7 @@ hipError_t launch_attn_bits(const AttnArgs& a, hipStream_t st) {
 }  // namespace
 
 // How the work is cut (see above).
-AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int, int max_len, int window) {
+AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int max_len, int window) {
   AttnPlan p{1, 4, 0, 0};
   int64_t tiles = (static_cast<int64_t>(max_len) + kTile - 1) / kTile;
   if (window > 0) {

@@ -92,7 +92,7 @@ struct AttnPlan {
   int n_shares;
   size_t ws_bytes;            // a slot's rows of head_dim + 2 floats each
 };
-AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int bits, int max_len, int window);
+AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int max_len, int window);
 
 size_t gemm8_workspace(int M, int N, int K);
 

@@ -21,7 +21,7 @@ bool rows_ok(int64_t ld, int64_t width) { return ld >= width && ld % 8 == 0; }
 
 // What is wrong with a packed matrix's shape, or nullptr.
 const char* packed_fault(int N, int K) {
-  if (N < 1 || K < 128 || K % 128 != 0) return "need N >= 1 and K a positive multiple of 128";
+  if (N < 1 || N > (1 << 30) || K < 128 || K % 128 != 0) return "need 1 <= N <= 2^30 and K a positive multiple of 128";
   if (K > (1 << 22) || (static_cast<int64_t>(N) + 15) / 16 * 16 * K >= (int64_t(1) << 40)) return "K above 2^22, or the matrix above 2^40 bytes";
   return nullptr;
 }
@@ -85,7 +85,7 @@ pw_status pw_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t 
 
 pw_status pw_gemm_fp8_workspace(int M, int N, int K, size_t* ws_bytes) {
   if (!ws_bytes) return set_error(PW_EINVAL, "null argument");
-  if (M < 0) return set_error(PW_EINVAL, "need M >= 0");
+  if (M < 0 || M > (1 << 30)) return set_error(PW_EINVAL, "need 0 <= M <= 2^30");
   if (const char* f = packed_fault(N, K)) return set_error(PW_EINVAL, f);
   *ws_bytes = pw::gemm8_workspace(M, N, K);
   return PW_OK;
@@ -109,7 +109,7 @@ pw_status pw_gemm_fp8_pack(const void* w, int64_t ldw, int N, int K, void* packe
 
 pw_status pw_gemm_fp8(const void* a, int64_t lda, const float* a_scale, const void* w_packed, const float* w_scale, int M,
                       int N, int K, void* y, int64_t ldy, int y_type, void* ws, size_t ws_bytes, void* stream) {
-  if (M < 0) return set_error(PW_EINVAL, "need M >= 0");
+  if (M < 0 || M > (1 << 30)) return set_error(PW_EINVAL, "need 0 <= M <= 2^30");
   if (const char* f = packed_fault(N, K)) return set_error(PW_EINVAL, f);
   if (y_type != PW_F16 && y_type != PW_BF16 && y_type != PW_F32)
     return set_error(PW_EINVAL, "y_type must be PW_F16, PW_BF16 or PW_F32");
@@ -155,7 +155,7 @@ pw_status pw_attn_workspace(const pw_kv_cache* c, int B, int n_q_heads, int max_
   if (const char* f = attn_fault(c, B, n_q_heads, max_len, window)) return set_error(PW_EINVAL, f);
   if (!ws_bytes) return set_error(PW_EINVAL, "null argument");
   if (attn_too_wide(B, n_q_heads)) return set_error(PW_EUNSUPPORTED, "B and n_q_heads must stay below 65536, their product below 2^23");
-  *ws_bytes = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window).ws_bytes;
+  *ws_bytes = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, max_len, window).ws_bytes;
   return PW_OK;
 }
 
@@ -173,7 +173,7 @@ pw_status pw_attn_decode(const pw_kv_cache* c, const void* q, int64_t ldq, int64
   if (!q || !seq_lens || !out || (max_len > 0 && !block_table)) return set_error(PW_EINVAL, "null argument");
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(lse, 4))
     return set_error(PW_EINVAL, "q and out must be 16-byte aligned, the other buffers 4-byte");
-  const pw::AttnPlan p = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window);
+  const pw::AttnPlan p = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, max_len, window);
   if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes)) return set_error(PW_ENOMEM, "workspace too small (pw_attn_workspace)");
   if (p.ws_bytes && !aligned(ws, 16)) return set_error(PW_EINVAL, "the workspace must be 16-byte aligned");
   pw::AttnArgs a{};
@@ -214,7 +214,7 @@ pw_status pw_route_grouped(const void* logits, int logit_type, const float* bias
   if (K > top_groups * (E / n_groups)) return set_error(PW_EINVAL, "K exceeds the experts of top_groups groups");
   if (!std::isfinite(w_scale)) return set_error(PW_EINVAL, "w_scale must be finite");
   const int Kt = K + n_shared;
-  if (static_cast<int64_t>(T) * Kt >= (int64_t(1) << 31)) return set_error(PW_EINVAL, "T*K too large");
+  if (T > (1 << 30) || static_cast<int64_t>(T) * Kt >= (int64_t(1) << 31)) return set_error(PW_EINVAL, "need T <= 2^30 and T * (K + n_shared) < 2^31");
   if (!offsets || (T > 0 && (!logits || !ids || !w || !sorted_slot || !slot_pos))) return set_error(PW_EINVAL, "null argument");
   pw::RouteArgs a{};
   a.logits = logits;

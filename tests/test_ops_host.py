@@ -191,3 +191,17 @@ def test_tensor_level_checks():
         ops.route_grouped(torch.zeros(4, 8), 2)
     with pytest.raises(pw.PWError):
         ops.KVCache(4, 32, 1, 96, torch.bfloat16)
+
+
+@pytest.mark.parametrize("bad", [dict(M=(1 << 30) + 1), dict(M=(1 << 31) - 1), dict(N=(1 << 30) + 1, ldy=(1 << 31) - 1),
+                                 dict(N=(1 << 31) - 1, ldy=(1 << 31) - 1)])
+def test_gemm_sizes_whose_tiles_pass_32_bits(bad):
+    """Sizes that the tile counts would overflow at are refused, K as small as it goes."""
+    _refused(pw.PW_EINVAL, _call(pw.pw_gemm_fp8, GEMM, GEMM_OK, **bad))
+    _refused(pw.PW_EINVAL, pw.pw_gemm_fp8_workspace, bad.get("M", 1), bad.get("N", 1), 128)
+    if "N" in bad:
+        _refused(pw.PW_EINVAL, pw.pw_gemm_fp8_packed_bytes, bad["N"], 128)
+
+
+def test_route_tokens_that_pass_32_bits():
+    _refused(pw.PW_EINVAL, _call(pw.pw_route_grouped, ROUTE, ROUTE_OK, K=1, T=(1 << 30) + 1))
