@@ -782,9 +782,21 @@ AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int max_l
     p.ws_bytes = static_cast<size_t>(resident + items) * slot;
     return p;
   }
-  int64_t n = (resident + items - 1) / items;
-  const int64_t most = (tiles + 15) / 16;
-  n = n < most ? n : most;
+  // A second workgroup per item costs the join, 5 to 6 us with its launch: it is
+  // left out where one workgroup takes no longer than that over the tiles, and
+  // where there is an item for every CU. 16 bits, 8 key heads, one workgroup /
+  // split (us): 128 channels, 4 sequences of 1000 tokens 13.0 / 15.3, of 1300
+  // 14.6 / 16.8, of 1600 18.1 / 16.4; 64 channels, of 2000 15.2 / 16.1, of 2800
+  // 20.2 / 15.9; 256 channels, of 400 12.4 / 16.2, of 800 18.8 / 18.2 (16.6 in
+  // finer splits); 2 key heads of 128, 64 sequences of 516 10.4 / 17.5. From 256
+  // items on: 32 sequences of 2000 42.6 / 48.7, of 2900 61.0 / 67.2, ragged 37.7 /
+  // 42.9, in 8 bits 34.5 / 38.6, ragged 30.7 / 26.7; 40 of 2000 61.5 / 58.5.
+  int64_t n = 1;
+  if (tiles * (head_dim + 64) > 8192 && items < 256) {
+    const int64_t most = (tiles + 15) / 16;
+    n = (resident + items - 1) / items;
+    n = n < most ? n : most;
+  }
   const int64_t per = ((tiles + n - 1) / n + kAttnWaves - 1) / kAttnWaves * kAttnWaves;
   n = (tiles + per - 1) / per;
   p.split_tiles = static_cast<int>(per);
