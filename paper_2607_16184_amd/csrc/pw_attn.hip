@@ -287,9 +287,9 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
 // Attention
 // ---------------------------------------------------------------------------
 //
-// One workgroup of four waves takes a split of a sequence for one key head and
-// up to 16 of its query heads; a wave takes every fourth tile of 32 tokens. In
-// matrix instructions of 16 x 16 x 32:
+// One workgroup of four or eight waves takes a split of a sequence for one key
+// head and up to 16 of its query heads; the waves take its tiles of 32 tokens in
+// turn. In matrix instructions of 16 x 16 x 32:
 //   scores S[token, head] = K q^T: two row tiles of 16 tokens, keys as the row
 //     operand straight from memory, queries (in registers all along) as the
 //     column operand; a lane then holds tokens 4 g .. 4 g + 3 of either tile
@@ -307,7 +307,8 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
 // scores, the values' scales the probabilities.
 
 constexpr int kTile = 32;
-constexpr int kAttnWaves = 4;
+constexpr int kAttnWaves = 4, kManyWaves = 8;
+constexpr int kFewBytes = 256;        // of a token's key, for the second
 constexpr float kNoMax = -1e30f;      // below every score, and exp2(-inf - it) = 0
 constexpr float kSlack = 8.0f;
 
@@ -378,26 +379,26 @@ __device__ __forceinline__ int block_at(const AttnArgs& a, int b, int tile) {
   return a.table[b * a.ld_table + (static_cast<int64_t>(tile) * kTile >> __builtin_ctz(a.kv.block_tokens))];   // (a power of two)
 }
 
-template <int D>
+template <int D, int W>
 struct AttnLds {
-  float o[kAttnWaves][16][D + 4];
-  float m[kAttnWaves][16], l[kAttnWaves][16];
+  float o[W][16][D + 4];
+  float m[W][16], l[W][16];
 };
 
 // Tiles [begin, end) of a sequence's span for one key head h and its query
-// heads 16 qt and up, by the workgroup. ids: block numbers of the wave's first
+// heads 16 qt and up, by the workgroup's W waves. ids: block numbers of the wave's first
 // 64 tiles, one per lane. whole: no other workgroup has tiles of the item, the
 // result goes to the output; else to slot `slot`.
-template <int ACT, int BITS, int D>
-__device__ __forceinline__ void attend(const AttnArgs& a, AttnLds<D>& lds, int b, int h, int qt, const Span& sp, int begin,
+template <int ACT, int BITS, int D, int W>
+__device__ __forceinline__ void attend(const AttnArgs& a, AttnLds<D, W>& lds, int b, int h, int qt, const Span& sp, int begin,
                                        int end, int ids, bool whole, int64_t slot) {
   constexpr int kPv = BITS == 8 ? PW_BF16 : ACT;      // 16-bit type of the second product
   constexpr int kLoads = D * BITS / 8 * 16 / 1024;    // 1 KB loads of 16 tokens' keys
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
   const int col = lane & 15, lg = lane >> 4;
   const int P = a.kv.block_tokens;
-  const int first = begin + wave;                                // the wave's tiles: first, first + 4, ...
-  const int n_my = first < end ? (end - first + kAttnWaves - 1) / kAttnWaves : 0;
+  const int first = begin + wave;                                // the wave's tiles: first, first + W, ...
+  const int n_my = first < end ? (end - first + W - 1) / W : 0;
 
   const int g = a.n_q_heads / a.kv.n_kv_heads;
   const int n_col = g - 16 * qt < 16 ? g - 16 * qt : 16;
@@ -418,7 +419,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, AttnLds<D>& lds, int b
   const auto advance = [&] {
     while (todo == 0 && chunk + 64 < n_my) {
       chunk += 64;
-      ids = chunk + lane < n_my ? block_at(a, b, sp.t0 + first + kAttnWaves * (chunk + lane)) : -1;
+      ids = chunk + lane < n_my ? block_at(a, b, sp.t0 + first + W * (chunk + lane)) : -1;
       todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
     }
     next_t = -1;
@@ -426,7 +427,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, AttnLds<D>& lds, int b
       const int l = __ffsll(static_cast<long long>(todo)) - 1;
       todo &= todo - 1;
       next_id = __builtin_amdgcn_readlane(ids, l);
-      next_t = (sp.t0 + first + kAttnWaves * (chunk + l)) * kTile;
+      next_t = (sp.t0 + first + W * (chunk + l)) * kTile;
     }
   };
   const size_t head_off = static_cast<size_t>(2 * h) * P * D * (BITS / 8);
@@ -559,7 +560,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, AttnLds<D>& lds, int b
     if (next_t >= 0) load_v();
   }
 
-  // join the four waves
+  // join the waves
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   if (col < n_col) {
@@ -572,15 +573,15 @@ __device__ __forceinline__ void attend(const AttnArgs& a, AttnLds<D>& lds, int b
   }
   __syncthreads();
   const int n_part = g < 16 ? g : 16;                            // rows of a slot
-  for (int e = threadIdx.x; e < n_col * (D / 4); e += 64 * kAttnWaves) {
+  for (int e = threadIdx.x; e < n_col * (D / 4); e += 64 * W) {
     const int c = e / (D / 4), d = 4 * (e % (D / 4));
     float mx = lds.m[0][c];
 #pragma unroll
-    for (int w = 1; w < kAttnWaves; ++w) mx = fmaxf(mx, lds.m[w][c]);
+    for (int w = 1; w < W; ++w) mx = fmaxf(mx, lds.m[w][c]);
     f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     float sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float f = __builtin_amdgcn_exp2f(lds.m[w][c] - mx);
       sum = fmaf(f, lds.l[w][c], sum);
       const f32x4 x = *reinterpret_cast<const f32x4*>(&lds.o[w][c][d]);
@@ -604,29 +605,29 @@ __device__ __forceinline__ void attend(const AttnArgs& a, AttnLds<D>& lds, int b
   }
 }
 
-template <int ACT, int BITS, int D>
-__global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn(AttnArgs a, int q_tiles) {
-  __shared__ AttnLds<D> lds;
+template <int ACT, int BITS, int D, int W>
+__global__ __launch_bounds__(64 * W, D <= 128 || W > kAttnWaves ? 2 : 1) void k_attn(AttnArgs a, int q_tiles) {
+  __shared__ AttnLds<D, W> lds;
   const int split = blockIdx.x, b = blockIdx.z;
   const int h = q_tiles == 1 ? blockIdx.y : blockIdx.y / q_tiles, qt = q_tiles == 1 ? 0 : blockIdx.y % q_tiles;
   const int wave = static_cast<int>(threadIdx.x) >> 6, lane = lane_id();
   const int begin = split * a.split_tiles;
   // Without a window the block numbers do not hang on the sequence's length, so
   // they come along with it (what lies past the length is dropped later).
-  int ids = a.window == 0 ? block_at(a, b, begin + wave + kAttnWaves * lane) : -1;
+  int ids = a.window == 0 ? block_at(a, b, begin + wave + W * lane) : -1;
   const Span sp = span_of(a, a.lens[b]);
   const int n_act = (sp.tiles + a.split_tiles - 1) / a.split_tiles;
   if (split > 0 && split >= n_act) return;
-  if (a.window > 0) ids = block_at(a, b, sp.t0 + begin + wave + kAttnWaves * lane);
+  if (a.window > 0) ids = block_at(a, b, sp.t0 + begin + wave + W * lane);
   const int end = begin + a.split_tiles < sp.tiles ? begin + a.split_tiles : sp.tiles;
   const int64_t item = static_cast<int64_t>(b) * gridDim.y + blockIdx.y;
-  attend<ACT, BITS, D>(a, lds, b, h, qt, sp, begin, end, ids, n_act <= 1, item * a.n_splits + split);
+  attend<ACT, BITS, D, W>(a, lds, b, h, qt, sp, begin, end, ids, n_act <= 1, item * a.n_splits + split);
 }
 
 // The workgroup's share, an item's part after the other.
 template <int ACT, int BITS, int D>
 __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn_shares(AttnArgs a, int q_tiles) {
-  __shared__ AttnLds<D> lds;
+  __shared__ AttnLds<D, kAttnWaves> lds;
   const int w = blockIdx.x, wave = static_cast<int>(threadIdx.x) >> 6, lane = lane_id();
   const int per_seq = a.kv.n_kv_heads * q_tiles;                 // items of a sequence
   // lane l sums sequences l per .. (l + 1) per - 1, then the lanes' sums
@@ -659,7 +660,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, D <= 128 ? 2 : 1) void k_attn_shar
     const int n = min(sp.tiles - begin, stop - pos);
     const int h = item / q_tiles, qt = item % q_tiles;
     const int ids = block_at(a, b, sp.t0 + begin + wave + kAttnWaves * lane);
-    attend<ACT, BITS, D>(a, lds, b, h, qt, sp, begin, begin + n, ids, n == sp.tiles,
+    attend<ACT, BITS, D, kAttnWaves>(a, lds, b, h, qt, sp, begin, begin + n, ids, n == sp.tiles,
                          w + static_cast<int64_t>(b) * per_seq + item);
     pos += n;
     if (pos >= stop) return;
@@ -732,8 +733,12 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 template <int ACT, int BITS, int D>
 hipError_t launch_attn_d(const AttnArgs& a, hipStream_t st) {
   const int g = a.n_q_heads / a.kv.n_kv_heads, q_tiles = (g + 15) / 16;
-  if (a.n_splits > 0)
-    k_attn<ACT, BITS, D><<<dim3(a.n_splits, a.kv.n_kv_heads * q_tiles, a.B), 64 * kAttnWaves, 0, st>>>(a, q_tiles);
+  const dim3 items(a.n_splits, a.kv.n_kv_heads * q_tiles, a.B);
+  constexpr int kMost = D * BITS / 8 <= kFewBytes ? kManyWaves : kAttnWaves;
+  if (a.n_splits > 0 && a.many_waves)
+    k_attn<ACT, BITS, D, kMost><<<items, 64 * kMost, 0, st>>>(a, q_tiles);
+  else if (a.n_splits > 0)
+    k_attn<ACT, BITS, D, kAttnWaves><<<items, 64 * kAttnWaves, 0, st>>>(a, q_tiles);
   else
     k_attn_shares<ACT, BITS, D><<<a.n_shares, 64 * kAttnWaves, 0, st>>>(a, q_tiles);
   hipError_t e = hipGetLastError();
@@ -756,8 +761,8 @@ hipError_t launch_attn_bits(const AttnArgs& a, hipStream_t st) {
 }  // namespace
 
 // How the work is cut (see above).
-AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int max_len, int window) {
-  AttnPlan p{1, 4, 0, 0};
+AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int bits, int max_len, int window) {
+  AttnPlan p{1, kManyWaves, 0, 0, 0};
   int64_t tiles = (static_cast<int64_t>(max_len) + kTile - 1) / kTile;
   if (window > 0) {
     const int64_t w = (static_cast<int64_t>(window) + 2 * kTile - 2) / kTile;   // a window that starts inside a tile
@@ -782,25 +787,33 @@ AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int max_l
     p.ws_bytes = static_cast<size_t>(resident + items) * slot;
     return p;
   }
+  // A CU reads 57 KB/us at most, which four waves reach with more than 16 KB each
+  // in flight; smaller tiles take eight where there are no more workgroups than
+  // CUs. Eight / four waves (us): 8 bits, 4 sequences of 1000 tokens with 8 key
+  // heads of 128 9.6 / 12.3, 16 of them 11.5 / 13.3, 32 of 1300 16.4 / 18.3; heads
+  // of 64 in 16 bits, 4 of 1500 10.3 / 13.0; of 256 in 8 bits, 16 of 600 13.3 /
+  // 14.6; of 128 in 16 bits 12.9 / 13.0.
   // A second workgroup per item costs the join, 5 to 6 us with its launch: it is
   // left out where one workgroup takes no longer than that over the tiles, and
   // where there is an item for every CU. 16 bits, 8 key heads, one workgroup /
   // split (us): 128 channels, 4 sequences of 1000 tokens 13.0 / 15.3, of 1300
-  // 14.6 / 16.8, of 1600 18.1 / 16.4; 64 channels, of 2000 15.2 / 16.1, of 2800
-  // 20.2 / 15.9; 256 channels, of 400 12.4 / 16.2, of 800 18.8 / 18.2 (16.6 in
-  // finer splits); 2 key heads of 128, 64 sequences of 516 10.4 / 17.5. From 256
-  // items on: 32 sequences of 2000 42.6 / 48.7, of 2900 61.0 / 67.2, ragged 37.7 /
-  // 42.9, in 8 bits 34.5 / 38.6, ragged 30.7 / 26.7; 40 of 2000 61.5 / 58.5.
+  // 14.6 / 16.8, of 1600 18.1 / 16.4; 256 channels, of 400 12.4 / 16.2, of 800
+  // 18.8 / 18.2 (16.6 in finer splits); 2 key heads of 128, 64 sequences of 516
+  // 10.4 / 17.5. From 256 items on: 32 sequences of 2000 42.6 / 48.7, of 2900 61.0
+  // / 67.2, ragged 37.7 / 42.9, in 8 bits 34.5 / 38.6, ragged 30.7 / 26.7; 40 of
+  // 2000 61.5 / 58.5.
+  const int row = head_dim * bits / 8;
   int64_t n = 1;
-  if (tiles * (head_dim + 64) > 8192 && items < 256) {
+  if (tiles * (row < 128 ? 128 : row) > 40 * 256 && items < 256) {
     const int64_t most = (tiles + 15) / 16;
     n = (resident + items - 1) / items;
     n = n < most ? n : most;
   }
-  const int64_t per = ((tiles + n - 1) / n + kAttnWaves - 1) / kAttnWaves * kAttnWaves;
+  const int64_t per = ((tiles + n - 1) / n + kManyWaves - 1) / kManyWaves * kManyWaves;
   n = (tiles + per - 1) / per;
   p.split_tiles = static_cast<int>(per);
   p.n_splits = static_cast<int>(n);
+  p.many_waves = row <= kFewBytes && items * n <= 256;
   if (n > 1) p.ws_bytes = static_cast<size_t>(items * n) * slot;
   return p;
 }

@@ -68,7 +68,7 @@ struct AttnArgs {
   float scale;
   uint16_t* out;
   float* lse;
-  int n_splits, split_tiles, n_shares;
+  int n_splits, split_tiles, n_shares, many_waves;
   float* part_o;           // [slots][min(16, query heads per key head)][D], not normalised
   float* part_ml;          // [slots][the same][2]: maximum (base 2), sum
 };
@@ -90,9 +90,10 @@ struct RouteArgs {
 struct AttnPlan {
   int n_splits, split_tiles;  // n_splits 0: equal shares of all tiles
   int n_shares;
+  int many_waves;             // eight waves per workgroup, else four
   size_t ws_bytes;            // a slot's rows of head_dim + 2 floats each
 };
-AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int max_len, int window);
+AttnPlan attn_plan(int B, int n_q_heads, int n_kv_heads, int head_dim, int bits, int max_len, int window);
 
 size_t gemm8_workspace(int M, int N, int K);
 

@@ -155,7 +155,7 @@ pw_status pw_attn_workspace(const pw_kv_cache* c, int B, int n_q_heads, int max_
   if (const char* f = attn_fault(c, B, n_q_heads, max_len, window)) return set_error(PW_EINVAL, f);
   if (!ws_bytes) return set_error(PW_EINVAL, "null argument");
   if (attn_too_wide(B, n_q_heads)) return set_error(PW_EUNSUPPORTED, "B and n_q_heads must stay below 65536, their product below 2^23");
-  *ws_bytes = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, max_len, window).ws_bytes;
+  *ws_bytes = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window).ws_bytes;
   return PW_OK;
 }
 
@@ -173,7 +173,7 @@ pw_status pw_attn_decode(const pw_kv_cache* c, const void* q, int64_t ldq, int64
   if (!q || !seq_lens || !out || (max_len > 0 && !block_table)) return set_error(PW_EINVAL, "null argument");
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(lse, 4))
     return set_error(PW_EINVAL, "q and out must be 16-byte aligned, the other buffers 4-byte");
-  const pw::AttnPlan p = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, max_len, window);
+  const pw::AttnPlan p = pw::attn_plan(B, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window);
   if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes)) return set_error(PW_ENOMEM, "workspace too small (pw_attn_workspace)");
   if (p.ws_bytes && !aligned(ws, 16)) return set_error(PW_EINVAL, "the workspace must be 16-byte aligned");
   pw::AttnArgs a{};
@@ -194,6 +194,7 @@ pw_status pw_attn_decode(const pw_kv_cache* c, const void* q, int64_t ldq, int64
   a.n_splits = p.n_splits;
   a.split_tiles = p.split_tiles;
   a.n_shares = p.n_shares;
+  a.many_waves = p.many_waves;
   a.part_o = static_cast<float*>(ws);
   a.part_ml = a.part_o + p.ws_bytes / sizeof(float) / (c->head_dim + 2) * c->head_dim;
   return launched(pw::launch_attn(a, static_cast<hipStream_t>(stream)), "attention launch");

@@ -497,6 +497,19 @@ def test_attend_equal_shares_of_many_sequences(window):
     _attend_case([0] * 150, 32, 2, 2, 64, BF, 16, window=window, seed=7, max_len=5000)
 
 
+@pytest.mark.parametrize("B", [256, 257])
+@pytest.mark.parametrize("D,bits,act", [(64, 16, FP), (128, 8, BF), (128, 16, BF), (192, 8, FP), (256, 8, BF), (256, 16, FP)])
+def test_attend_around_one_workgroup_per_cu(B, D, bits, act):
+    """Lengths around the tiles of four and of eight waves, and of none."""
+    _attend_case([(53 * i + 31 * (i % 4)) % 300 for i in range(B)], 32, 1, 3, D, act, bits, seed=B)
+
+
+@pytest.mark.parametrize("tiles", [19, 20, 21, 39, 40, 41, 79, 80, 81])
+@pytest.mark.parametrize("D,bits", [(64, 16), (128, 8), (128, 16), (256, 16)])
+def test_attend_around_the_first_split(tiles, D, bits):
+    _attend_case([32 * tiles, 32 * tiles - 31, 5], 64, 1, 2, D, BF, bits, seed=tiles, max_len=32 * tiles)
+
+
 def test_attend_runs_twice_the_same_and_on_other_streams():
     side = torch.cuda.Stream()
     _, a = _attend_case([3000, 50], 64, 2, 4, 128, BF, 8, seed=4)
