@@ -243,9 +243,14 @@ def route_grouped(logits: torch.Tensor, K: int, score: str = "softmax", bias: to
     if out is None:
         with torch.cuda.stream(stream):
             out = PagedLayer.routing_buffers(T, E + n_shared, Kt, logits.device)
-    ids, w, offsets, ss, sp = out
-    _need(ids.shape == (T, Kt) and w.shape == (T, Kt) and offsets.numel() == E + n_shared + 1
-          and min(ss.numel(), sp.numel()) >= T * Kt, "the routing buffers are of another size (PagedLayer.routing_buffers)")
+        ids, w, offsets, ss, sp = out
+    else:
+        ids, w, offsets, ss, sp = out
+        _packed(ids, (T, Kt), torch.int32, "ids")
+        _packed(w, (T, Kt), torch.float32, "w")
+        for t, n in ((offsets, E + n_shared + 1), (ss, T * Kt), (sp, T * Kt)):
+            _need(t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() >= n,
+                  "the routing buffers are of another kind (PagedLayer.routing_buffers)")
     pw.pw_route_grouped(logits.data_ptr(), _TYPE[logits.dtype], _ptr(bias), T, E, K, _SCORE[score], groups, top_groups,
                         group_top, int(renorm), scale, n_shared, _ptr(gate), ids.data_ptr(), w.data_ptr(),
                         offsets.data_ptr(), ss.data_ptr(), sp.data_ptr(), _on(logits, stream))

@@ -741,3 +741,15 @@ def test_gemm_fp32_sums_are_fp32(M, N, K):
     want = af @ (w.double() * w_s.double().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)).T
     off = float((y - want).norm() / want.norm())
     assert off <= (K / 32 + K / 128) ** 0.5 * 2.0 ** -22, off
+
+
+def test_route_refuses_other_buffers():
+    from paper_2607_16184_amd.layer import PagedLayer
+    ops, logits = _ops(), torch.randn(6, 16, device="cuda")
+    good = PagedLayer.routing_buffers(6, 16, 4)
+    ops.route_grouped(logits, 4, out=good)
+    for i in range(5):
+        short = good[i][:2] if i < 2 else good[i][:-1]
+        for bad in (good[i].cpu(), good[i].double(), short):
+            with pytest.raises(ValueError):
+                ops.route_grouped(logits, 4, out=tuple(bad if j == i else t for j, t in enumerate(good)))
