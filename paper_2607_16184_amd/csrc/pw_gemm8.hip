@@ -227,12 +227,22 @@ hipError_t launch_stream(const Gemm8Args& a, hipStream_t st) {
 }
 
 // Two row tiles per workgroup share its loads of the tokens, where enough
-// workgroups are left.
+// workgroups are left. 33 to 64 tokens go to one workgroup, or to two that read
+// the weights twice: to one where the row tiles' workgroups fit the CUs once and
+// twice as many do not. Two / one (us): 40 tokens x 2048 x 2048 (128 row units)
+// 6.0 / 6.7, x 2560 x 2048 (160) 7.5 / 6.8, x 6144 x 4096 (192) 14.6 / 12.1; 64 x
+// 6144 x 4096 16.6 / 14.9, x 8192 x 2048 (256; 56 tokens) 10.6 / 9.7, x 12288 x
+// 1024 (384) 8.6 / 9.8.
+template <int RT, bool WIDE>
+hipError_t launch_stream_rows(const Gemm8Args& a, hipStream_t st) {
+  const int units = (a.N + 16 * RT - 1) / (16 * RT);
+  if (a.M <= 16) return launch_stream<RT, 1, WIDE>(a, st);
+  if (a.M <= 32 || a.M > 64 || units <= 128 || units > 256) return launch_stream<RT, 2, WIDE>(a, st);
+  return a.M <= 48 ? launch_stream<RT, 3, WIDE>(a, st) : launch_stream<RT, 4, WIDE>(a, st);
+}
 template <bool WIDE>
 hipError_t launch_stream_of(const Gemm8Args& a, hipStream_t st) {
-  const bool two = a.N >= 5120;
-  if (a.M <= 16) return two ? launch_stream<2, 1, WIDE>(a, st) : launch_stream<1, 1, WIDE>(a, st);
-  return two ? launch_stream<2, 2, WIDE>(a, st) : launch_stream<1, 2, WIDE>(a, st);
+  return a.N >= 5120 ? launch_stream_rows<2, WIDE>(a, st) : launch_stream_rows<1, WIDE>(a, st);
 }
 
 // Tiled kernel: TN weight rows x TM tokens per workgroup, WN x WM waves. K
@@ -496,7 +506,7 @@ __global__ __launch_bounds__(256) void k_gemm8_join(Gemm8Args a) {
 
 // Which kernel runs, and into how many parts K is cut. Measured (us):
 //   streaming / 128 x 128 tiles: 64 tokens x 1024 x 2048 5.8 / 11.8, x 4000 x
-//     2048 8.9 / 13.2, x 6144 x 4096 16.8 / 17.2, x 4096 x 14336 45 / 23.9, x
+//     2048 8.9 / 13.2, x 6144 x 4096 14.9 / 17.2, x 4096 x 14336 45 / 23.9, x
 //     28672 x 4096 52.6 / 34.0; 128 x 4000 x 2048 14.8 / 14.6;
 //   128 x 128 tiles whole / in parts of K: 128 x 6144 x 4096 24.1 / 18.0, 128 x
 //     4096 x 14336 109 / 27, 256 x 4000 x 2048 14.3 / 18.9;

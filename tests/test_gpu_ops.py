@@ -753,3 +753,12 @@ def test_route_refuses_other_buffers():
         for bad in (good[i].cpu(), good[i].double(), short):
             with pytest.raises(ValueError):
                 ops.route_grouped(logits, 4, out=tuple(bad if j == i else t for j, t in enumerate(good)))
+
+
+@pytest.mark.parametrize("M", [33, 48, 49, 64])
+@pytest.mark.parametrize("N,K", [(2048, 256), (2049, 384), (4096, 256), (4112, 256), (5120, 384), (8192, 256), (8193, 256)])
+@pytest.mark.parametrize("out", [BF, F32])
+def test_gemm_decode_batches(M, N, K, out):
+    """One and two workgroups for the tokens, one and two row tiles."""
+    a, a_s, w, w_s = _gemm_case(M, N, K, M + N)
+    _check_gemm(_ops().Linear8(w.cuda(), w_s.cuda()).forward(a.cuda(), a_s.cuda(), dtype=out), a, a_s, w, w_s)
