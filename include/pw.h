@@ -667,7 +667,9 @@ pw_status pw_kv_append(const pw_kv_cache* cache, const void* k, const void* v, i
  * A sequence of length 0 (or less) gives zeros and an lse of -infinity.
  * Positions in a block outside 0 .. n_blocks - 1 are left out. What lies in
  * the cache outside the attended positions is not used, NaN and infinities
- * included. Scores, softmax and sums are in fp32.
+ * included. Scores, exponentials and sums are in fp32; a weight enters the product
+ * with the values to within 2^-16 of itself, however small it is (in fp16 caches
+ * and 2^-52 of the row's largest weight).
  * Constraints: B >= 0; n_q_heads a multiple of n_kv_heads; max_len >= 0, below
  * 2^31 - 256; window >= 0; scale finite (PW_EINVAL otherwise); B and
  * n_q_heads < 65536, their product < 2^23 (PW_EUNSUPPORTED: split the batch).
