@@ -323,7 +323,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
 constexpr int kTile = 32;
 constexpr int kAttnWaves = 4, kManyWaves = 8;
 constexpr int kFewBytes = 256;        // of a token's key, for the second
-constexpr float kNoMax = -1e30f;      // below every score, and exp2(-inf - it) = 0
+constexpr float kNoMax = -3.402823466e38f;   // no finite score is below it, and exp2(-inf - it) = 0
 constexpr float kSlack = 8.0f;
 constexpr float kLift = 32768.0f, kLow = 4096.0f;   // factors of fp16 probabilities and of their second term
 

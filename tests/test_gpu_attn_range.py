@@ -81,3 +81,26 @@ def test_sink_before_equal_keys_in_one_workgroup():
     k, v, q = k.to(FP), v.to(FP), q.to(FP)
     out, lse = _attend([k, k], [v, v], q, 64, FP, 16)
     _check(out, lse, [k, k], [v, v], q, FP, 16)
+
+
+@pytest.mark.parametrize("act,bits", [(BF, 16), (BF, 8)])
+@pytest.mark.parametrize("lens,max_len", [([1, 20, 33, 300], None), ([5000], None), ([1500, 40, 7000], 40000)])
+def test_scores_near_the_lowest_number(act, bits, lens, max_len):
+    """Scores of -2^105 and multiples of it, none above: the softmax is that of
+    their differences, the lowest magnitude's tokens in equal parts."""
+    g = _gen(len(lens))
+    k, v = [], []
+    for n in lens:
+        kb = torch.randn(n, 2, 64, generator=g)
+        kb[:, :, 1] = -2.0 ** 55 * (1 + torch.arange(n) % 4)[:, None]
+        k.append(kb.to(act))
+        v.append(torch.randn(n, 2, 64, generator=g).to(act))
+    q = torch.zeros(len(lens), 4, 64)
+    q[:, :, 1] = 2.0 ** 50
+    q = q.to(act)
+    out, lse = _attend(k, v, q, 64, act, bits, max_len)
+    for b, n in enumerate(lens):
+        vv = R.cached(v[b], bits)[::4].repeat_interleave(2, 1)
+        o, mass = vv.mean(0), vv.abs().mean(0)
+        _within(out[b], o, R.U[act] * (1 + 2 ** -8) * o.abs() + ((n + 64) * 2.0 ** -23 + 2.0 ** -15) * mass, "row %d" % b)
+        _within(lse[b], torch.full((4,), -2.0 ** 105), torch.tensor(2.0 ** 105 * 2.0 ** -21), "lse %d" % b)
