@@ -38,14 +38,24 @@ class BlockTables:
         self.table = np.full((sequences, -(-max_len // block_tokens)), -1, dtype=np.int32)
         self.length = np.zeros(sequences, dtype=np.int64)
 
-    def extend(self, sequence: int, tokens: int) -> np.ndarray:
-        """The slots of the sequence's next tokens."""
+    def _new_blocks(self, sequence: int, tokens: int) -> range:
+        """The table columns that so many more tokens need, refused where they
+        cannot be had; nothing is changed."""
+        if not 0 <= sequence < len(self.length):
+            raise ValueError("there is no sequence %d" % sequence)
+        if tokens < 0:
+            raise ValueError("sequence %d: %d tokens" % (sequence, tokens))
         first, last = int(self.length[sequence]), int(self.length[sequence]) + tokens
         if last > self.max_len:
             raise ValueError("sequence %d would pass %d tokens" % (sequence, self.max_len))
-        new = range(-(-first // self.P), -(-last // self.P))
+        return range(-(-first // self.P), -(-last // self.P))
+
+    def extend(self, sequence: int, tokens: int) -> np.ndarray:
+        """The slots of the sequence's next tokens."""
+        new = self._new_blocks(sequence, tokens)
         if len(new) > len(self.free):
             raise MemoryError("no block is free")
+        first, last = int(self.length[sequence]), int(self.length[sequence]) + tokens
         for i in new:
             self.table[sequence, i] = self.free.pop()
         self.length[sequence] = last
@@ -60,10 +70,13 @@ class BlockTables:
 
     def step(self, sequences: Sequence[int], tokens: Sequence[int], device="cuda"):
         """(block_table, lens, slots) of a step that gives each listed sequence
-        so many new tokens, a row per token."""
+        so many new tokens, a row per token. A step that is refused changes
+        nothing."""
         if len(set(sequences)) < len(sequences):
             raise ValueError("a sequence is listed once, with all its new tokens")
-        need = sum(-(-(int(self.length[s]) + n) // self.P) - -(-int(self.length[s]) // self.P) for s, n in zip(sequences, tokens))
+        if len(tokens) != len(sequences):
+            raise ValueError("%d counts of tokens for %d sequences" % (len(tokens), len(sequences)))
+        need = sum(len(self._new_blocks(s, n)) for s, n in zip(sequences, tokens))
         if need > len(self.free):
             raise MemoryError("%d blocks are needed, %d are free" % (need, len(self.free)))
         slots = [self.extend(s, n) for s, n in zip(sequences, tokens)]

@@ -46,3 +46,26 @@ def test_refusals():
     with pytest.raises(MemoryError):
         BlockTables(3, 32, 2, 100).step([0, 1], [64, 64], device="cpu")
     assert len(t.free) == 4 and not t.length.any()
+
+
+@pytest.mark.parametrize("sequences,tokens,error", [
+    ([0, 1], [10, 51], ValueError),          # the second would pass max_len
+    ([1, 0], [3, 50], ValueError),           # the second would, with what it has
+    ([0, 1], [10], ValueError), ([0], [10, 10], ValueError),
+    ([0, 1], [10, -1], ValueError), ([1], [-2], ValueError),
+    ([0, 3], [10, 1], ValueError), ([2, -1], [10, 1], ValueError),
+    ([0, 1, 2], [49, 50, 50], MemoryError)])
+def test_a_refused_step_changes_nothing(sequences, tokens, error):
+    """Also where the fault lies with a later sequence of the step."""
+    t = BlockTables(5, 32, 3, 50)
+    t.step([0, 1], [1, 2], device="cpu")
+    t.release(1)
+    table, length, free = t.table.copy(), t.length.copy(), list(t.free)
+    with pytest.raises(error):
+        t.step(sequences, tokens, device="cpu")
+    assert np.array_equal(t.table, table) and np.array_equal(t.length, length) and t.free == free
+    for s, n in zip(sequences, tokens):
+        if n < 0:
+            with pytest.raises(error):
+                t.extend(s, n)
+            assert np.array_equal(t.table, table) and np.array_equal(t.length, length) and t.free == free
