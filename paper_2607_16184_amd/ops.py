@@ -10,7 +10,8 @@ Work goes to the current stream, or to ``stream``: what this module allocates
 then belongs to that stream; the caller orders it after whatever wrote the
 inputs, and keeps them until it is done. A handle may be used on several
 streams; graphs that were captured on one stream share its workspace and are
-replayed one after the other.
+replayed one after the other. A call's tensors and its stream belong to one
+device, which need not be the current one.
 """
 from __future__ import annotations
 
@@ -34,15 +35,29 @@ def _ptr(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.data_ptr()
 
 
-def _on(t: torch.Tensor, stream) -> int:
-    """The given stream, or the current one of the tensor's device. (Its raw
-    handle: 0.1 us, a Stream object 3 us, as long as a launch.)"""
-    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
+def _on(dev: int, stream) -> int:
+    """The given stream, or the current one of the device. (Its raw handle: 0.1
+    us, a Stream object 3 us, as long as a launch.)"""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError("the stream belongs to device %d, the tensors to %d" % (stream.device_index, dev))
+    return stream.cuda_stream
 
 
-def _packed(t: Optional[torch.Tensor], shape, dtype, name: str):
-    if t is not None and not (t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous()):
-        raise ValueError("%s must be a contiguous device tensor of %s, %s" % (name, shape, dtype))
+def _call(dev: int, fn, *args):
+    """fn(*args) with `dev` as the current device: a default stream's handle (0)
+    means the current device's."""
+    if torch._C._cuda_getDevice() == dev:
+        fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            fn(*args)
+
+
+def _packed(t: Optional[torch.Tensor], shape, dtype, dev: int, name: str):
+    if t is not None and not (t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous()):
+        raise ValueError("%s must be a contiguous tensor of %s, %s, on device %d" % (name, tuple(shape), dtype, dev))
 
 
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
@@ -62,17 +77,18 @@ class _Workspace:
     def __init__(self, device):
         self.device, self.of, self.kept = device, {}, []
 
-    def run(self, st: int, stream, fn, args, need):
+    def run(self, dev: int, stream, fn, args, need):
+        st = _on(dev, stream)
         at = self.of.get(st, (0, 0))
         try:
-            fn(*args, *at, st)
+            _call(dev, fn, *args, *at, st)
         except pw.PWError as e:
             if e.status != pw.PW_ENOMEM:
                 raise
             t = _empty(1 << (need() - 1).bit_length(), torch.uint8, self.device, stream)
             self.kept.append(t)
             at = self.of[st] = (t.data_ptr(), t.numel())
-            fn(*args, *at, st)
+            _call(dev, fn, *args, *at, st)
 
 
 # ---------------------------------------------------------------------------
@@ -96,27 +112,27 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: O
     """Root-mean-square norm of x (+ residual): (sum, y16, y8, y8_scale), the
     wanted ones of them or those that ``out`` holds (pw_rms_norm)."""
     T, H = x.shape
-    act = x.dtype
+    act, dev = x.dtype, x.get_device()
     ldx, inner = x.stride()
-    _need((act is torch.bfloat16 or act is torch.float16) and x.is_cuda and inner == 1, "x must be 16-bit rows on the device")
+    _need((act is torch.bfloat16 or act is torch.float16) and dev >= 0 and inner == 1, "x must be 16-bit rows on the device")
     ldr = H
     if residual is not None:
         ldr, inner = residual.stride()
-        _need(residual.shape == x.shape and residual.dtype is act and residual.is_cuda and inner == 1,
-              "residual must have x's shape and type")
+        _need(residual.shape == x.shape and residual.dtype is act and residual.get_device() == dev and inner == 1,
+              "residual must have x's shape, type and device")
     if T <= 1:                         # a single row may have any stride
         ldx = ldr = H
-    _packed(weight, (H,), act, "weight")
+    _packed(weight, (H,), act, dev, "weight")
     if out is None:
         with torch.cuda.stream(stream):
             out = norm_buffers(T, H, act, residual is not None, y16, y8, x.device)
     s, y, q, qs = out
-    _packed(s, (T, H), act, "the sum")
-    _packed(y, (T, H), act, "y16")
-    _packed(q, (T, H), _F8, "y8")
-    _packed(qs, (T, H // 128), torch.float32, "y8_scale")
-    pw.pw_rms_norm(x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), T, H, eps, _TYPE[act], _ptr(s), _ptr(y), _ptr(q),
-                   _ptr(qs), _on(x, stream))
+    _packed(s, (T, H), act, dev, "the sum")
+    _packed(y, (T, H), act, dev, "y16")
+    _packed(q, (T, H), _F8, dev, "y8")
+    _packed(qs, (T, H // 128), torch.float32, dev, "y8_scale")
+    _call(dev, pw.pw_rms_norm, x.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), T, H, eps, _TYPE[act], _ptr(s), _ptr(y),
+          _ptr(q), _ptr(qs), _on(dev, stream))
     return out
 
 
@@ -131,14 +147,15 @@ class Linear8:
     kept."""
 
     def __init__(self, w8: torch.Tensor, w_scale: torch.Tensor, stream=None):
-        _need(w8.dtype is _F8 and w8.dim() == 2 and w8.stride(1) == 1 and w8.is_cuda, "w8 must be e4m3 rows on the device")
+        self.dev = dev = w8.get_device()
+        _need(w8.dtype is _F8 and w8.dim() == 2 and w8.stride(1) == 1 and dev >= 0, "w8 must be e4m3 rows on the device")
         self.N, self.K = w8.shape
         _need(self.K % 128 == 0, "K must be a multiple of 128")
-        _packed(w_scale, (-(-self.N // 128), self.K // 128), torch.float32, "w_scale")
+        _packed(w_scale, (-(-self.N // 128), self.K // 128), torch.float32, dev, "w_scale")
         self.w_scale = w_scale
         self.packed = _empty(pw.pw_gemm_fp8_packed_bytes(self.N, self.K), torch.uint8, w8.device, stream)
-        pw.pw_gemm_fp8_pack(w8.data_ptr(), w8.stride(0) if self.N > 1 else self.K, self.N, self.K, self.packed.data_ptr(),
-                            _on(w8, stream))
+        _call(dev, pw.pw_gemm_fp8_pack, w8.data_ptr(), w8.stride(0) if self.N > 1 else self.K, self.N, self.K,
+              self.packed.data_ptr(), _on(dev, stream))
         if stream is not None:
             w8.record_stream(stream)       # the caller may drop it before the packing has run
         self._ws = _Workspace(w8.device)
@@ -147,16 +164,17 @@ class Linear8:
                 stream=None) -> torch.Tensor:
         """x8 [M, K] e4m3 rows with x_scale [M, K / 128] (as rms_norm gives
         them) -> [M, N] (pw_gemm_fp8)."""
-        M, N, K = x8.shape[0], self.N, self.K
-        _need(x8.dtype is _F8 and x8.shape == (M, K) and x8.is_cuda and x8.stride(1) == 1, "x8 must be [M, K] e4m3 rows")
-        _packed(x_scale, (M, K // 128), torch.float32, "x_scale")
+        M, N, K, dev = x8.shape[0], self.N, self.K, self.dev
+        _need(x8.dtype is _F8 and x8.shape == (M, K) and x8.get_device() == dev and x8.stride(1) == 1,
+              "x8 must be [M, K] e4m3 rows on the weights' device")
+        _packed(x_scale, (M, K // 128), torch.float32, dev, "x_scale")
         if out is None:
             out = _empty((M, N), dtype, x8.device, stream)
-        _need(out.shape == (M, N) and out.dtype in _TYPE and out.is_cuda and (N == 1 or out.stride(1) == 1),
-              "out must be [M, N] rows")
+        _need(out.shape == (M, N) and out.dtype in _TYPE and out.get_device() == dev and (N == 1 or out.stride(1) == 1),
+              "out must be [M, N] rows on the weights' device")
         args = (x8.data_ptr(), x8.stride(0) if M > 1 else K, x_scale.data_ptr(), self.packed.data_ptr(),
                 self.w_scale.data_ptr(), M, N, K, out.data_ptr(), out.stride(0) if M > 1 else N, _TYPE[out.dtype])
-        self._ws.run(_on(x8, stream), stream, pw.pw_gemm_fp8, args, lambda: pw.pw_gemm_fp8_workspace(M, N, K))
+        self._ws.run(dev, stream, pw.pw_gemm_fp8, args, lambda: pw.pw_gemm_fp8_workspace(M, N, K))
         return out
 
 
@@ -179,7 +197,8 @@ class KVCache:
         self.desc.block_stride = block_stride or self.block_bytes
         if pool is None:
             pool = torch.empty(max(n_blocks - 1, 0) * self.desc.block_stride + self.block_bytes, dtype=torch.uint8, device=device)
-        _need(pool.dtype == torch.uint8 and pool.is_contiguous() and pool.is_cuda, "the pool must be contiguous device bytes")
+        self.dev = pool.get_device()
+        _need(pool.dtype == torch.uint8 and pool.is_contiguous() and self.dev >= 0, "the pool must be contiguous device bytes")
         _need(pool.numel() >= (n_blocks - 1) * self.desc.block_stride + self.block_bytes, "the pool is smaller than its blocks")
         self.pool = pool
         self.desc.pool = pool.data_ptr()
@@ -188,13 +207,14 @@ class KVCache:
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
         """Write k, v [T, kv_heads, head_dim] to the slots [T] int64 (block *
         block_tokens + position in it; negative: nothing) (pw_kv_append)."""
-        T = k.shape[0]
+        T, dev = k.shape[0], self.dev
         _need(k.shape == (T, self.kv_heads, self.head_dim) and v.shape == k.shape, "k and v must be [T, kv_heads, head_dim]")
         ld, ldh, inner = k.stride()
-        _need(k.dtype is self.act and v.dtype is self.act and k.is_cuda and v.is_cuda and v.stride() == (ld, ldh, inner)
-              and inner == 1, "k and v must be of the cache's type, with equal strides and contiguous channels")
-        _packed(slots, (T,), torch.int64, "slots")
-        pw.pw_kv_append(self.desc, k.data_ptr(), v.data_ptr(), ld, ldh, slots.data_ptr(), T, _on(k, stream))
+        _need(k.dtype is self.act and v.dtype is self.act and k.get_device() == dev and v.get_device() == dev
+              and v.stride() == (ld, ldh, inner) and inner == 1,
+              "k and v must be of the cache's type and device, with equal strides and contiguous channels")
+        _packed(slots, (T,), torch.int64, dev, "slots")
+        _call(dev, pw.pw_kv_append, self.desc, k.data_ptr(), v.data_ptr(), ld, ldh, slots.data_ptr(), T, _on(dev, stream))
 
     def attend(self, q: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, max_len: int, scale: float = None,
                window: int = 0, out: torch.Tensor = None, lse: torch.Tensor = None, stream=None) -> torch.Tensor:
@@ -202,21 +222,22 @@ class KVCache:
         first lens[b] cached tokens of the blocks block_table[b] (the last
         ``window`` of them) -> [B, heads, head_dim] (pw_attn_decode)."""
         B, heads, D = q.shape
+        dev = self.dev
         ldq, ldqh, inner = q.stride()
-        _need(q.dtype is self.act and D == self.head_dim and q.is_cuda and inner == 1,
-              "q must be [B, heads, head_dim] of the cache's type")
+        _need(q.dtype is self.act and D == self.head_dim and q.get_device() == dev and inner == 1,
+              "q must be [B, heads, head_dim] of the cache's type and device")
         rows, blocks = block_table.shape
-        _need(block_table.dtype is torch.int32 and rows == B and block_table.is_cuda
-              and (block_table.stride(1) == 1 or blocks <= 1), "block_table must be [B, blocks] int32")
-        _packed(lens, (B,), torch.int32, "lens")
+        _need(block_table.dtype is torch.int32 and rows == B and block_table.get_device() == dev
+              and (block_table.stride(1) == 1 or blocks <= 1), "block_table must be [B, blocks] int32 on the cache's device")
+        _packed(lens, (B,), torch.int32, dev, "lens")
         _need(blocks * self.block_tokens >= max_len, "the block table is shorter than max_len")
         if out is None:
             out = _empty((B, heads, D), self.act, q.device, stream)
-        _packed(out, (B, heads, D), self.act, "out")
-        _packed(lse, (B, heads), torch.float32, "lse")
+        _packed(out, (B, heads, D), self.act, dev, "out")
+        _packed(lse, (B, heads), torch.float32, dev, "lse")
         args = (self.desc, q.data_ptr(), ldq, ldqh, heads, block_table.data_ptr(), block_table.stride(0) if B > 1 else blocks,
                 lens.data_ptr(), B, max_len, D ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse))
-        self._ws.run(_on(q, stream), stream, pw.pw_attn_decode, args,
+        self._ws.run(dev, stream, pw.pw_attn_decode, args,
                      lambda: pw.pw_attn_workspace(self.desc, B, heads, max_len, window))
         return out
 
@@ -235,10 +256,11 @@ def route_grouped(logits: torch.Tensor, K: int, score: str = "softmax", bias: to
     sorted_slot, slot_pos), n_shared shared-expert columns after the K routed
     ones (pw_route_grouped)."""
     T, E = logits.shape
-    _need(logits.dtype in _TYPE and logits.is_cuda and logits.is_contiguous(), "logits must be packed fp32, fp16 or bf16 rows")
+    dev = logits.get_device()
+    _need(logits.dtype in _TYPE and dev >= 0 and logits.is_contiguous(), "logits must be packed fp32, fp16 or bf16 rows")
     _need(score in _SCORE, "score must be softmax or sigmoid")
-    _packed(bias, (E,), torch.float32, "bias")
-    _packed(gate, (T, n_shared), torch.float32, "gate")
+    _packed(bias, (E,), torch.float32, dev, "bias")
+    _packed(gate, (T, n_shared), torch.float32, dev, "gate")
     Kt = K + n_shared
     if out is None:
         with torch.cuda.stream(stream):
@@ -246,12 +268,12 @@ def route_grouped(logits: torch.Tensor, K: int, score: str = "softmax", bias: to
         ids, w, offsets, ss, sp = out
     else:
         ids, w, offsets, ss, sp = out
-        _packed(ids, (T, Kt), torch.int32, "ids")
-        _packed(w, (T, Kt), torch.float32, "w")
+        _packed(ids, (T, Kt), torch.int32, dev, "ids")
+        _packed(w, (T, Kt), torch.float32, dev, "w")
         for t, n in ((offsets, E + n_shared + 1), (ss, T * Kt), (sp, T * Kt)):
-            _need(t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() >= n,
+            _need(t.dtype is torch.int32 and t.get_device() == dev and t.is_contiguous() and t.numel() >= n,
                   "the routing buffers are of another kind (PagedLayer.routing_buffers)")
-    pw.pw_route_grouped(logits.data_ptr(), _TYPE[logits.dtype], _ptr(bias), T, E, K, _SCORE[score], groups, top_groups,
-                        group_top, int(renorm), scale, n_shared, _ptr(gate), ids.data_ptr(), w.data_ptr(),
-                        offsets.data_ptr(), ss.data_ptr(), sp.data_ptr(), _on(logits, stream))
+    _call(dev, pw.pw_route_grouped, logits.data_ptr(), _TYPE[logits.dtype], _ptr(bias), T, E, K, _SCORE[score], groups,
+          top_groups, group_top, int(renorm), scale, n_shared, _ptr(gate), ids.data_ptr(), w.data_ptr(), offsets.data_ptr(),
+          ss.data_ptr(), sp.data_ptr(), _on(dev, stream))
     return ids, w, offsets, ss, sp
