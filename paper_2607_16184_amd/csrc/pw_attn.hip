@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
             if (here) *reinterpret_cast<u32x4*>(dst + (u * (D / 32) + i) * 1024 + 16 * lane) = x[u][i];
           } else {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) *reinterpret_cast<uint32_t*>(row + 64 * i + 4 * w) = x[u][i][w];
+            for (int w = 0; w < 4; ++w) *reinterpret_cast<any_u32*>(row + 64 * i + 4 * w) = x[u][i][w];
           }
         }
       } else {
@@ -193,13 +193,13 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
                   u32x4{q[i][0], q[i][1], q[i + 1][0], q[i + 1][1]};
           } else {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) *reinterpret_cast<uint32_t*>(row + 32 * (i + w / 2) + 4 * (w & 1)) = q[i + w / 2][w & 1];
+            for (int w = 0; w < 4; ++w) *reinterpret_cast<any_u32*>(row + 32 * (i + w / 2) + 4 * (w & 1)) = q[i + w / 2][w & 1];
           }
         }
       }
     }
     if (is_v) {
-      __builtin_amdgcn_wave_barrier();                           // the wave's own LDS: in order
+      wave_exchange();
       // lane: channel c of a tile, places 4 lg .. + 3 of either half
       bool all[2], some[2];
 #pragma unroll
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int tok = 16 * (w / 2) + 4 * lg + 2 * (w & 1) + e;
-              o |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(mine + tok * kPitch + 2 * (16 * j + c))) << (16 * e);
+              o |= static_cast<uint32_t>(*reinterpret_cast<const any_u16*>(mine + tok * kPitch + 2 * (16 * j + c))) << (16 * e);
             }
           } else {
 #pragma unroll
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
           }
         }
       }
-      __builtin_amdgcn_wave_barrier();
+      wave_exchange();
     }
   }
   if (single) {

@@ -98,6 +98,19 @@ __device__ __forceinline__ u32x4 ld16_nt(const uint8_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
 
+// Between writes to LDS by some lanes of a wave and reads of them by others, and
+// before the next writes over what was read. The hardware keeps a wave's LDS
+// accesses in order, the compiler need not: it sees one lane's addresses and types
+// and may take a read for unrelated to a write. (No instruction comes of it.)
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+// Parts of memory that is accessed in other types, too.
+typedef uint32_t __attribute__((may_alias)) any_u32;
+typedef uint16_t __attribute__((may_alias)) any_u16;
+
 // Two values rounded to nearest even, as one 32-bit pair. NaN stays NaN (the
 // hardware's conversions keep it; the bit formula of bf16_rne need not).
 template <int ACT>

@@ -462,12 +462,16 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
     for (int j = 0; j < G::RM; ++j) {
 #pragma unroll
       for (int i = 0; i < G::RN; ++i) put(w + c * kPitch + (i * 16 + 4 * lg) * kE, acc[i][j]);
+      wave_exchange();
+      u32x4 v[16 * kLanes / 64];
+#pragma unroll
+      for (int k = 0; k < 16 * kLanes; k += 64) v[k / 64] = lds16(w + (k + lane) / kLanes * kPitch + 16 * ((k + lane) % kLanes));
+      wave_exchange();
 #pragma unroll
       for (int k = 0; k < 16 * kLanes; k += 64) {
         const int row = (k + lane) / kLanes, p = (k + lane) % kLanes;
-        const u32x4 v = lds16(w + row * kPitch + 16 * p);
         const int m = m0 + (wm * G::RM + j) * 16 + row;
-        if (m < a.M) store_piece<kE>(out, m, n0 + wn * G::RN * 16 + p * (16 / kE), v);
+        if (m < a.M) store_piece<kE>(out, m, n0 + wn * G::RN * 16 + p * (16 / kE), v[k / 64]);
       }
     }
   };

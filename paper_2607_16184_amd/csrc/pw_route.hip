@@ -212,7 +212,7 @@ __device__ __forceinline__ bool choose32(const RouteArgs& a, const Token& tk, in
       g2 = h2;
     } else {
       *reinterpret_cast<f32x4*>(lds + 4 * lane) = f32x4{c[0], c[1], c[2], c[3]};
-      __builtin_amdgcn_wave_barrier();
+      wave_exchange();
       g1 = g2 = -INFINITY;
       if (lane < a.n_groups) {
         for (int i = 0; i < gsize; ++i) {
@@ -285,13 +285,14 @@ __device__ __forceinline__ void choose64(const RouteArgs& a, const Token& tk, in
   for (int q = 0; q < kPerLane; ++q) p[q] = sum > 0.0 ? p[q] / sum : 0.0;
   }
   uint64_t key[kPerLane];
+  wave_exchange();                       // (choose32 read there)
 #pragma unroll
   for (int q = 0; q < kPerLane; ++q) {
     const double c = p[q] + static_cast<double>(tk.b[q]);
     key[q] = tk.x[q] > -INFINITY && c > -__builtin_huge_val() ? order_key(c) : 0ull;
     lds[kPerLane * lane + q] = key[q];
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_exchange();
   if (a.top_groups < a.n_groups) {
     uint64_t gk = 0;
     if (lane < a.n_groups) {

@@ -205,3 +205,21 @@ def test_gemm_sizes_whose_tiles_pass_32_bits(bad):
 
 def test_route_tokens_that_pass_32_bits():
     _refused(pw.PW_EINVAL, _call(pw.pw_route_grouped, ROUTE, ROUTE_OK, K=1, T=(1 << 30) + 1))
+
+
+def test_lds_exchanges_inside_a_wave_are_fenced():
+    """Where lanes of a wave read what others wrote to LDS, without a workgroup
+    barrier, the source asks for the order: the wave barrier alone says nothing of
+    memory, and a test of today's code shows nothing of the next compiler's."""
+    import pathlib
+    import re
+    csrc = pathlib.Path(pw.LIB_PATH).parent / "csrc"
+    text = {p.name: p.read_text() for p in sorted(csrc.glob("*.h*"))}
+    helper = re.search(r"void wave_exchange\(\) \{(.*?)\n\}", text["pw_device.hpp"], re.S).group(1)
+    lines = [x.strip() for x in helper.strip().splitlines()]
+    assert lines == ['__builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");', "__builtin_amdgcn_wave_barrier();",
+                     '__builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");']
+    assert {n: t.count("__builtin_amdgcn_wave_barrier") for n, t in text.items() if "__builtin_amdgcn_wave_barrier" in t} == {"pw_device.hpp": 1}
+    # a turn through LDS: before the reads, and before the next writes
+    assert {n: t.count("wave_exchange();") for n, t in text.items() if "wave_exchange();" in t} == {
+        "pw_attn.hip": 2, "pw_gemm8.hip": 2, "pw_route.hip": 3}
