@@ -423,7 +423,8 @@ __global__ __launch_bounds__(64 * kRouteWaves) void k_route_grouped(RouteArgs a)
 // that its experts' starts are known without a second launch, then places its
 // slots in rounds of 64 per wave: a slot's rank among the wave's slots of its
 // expert comes from comparing the wave's 64 ids one by one, the rounds' and
-// waves' counts give the start. Nothing depends on timing. Against one workgroup
+// waves' counts give the start. Nothing depends on timing. Slot numbers are
+// unsigned where they may pass the last slot, which may be 2^31 - 2. Against one workgroup
 // per expert, each going over all slots (the plain router's permutation): 7.7
 // us in place of 9.2 for 24576 slots of 64 experts, 8.1 for 10.8 at 32768 of 256,
 // equal near 16384, and 1 us slower below. The LDS atomics bound it.
@@ -440,7 +441,7 @@ __device__ __forceinline__ void permute_part(const int32_t* ids, int S, int E, i
   const int tid = threadIdx.x, wave = tid >> 6, lane = lane_id();
   if (tid < 2 * kMaxE) m.count[tid] = 0;
   __syncthreads();
-  const auto add = [&](int s, int id) { atomicAdd(&m.count[id + (s < s0 ? 0 : kMaxE)], 1); };
+  const auto add = [&](uint32_t s, int id) { atomicAdd(&m.count[id + (s < static_cast<uint32_t>(s0) ? 0 : kMaxE)], 1); };
   // four ids to a load, eight loads in flight per thread (the ids come from
   // another kernel, so from beyond the L2: a round of loads is about 1 us)
   const int head = static_cast<int>(-(reinterpret_cast<uintptr_t>(ids) / 4) & 3), n4 = S > head ? (S - head) / 4 : 0;
@@ -451,7 +452,7 @@ __device__ __forceinline__ void permute_part(const int32_t* ids, int S, int E, i
     for (int j = 0; j < 8; ++j) id[j] = base + j * kPermRound < n4 ? v[base + j * kPermRound] : int4{-1, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int s = head + 4 * (base + j * kPermRound);
+      const uint32_t s = head + 4u * (base + j * kPermRound);
       if (id[j].x >= 0) {
         add(s, id[j].x);
         add(s + 1, id[j].y);
@@ -461,8 +462,8 @@ __device__ __forceinline__ void permute_part(const int32_t* ids, int S, int E, i
     }
   }
   if (tid < 8) {                         // what the quads leave at either end
-    const int s = tid < 4 ? tid : head + 4 * n4 + tid - 4;
-    if (tid < 4 ? s < head && s < S : s < S) add(s, ids[s]);
+    const uint32_t s = tid < 4 ? tid : head + 4u * n4 + (tid - 4);
+    if ((tid >= 4 || tid < head) && s < static_cast<uint32_t>(S)) add(s, ids[s]);
   }
   __syncthreads();
   // exclusive sums over the experts
@@ -486,13 +487,13 @@ __device__ __forceinline__ void permute_part(const int32_t* ids, int S, int E, i
       if (tid == E - 1) offsets[E] = sum;
     }
   }
-  for (int base = s0; base < s1; base += kPermRound) {
+  for (uint32_t base = s0; base < static_cast<uint32_t>(s1); base += kPermRound) {
     for (int i = tid; i < kPermWaves * kMaxE; i += kPermRound) m.cnt[i / kMaxE][i % kMaxE] = 0;
     __syncthreads();
-    const int s = base + 64 * wave + lane;
-    const int id = s < s1 ? ids[s] : -1;
+    const uint32_t s = base + 64 * wave + lane;
+    const int id = s < static_cast<uint32_t>(s1) ? ids[s] : -1;
     int rank = 0, n = 0;
-    if (base + 64 * wave < s1) {
+    if (base + 64 * wave < static_cast<uint32_t>(s1)) {
       // (short code: a workgroup runs it a few times, mostly from a cold
       // instruction cache)
 #pragma unroll 8
@@ -517,7 +518,7 @@ __device__ __forceinline__ void permute_part(const int32_t* ids, int S, int E, i
     __syncthreads();
     if (id >= 0) {
       const int pos = m.cnt[wave][id] + rank;
-      sorted_slot[pos] = s;
+      sorted_slot[pos] = static_cast<int32_t>(s);
       slot_pos[s] = pos;
     }
     __syncthreads();
