@@ -535,13 +535,20 @@ __global__ __launch_bounds__(kPermRound) void k_permute_parts(const int32_t* __r
 }
 
 constexpr int64_t kManySlots = 16384;    // where the two permutations take the same time
+constexpr int kLaunchTokens = 1 << 25;   // of one launch, which takes fewer than 2^32 threads
 
 template <int LT>
 hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
   const int64_t S = static_cast<int64_t>(a.T) * (a.K + a.n_shared);
   hipError_t e = hipSuccess;
-  if (a.T > 0) {
-    k_route_grouped<LT><<<static_cast<uint32_t>((a.T + kRouteWaves - 1) / kRouteWaves), 64 * kRouteWaves, 0, st>>>(a);
+  for (int64_t t0 = 0; t0 < a.T; t0 += kLaunchTokens) {
+    RouteArgs p = a;
+    p.T = static_cast<int>(a.T - t0 < kLaunchTokens ? a.T - t0 : kLaunchTokens);
+    p.logits = static_cast<const uint8_t*>(a.logits) + t0 * a.E * (LT == PW_F32 ? 4 : 2);
+    p.ids += t0 * (a.K + a.n_shared);
+    p.w += t0 * (a.K + a.n_shared);
+    if (a.gate) p.gate += t0 * a.n_shared;
+    k_route_grouped<LT><<<static_cast<uint32_t>((p.T + kRouteWaves - 1) / kRouteWaves), 64 * kRouteWaves, 0, st>>>(p);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
