@@ -225,7 +225,6 @@ __global__ __launch_bounds__(64 * kStreamWaves) void k_gemm8_stream(Gemm8Args a)
 template <int RT, int MT, bool WIDE>
 hipError_t launch_stream(const Gemm8Args& a, hipStream_t st) {
   const int64_t grid = static_cast<int64_t>((a.N + 16 * RT - 1) / (16 * RT)) * ((a.M + 16 * MT - 1) / (16 * MT));
-  if (grid > (1 << 22)) return hipErrorInvalidConfiguration;
   k_gemm8_stream<RT, MT, WIDE><<<static_cast<uint32_t>(grid), 64 * kStreamWaves, 0, st>>>(a);
   return hipGetLastError();
 }
@@ -494,7 +493,6 @@ __global__ __launch_bounds__(64 * WN * WM, SLOTS > 2 ? 1 : 2) void k_gemm8_tiled
 template <int TN, int TM, int WN, int WM, int SLOTS, bool WIDE = false>
 hipError_t launch_tiled(const Gemm8Args& a, hipStream_t st) {
   const int64_t grid = static_cast<int64_t>((a.N + TN - 1) / TN) * ((a.M + TM - 1) / TM) * a.ksplit;
-  if (grid >= (1 << 22)) return hipErrorInvalidConfiguration;
   k_gemm8_tiled<TN, TM, WN, WM, SLOTS, WIDE><<<static_cast<uint32_t>(grid), 64 * WN * WM, 0, st>>>(a);
   return hipGetLastError();
 }
@@ -553,6 +551,33 @@ Plan8 plan8(int M, int N, int K, bool widened) {
 }
 int64_t part_ld(int N) { return (static_cast<int64_t>(N) + 3) / 4 * 4; }
 
+// The product in launches that each take fewer than 2^32 threads: tiles of 128 x
+// 128 below 2^22 (the least that the tiled kernels have, with up to 512 threads),
+// weight rows up to 2^24 (32 or more of them to a workgroup of the streaming
+// kernel). Sizes below that, all that are cut in parts of K among them, are one.
+template <class Launch>
+hipError_t in_launches(const Gemm8Args& a, Launch&& launch) {
+  constexpr int64_t kRows = 1 << 24, kTiles = 1 << 22;
+  const int64_t KB = a.K / 128, elt = a.y_type == PW_F32 ? 4 : 2;
+  for (int64_t n0 = 0; n0 < a.N; n0 += kRows) {
+    const int64_t n = a.N - n0 < kRows ? a.N - n0 : kRows;
+    const int64_t most = (kTiles - 1) / ((n + 127) / 128) * 128;   // tokens
+    for (int64_t m0 = 0; m0 < a.M; m0 += most) {
+      Gemm8Args p = a;
+      p.N = static_cast<int>(n);
+      p.M = static_cast<int>(a.M - m0 < most ? a.M - m0 : most);
+      p.a += m0 * a.lda;
+      p.a_scale += m0 * KB;
+      p.w += n0 / 16 * KB * 2048;
+      p.w_scale += n0 / 128 * KB;
+      p.y = static_cast<uint8_t*>(a.y) + (m0 * a.ldy + n0) * elt;
+      const hipError_t e = launch(p);
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
 }  // namespace
 
 // (for any type of y)
@@ -575,14 +600,14 @@ hipError_t launch_gemm8(const Gemm8Args& args, hipStream_t st) {
   a.ksplit = p.ksplit;
   a.kb_per = p.kb_per;
   a.ldp = part_ld(a.N);
-  hipError_t e;
-  switch (p.kernel) {
-    case kStream8:
-      return widened ? launch_stream_of<true>(a, st) : launch_stream_of<false>(a, st);
-    case kSmall8: e = widened ? launch_tiled<128, 128, 2, 4, 4, true>(a, st) : launch_tiled<128, 128, 2, 4, 4>(a, st); break;
-    case kSmallPair8: e = widened ? launch_tiled<128, 128, 2, 2, 2, true>(a, st) : launch_tiled<128, 128, 2, 2, 2>(a, st); break;
-    default: e = launch_tiled<256, 256, 2, 4, 2>(a, st);
-  }
+  const hipError_t e = in_launches(a, [&](const Gemm8Args& g) {
+    switch (p.kernel) {
+      case kStream8: return widened ? launch_stream_of<true>(g, st) : launch_stream_of<false>(g, st);
+      case kSmall8: return widened ? launch_tiled<128, 128, 2, 4, 4, true>(g, st) : launch_tiled<128, 128, 2, 4, 4>(g, st);
+      case kSmallPair8: return widened ? launch_tiled<128, 128, 2, 2, 2, true>(g, st) : launch_tiled<128, 128, 2, 2, 2>(g, st);
+      default: return launch_tiled<256, 256, 2, 4, 2>(g, st);
+    }
+  });
   if (e != hipSuccess || a.ksplit == 1) return e;
   const int64_t blocks = (static_cast<int64_t>(a.M) * (a.ldp / 4) + 255) / 256;
   k_gemm8_join<<<static_cast<uint32_t>(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(a);
