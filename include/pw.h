@@ -558,11 +558,12 @@ enum { PW_F32 = 2 };
  *   z = x + residual (fp32; residual NULL: z = x)
  *   y = z * rsqrt(mean(z^2) + eps) * weight (weight NULL: 1), in fp32
  * and, each where its pointer is not NULL,
- *   sum_out [T,H] act   z, rounded once (may be x's or residual's own buffer)
- *   y16     [T,H] act   y, rounded once (may be x's own buffer)
+ *   sum_out [T,H] act   z, rounded once
+ *   y16     [T,H] act   y, rounded once
  *   y8      [T,H] e4m3  codes of y in groups of 128 columns, with their scales
  *   y8_scale [T,H/128] fp32 (both or neither).
- * The norm is taken of z before it is rounded.
+ * sum_out and y16 may each be x's or residual's own buffer, where that one's rows
+ * are packed; the outputs share none. The norm is taken of z before it is rounded.
  *   act: PW_F16 or PW_BF16 (x, residual, weight, sum_out, y16).
  *   ldx, ldr: row strides of x and residual, at least H and multiples of 8;
  *   the outputs' rows are packed.

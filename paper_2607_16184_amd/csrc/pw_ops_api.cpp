@@ -77,6 +77,12 @@ pw_status pw_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t 
   if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(weight, 16) || !aligned(sum_out, 16) || !aligned(y16, 16) ||
       !aligned(y8, 16) || !aligned(y8_scale, 4))
     return set_error(PW_EINVAL, "buffers must be 16-byte aligned");
+  // an output's packed rows over an input's own: row by row, or the write of one
+  // row meets the read of another
+  const auto over_rows = [&](const void* out) { return out && ((out == x && ldx != H) || (out == residual && ldr != H)); };
+  if (T > 1 && (over_rows(sum_out) || over_rows(y16)))
+    return set_error(PW_EINVAL, "an output over x or residual needs that one's rows packed");
+  if (sum_out && sum_out == y16) return set_error(PW_EINVAL, "sum_out and y16 need buffers of their own");
   const pw::NormArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(residual),
                        static_cast<const uint16_t*>(weight), static_cast<uint16_t*>(sum_out), static_cast<uint16_t*>(y16),
                        static_cast<uint8_t*>(y8), y8_scale, ldx, ldr, T, H, eps, act};

@@ -223,3 +223,14 @@ def test_lds_exchanges_inside_a_wave_are_fenced():
     # a turn through LDS: before the reads, and before the next writes
     assert {n: t.count("wave_exchange();") for n, t in text.items() if "wave_exchange();" in t} == {
         "pw_attn.hip": 2, "pw_gemm8.hip": 2, "pw_route.hip": 3}
+
+
+B = A + (1 << 16)
+
+
+@pytest.mark.parametrize("bad", [dict(x=B, ldx=512, s=B), dict(r=B, ldr=264, s=B), dict(x=B, ldx=264, y=B), dict(r=B, ldr=512, y=B),
+                                 dict(s=B, y=B), dict(s=B, y=B, T=1)])
+def test_norm_refuses_outputs_over_rows_that_are_not_packed(bad):
+    """Output rows are packed: over an input with a longer stride they would be
+    written where other rows are still to be read."""
+    _refused(pw.PW_EINVAL, _call(pw.pw_rms_norm, NORM, dict(NORM_OK, x=A, r=2 * A, w=3 * A, s=4 * A, y=5 * A, q=6 * A, qs=7 * A), **bad))
