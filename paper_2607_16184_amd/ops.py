@@ -210,8 +210,13 @@ class KVCache:
         T, dev = k.shape[0], self.dev
         _need(k.shape == (T, self.kv_heads, self.head_dim) and v.shape == k.shape, "k and v must be [T, kv_heads, head_dim]")
         ld, ldh, inner = k.stride()
+        ldv, ldvh, inner_v = v.stride()
+        if T <= 1:                         # a single row, or head, may have any stride
+            ld = ldv = 0
+        if self.kv_heads == 1:
+            ldh = ldvh = 0
         _need(k.dtype is self.act and v.dtype is self.act and k.get_device() == dev and v.get_device() == dev
-              and v.stride() == (ld, ldh, inner) and inner == 1,
+              and ld == ldv and ldh == ldvh and inner == 1 and inner_v == 1,
               "k and v must be of the cache's type and device, with equal strides and contiguous channels")
         _packed(slots, (T,), torch.int64, dev, "slots")
         _call(dev, pw.pw_kv_append, self.desc, k.data_ptr(), v.data_ptr(), ld, ldh, slots.data_ptr(), T, _on(dev, stream))
@@ -224,6 +229,10 @@ class KVCache:
         B, heads, D = q.shape
         dev = self.dev
         ldq, ldqh, inner = q.stride()
+        if B <= 1:                         # a single sequence, or head, may have any stride
+            ldq = 0
+        if heads == 1:
+            ldqh = 0
         _need(q.dtype is self.act and D == self.head_dim and q.get_device() == dev and inner == 1,
               "q must be [B, heads, head_dim] of the cache's type and device")
         rows, blocks = block_table.shape
