@@ -64,8 +64,8 @@ __device__ __forceinline__ bool slot_ok(const AppendArgs& a, int64_t slot) {
   return slot >= 0 && slot / a.kv.block_tokens < a.kv.n_blocks;
 }
 
-// Few tokens, or none next to each other (a decode step): G lanes per token,
-// head and side.
+// Few tokens, or none next to each other (a decode step), or few heads: G lanes
+// per token, head and side.
 template <int ACT, int BITS>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int G) {
   const int H = a.kv.n_kv_heads;
@@ -84,14 +84,21 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a, int G) {
 // Tokens that follow each other inside a 32-token tile of the cache are a run;
 // the wave of the window that holds its first token writes it as a piece of the
 // tile: keys in the order in which they are loaded, 16 bytes a lane, values
-// turned in LDS. Tokens of runs shorter than kMinRun go one by one. (A value's
-// elements lie 16 bytes apart: written token by token, 4001 tokens of 8 heads
-// x 128 channels take 25.8 us in 16 bits and 18.2 in 8, as runs 8.3 and 10.4.
-// Tokens in no order lose by it, 512 of them 7.0 -> 13.6 us, and from 256 in a row
-// on runs win: the kernel is taken from kAppendMany on, where a step's tokens
-// are hardly those of a decode batch.)
+// turned in LDS. Tokens of runs shorter than kMinRun go one by one.
+// (A value's elements lie 16 bytes apart, so tokens written one by one take long
+// where there are many: 4001 of 8 heads x 128 channels 26.7 us in 16 bits and 18.1
+// in 8, as runs 10.9 and 12.5. A run is a longer chain of loads, turns and stores,
+// so few tokens or heads are done sooner one by one, whatever the channels. Runs /
+// one by one in us, consecutive tokens x heads x channels: 16 bits, 512 x 8 x 128
+// 8.0 / 6.7, 768 x 8 x 128 8.1 / 8.8, 3073 x 2 x 128 7.9 / 8.1, 4096 x 1 x 128 7.5
+// / 5.4, 768 x 8 x 64 5.7 / 5.5, 768 x 8 x 256 13.8 / 13.5; 8 bits, 1536 x 8 x 128
+// 11.6 / 10.0, 2048 12.1 / 11.7, 3073 12.6 / 15.6, 2048 x 8 x 64 7.6 / 7.7, 1024 x
+// 16 x 64 7.7 / 8.0, 2048 x 8 x 256 19.9 / 18.2. Tokens in no order lose by runs,
+// 512 x 8 x 128 in 16 bits 12.1 / 6.7: from kAppendMany on a step's tokens are
+// hardly those of a decode batch.)
 constexpr int kAppendWaves = 4;
 constexpr int kAppendMany = 512;          // tokens
+constexpr int kRunItems16 = 6144, kRunItems8 = 16384;   // tokens x heads
 constexpr int kMinRun = 8;
 template <int ACT, int BITS, int D>
 __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArgs a) {
@@ -891,7 +898,8 @@ hipError_t append_tiles(const AppendArgs& a, hipStream_t st) {
 
 template <int ACT, int BITS>
 hipError_t append(const AppendArgs& a, hipStream_t st) {
-  if (a.T >= kAppendMany) return append_tiles<ACT, BITS>(a, st);
+  const int64_t all = static_cast<int64_t>(a.T) * a.kv.n_kv_heads;
+  if (a.T >= kAppendMany && all >= (BITS == 16 ? kRunItems16 : kRunItems8)) return append_tiles<ACT, BITS>(a, st);
   int G = 8;
   while (8 * G < a.kv.head_dim) G *= 2;
   const int64_t per = 256 / G, items = static_cast<int64_t>(a.T) * a.kv.n_kv_heads * 2;
