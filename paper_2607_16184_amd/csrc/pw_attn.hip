@@ -324,7 +324,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
 // scores, the values' scales the probabilities.
 // Measured: 16 ragged sequences up to 32768 tokens, 8 key heads of 128 in 8 bits
 // (519 MB) 81 us in shares (6.4 TB/s) and 4.2 for their join; 64 up to 4096, 16
-// heads of 64, window 1500 (301 MB) 49.6 (6.1); one of 300 tokens 5.1, a chain of
+// heads of 64, window 1500 (301 MB) 49.8 (6.0); one of 300 tokens 5.1, a chain of
 // table, keys and values.
 
 constexpr int kTile = 32;

@@ -136,8 +136,10 @@ __global__ __launch_bounds__(256) void k_pack8(const uint8_t* __restrict__ w, in
 // Streaming kernel, for few tokens: 16 RT weight rows x 16 MT tokens per
 // workgroup, straight from memory to the matrix instructions. The eight waves
 // split K into eight runs of blocks and join in LDS in a fixed order; a wave has
-// kAhead blocks of weights in flight (2 KB RT each), which is what a kernel
-// bound by HBM needs.
+// kAhead blocks of weights in flight (2 KB RT each). One / two / four ahead, up to 16
+// tokens (us): 16 x 6144 x 4096 7.5 / 8.3 / 8.5, 16 x 28672 x 4096 24.4 / 24.9 / 26.6,
+// 16 x 4096 x 4096 6.8 / 6.4 / 7.0, 4 x 12288 x 2048 7.6 / 7.25 / 10.2, 8 x 4096 x
+// 14336 12.9 / 11.9 / 14.7, 1 x 14336 x 4096 12.3 / 11.3 / 11.4: two lose least.
 constexpr int kStreamWaves = 8;
 
 template <int RT, int MT, bool WIDE>

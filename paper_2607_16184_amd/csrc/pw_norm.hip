@@ -5,10 +5,11 @@
 // neighbouring lanes of 8 values, so its largest magnitude is four lane
 // exchanges inside a row of 16 lanes.
 //
-// Measured: 4095 rows of 4096 with residual, all outputs (151 MB), 23.7 us (6.4
-// TB/s; a large copy reaches 4.9). Four waves per row of 4096 take the same time
-// as the eight used; with cached stores, where eight took 31 us, two took 34 and
-// one 41.
+// Measured: 4095 rows of 4096 with residual, all outputs (151 MB), over eight sets of
+// buffers in turn (1.2 GB) 29.4 us (5.2 TB/s; a large copy reaches 4.9), over two
+// 24.5, as the 256 MB cache before the memory then holds a part of the inputs. Four
+// waves per row of 4096 take the same time as the eight used; with cached stores,
+// where eight took 31 us (two sets), two took 34 and one 41.
 #include "pw_device.hpp"
 #include "pw_ops.hpp"
 
@@ -24,10 +25,12 @@ __device__ __forceinline__ void unpack8(u32x4 v, float* f) {
   }
 }
 
-// 16-bit outputs of this size and more are stored past the caches: 4095 rows of
-// 4096 then take 23.7 us, with cached stores 30.0. 64 rows of 4096 take the same
-// time either way (8.0, most of it the launch) and stay in the caches for the
-// next kernel. 8-bit outputs past the caches gained nothing (24.1).
+// 16-bit outputs of this size and more are stored past the caches. Past them /
+// cached (us, 8 sets of buffers in turn): 2048 rows of 4096 16.8 / 18.9, 4095 29.4 /
+// 32.3, 8192 53 / 58; with a kernel after it that reads both outputs 28.0 / 27.6, 47.7
+// / 47.7, 88.8 / 89.0: the gain is left where what comes next takes the 8-bit rows.
+// Less than that stays in the caches (64 rows 3.4 us either way). 8-bit outputs past
+// the caches gained nothing.
 constexpr int64_t kStreamBytes = 16 << 20;
 
 template <bool STREAM>

@@ -156,8 +156,10 @@ __device__ __forceinline__ uint64_t keep_groups(T gk, int n_groups, int top_grou
 // false) a few that contain them. False where this cannot be told.
 //
 // Error of a score (u = 2^-24; exponentials and reciprocals here are good to
-// two units): sigmoid, below 4 u whatever the logit; softmax, p (1.5 d + 22) u
-// with d = m - x, below 2^-18 p + 2^-56; one more rounding, |c| u, with the bias.
+// two units): sigmoid, below 4 u whatever the logit; softmax, p (2.2 d + 30) u
+// with d = m - x (the exponent's two roundings and its constant's; the sum's
+// terms have d below 6 on the average), below 2^-17 p up to d = 44, where p is
+// below 2^-63 and b0 covers it; one more rounding, |c| u, with the bias.
 // A decision between scores v1 > v2 holds if they differ by more than f (b0 +
 // |v1| + |v2|): sigmoid f = 8 u, b0 = 1; softmax f = 2^-17, b0 = twice the
 // largest bias (p <= |c| + |b|) + 2^-33. Sums of two get twice that, with the
