@@ -688,6 +688,102 @@ pw_status pw_attn_decode(const pw_kv_cache* cache, const void* q, int64_t ldq, i
                          int max_len, float scale, int window, void* out, float* lse, void* ws,
                          size_t ws_bytes, void* stream);
 
+/* Position rotation: of each head the first `dims` channels turn in pairs, pair i
+ * by the angle position * inv_freq[i] (radians; both and their product in 64 bits,
+ * reduced to a part of a turn before they leave them), times the amplitude:
+ *   (x, y) -> amplitude (x cos - y sin, x sin + y cos).
+ * Channels past `dims` stay. A NULL rotation, or one of 0 channels, turns none.
+ * Constraints (PW_EINVAL otherwise): dims >= 0, a multiple of 16, at most the head's
+ * channels; amplitude finite; inv_freq 8-byte aligned.                        */
+typedef struct {
+    const double* inv_freq;  /* device, [dims / 2]                              */
+    int dims;
+    int interleaved;         /* pairs (2 i, 2 i + 1); 0: (i, i + dims / 2)      */
+    float amplitude;
+} pw_rotation;
+
+/* Norm and rotation of query and key heads. Per token t and head, x its head_dim
+ * channels:
+ *   y = x * rsqrt(mean(x^2) + eps) * weight (weight NULL: 1), in fp32; y = x where
+ *   norm is 0;
+ *   the rotation of y by position positions[t] + offset, in fp32, rounded once.
+ *   q [T, n_q], k [T, n_k]: act, element (t, h, d) at t * ldq + h * ldqh + d; either
+ *   may have no heads. q_weight, k_weight [head_dim] act. The outputs have strides
+ *   of their own, heads apart from each other; an output may be its input's own
+ *   buffer, with that one's strides, and shares no memory with anything else.
+ *   positions [T] int32 device, of any sign (not read without a rotation).
+ * Constraints: head_dim a multiple of 16, 16 to 256; act PW_F16 or PW_BF16; eps >= 0
+ * and finite; strides multiples of 8; heads and weights 16-byte aligned (PW_EINVAL
+ * otherwise); T < 2^25, T * (n_q + n_k) < 2^30 (PW_EUNSUPPORTED). T = 0 does
+ * nothing.                                                                   */
+pw_status pw_heads_norm_rotate(const pw_rotation* rot, const int32_t* positions, int offset, const void* q, int64_t ldq,
+                               int64_t ldqh, int n_q, const void* k, int64_t ldk, int64_t ldkh, int n_k,
+                               const void* q_weight, const void* k_weight, int norm, float eps, int T, int head_dim,
+                               int act, void* q_out, int64_t ldqo, int64_t ldqoh, void* k_out, int64_t ldko,
+                               int64_t ldkoh, void* stream);
+
+/* The same of a step's queries and keys, the keys and values written into the cache
+ * on the way: q to q_out as above; k's normed and turned values to the slots, rounded
+ * once to act, or to 8-bit codes of the fp32 values; v to the slots as pw_kv_append
+ * writes it. Queries of tokens whose slot writes nothing are computed all the same.
+ *   k and v [T, cache heads], strides ld and ldh, and slots as in pw_kv_append; n_q
+ *   may be 0.
+ * Constraints: those of pw_kv_append and pw_heads_norm_rotate; T * (n_q + 2
+ * n_kv_heads) < 2^30 (PW_EUNSUPPORTED).                                      */
+pw_status pw_kv_append_rotated(const pw_kv_cache* cache, const pw_rotation* rot, const int32_t* positions, int offset,
+                               const void* q, int64_t ldq, int64_t ldqh, int n_q, const void* k, const void* v,
+                               int64_t ld, int64_t ldh, const void* q_weight, const void* k_weight, int norm, float eps,
+                               const int64_t* slots, int T, void* q_out, int64_t ldqo, int64_t ldqoh, void* stream);
+
+/* Attention of several new tokens per sequence over the cache (their own keys and
+ * values are appended first): prompt chunks, and trees of drafted tokens. Rows
+ * starts[b] .. starts[b+1] - 1 of q belong to sequence b; with n of them its context
+ * is its first len - n positions, len = seq_lens[b], and row i's own token lies at
+ * position len - n + i.
+ *   masks NULL: row i sees the positions up to its own; window > 0: the last
+ *   `window` of them.
+ *   masks [T][words] 64-bit words, packed: row r sees the context, and of its
+ *   sequence's new tokens those j whose bit j mod 64 of word j / 64 of its mask is
+ *   set (its own only if that bit is; bits from n on are not looked at, tokens
+ *   past the words are not seen); window > 0: of the context the last window - m
+ *   positions, m the bits set.
+ *   q, out and lse [T, n_q_heads]; q's strides, scale, head sharing, block_table,
+ *   max_len and lse otherwise as in pw_attn_decode; positions from max_len on, or
+ *   below 0, do not exist.
+ * starts [B+1] int32 device, not decreasing, within 0 .. T: rows that no sequence
+ * has are not written. Rows that see nothing give zeros and an lse of -infinity.
+ * What lies in the cache at positions that a row does not see is not used for it,
+ * NaN and infinities included. Scores, exponentials and sums are in fp32; weights
+ * enter the product with the values as in pw_attn_decode.
+ * Constraints: B, T >= 0; n_q_heads a multiple of n_kv_heads; 1 <= words <= 1024;
+ * 0 <= max_len < 2^31 - 256; window >= 0; scale finite (PW_EINVAL otherwise); B <
+ * 65536, T * n_q_heads < 2^23, min(B, T) * n_kv_heads < 2^21 (PW_EUNSUPPORTED: split
+ * the batch).
+ * ws: device workspace of at least pw_attn_rows_workspace bytes, 16-byte aligned
+ * (PW_ENOMEM below; may be NULL where that is 0), in use until `stream` passes the
+ * call. Deterministic.                                                       */
+pw_status pw_attn_rows_workspace(const pw_kv_cache* cache, int B, int T, int n_q_heads, int max_len, int window,
+                                 size_t* ws_bytes);
+pw_status pw_attn_rows(const pw_kv_cache* cache, const void* q, int64_t ldq, int64_t ldqh, int n_q_heads,
+                       const int32_t* starts, int T, const int64_t* masks, int words, const int32_t* block_table,
+                       int64_t ld_table, const int32_t* seq_lens, int B, int max_len, float scale, int window, void* out,
+                       float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Keep the accepted ones of each sequence's new tokens: with n = starts[b+1] -
+ * starts[b] new tokens after a context of seq_lens[b] - n positions, those whose bit
+ * is set in chosen [B][words] (as a row of masks above: the mask of the last token
+ * of an accepted path is the path) move, in their order, to the positions after the
+ * context; new_lens[b] = the context + their count. Keys, values and scales are
+ * moved as they are stored. A token whose old or new position lies in no block of
+ * the pool, or from max_len on, is counted and not moved; tokens below position 0 do
+ * not exist. Slots of other positions are not touched.
+ * Constraints: B >= 0, 0 <= max_len < 2^31 - 256, ld_table * block_tokens >= max_len,
+ * 1 <= words <= 1024, new_lens [B] not seq_lens' own buffer (PW_EINVAL otherwise); B <
+ * 65536 (PW_EUNSUPPORTED). Two sequences that share a block of new tokens: undefined. */
+pw_status pw_kv_keep(const pw_kv_cache* cache, const int32_t* starts, const int32_t* block_table, int64_t ld_table,
+                     const int32_t* seq_lens, int B, int max_len, const int64_t* chosen, int words, int32_t* new_lens,
+                     void* stream);
+
 /* Group-limited routing and token permutation. For each token, with p_e =
  * sigmoid(l_e) or softmax(l)_e of its logits and c_e = p_e + bias_e (bias NULL:
  * 0), both held in 64 bits:

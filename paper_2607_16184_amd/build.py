@@ -45,6 +45,8 @@ SOURCES = {
     "pw_norm.hip": [],
     "pw_gemm8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "pw_attn.hip": [],
+    "pw_heads.hip": [],
+    "pw_rows.hip": [],
     "pw_route.hip": [],
     "pw_api.cpp": [],
     "pw_ops_api.cpp": [],

@@ -1,12 +1,9 @@
 // Paged KV cache, gfx950: writing new tokens into it (k_kv_append) and the
 // attention of one new token per sequence over it (k_attn, k_attn_join).
-#include "pw_device.hpp"
-#include "pw_ops.hpp"
+#include "pw_kv.hpp"
 
 namespace pw {
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // ---------------------------------------------------------------------------
 // Append
@@ -20,49 +17,15 @@ __device__ __forceinline__ u32x4 load_one(const AppendArgs& a, int64_t tok, int 
 }
 template <int ACT, int BITS>
 __device__ __forceinline__ void append_one(const AppendArgs& a, u32x4 raw, int64_t slot, int h, int is_v, int c, int G) {
-  const int D = a.kv.head_dim, P = a.kv.block_tokens, H = a.kv.n_kv_heads;
-  const int t = static_cast<int>(slot % P);
-  uint8_t* blk = a.kv.pool + slot / P * a.kv.block_stride;
-  uint8_t* dst = blk + static_cast<size_t>(2 * h + is_v) * P * D * (BITS / 8);
   if constexpr (BITS == 16) {
-    if (8 * c >= D) return;
-    if (!is_v) {
-      *reinterpret_cast<u32x4*>(dst + ((t / 16) * (D / 32) + c / 4) * 1024 + 16 * (16 * (c & 3) + t % 16)) = raw;
-    } else {
-      uint16_t* p = reinterpret_cast<uint16_t*>(dst + ((t / 32) * (D / 16) + c / 2) * 1024) +
-                    8 * (16 * (t / 4 % 4) + 8 * (c & 1)) + 4 * (t / 16 % 2) + t % 4;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[8 * j] = static_cast<uint16_t>(raw[j / 2] >> (16 * (j & 1)));
-    }
+    put16(a.kv, raw, slot, h, is_v, c);
   } else {
-    float f[8], m = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      f[j] = val16(raw[j / 2] >> (16 * (j & 1)), ACT);
-      m = fmaxf(m, fabsf(f[j]));
-    }
-    for (int o = G / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    const float s = f8_scale(m);
-    if (8 * c >= D) return;
-    const u32x2 q = f8_codes8(f, s);
-    if (!is_v) {
-      *reinterpret_cast<u32x2*>(dst + ((t / 16) * (D / 64) + c / 8) * 1024 + 16 * (16 * (c & 3) + t % 16) +
-                                8 * (c / 4 % 2)) = q;
-    } else {
-      uint8_t* p = dst + ((t / 32) * (D / 32) + c / 4) * 1024 + 16 * (16 * (t / 4 % 4) + 8 * (c & 1)) +
-                   8 * (c / 2 % 2) + 4 * (t / 16 % 2) + t % 4;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[16 * j] = static_cast<uint8_t>(q[j / 4] >> (8 * (j & 3)));
-    }
-    if (c == 0) {
-      float* sc = reinterpret_cast<float*>(blk + static_cast<size_t>(2) * H * P * D);
-      sc[(is_v * H + h) * P + t] = s;
-    }
+    float f[8];
+    unpack8<ACT>(raw, f);
+    put8(a.kv, f, slot, h, is_v, c, G);
   }
 }
-__device__ __forceinline__ bool slot_ok(const AppendArgs& a, int64_t slot) {
-  return slot >= 0 && slot / a.kv.block_tokens < a.kv.n_blocks;
-}
+__device__ __forceinline__ bool slot_ok(const AppendArgs& a, int64_t slot) { return slot_ok(a.kv, slot); }
 
 // Few tokens, or none next to each other (a decode step), or few heads: G lanes
 // per token, head and side.
@@ -327,12 +290,8 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
 // heads of 64, window 1500 (301 MB) 49.8 (6.0); one of 300 tokens 5.1, a chain of
 // table, keys and values.
 
-constexpr int kTile = 32;
 constexpr int kAttnWaves = 4, kManyWaves = 8;
 constexpr int kFewBytes = 256;        // of a token's key, for the second
-constexpr float kNoMax = -3.402823466e38f;   // no finite score is below it, and exp2(-inf - it) = 0
-constexpr float kSlack = 8.0f;
-constexpr float kLift = 32768.0f, kLow = 4096.0f;   // factors of fp16 probabilities and of their second term
 
 // Attended positions [lo, hi) of a sequence of n cached tokens, and their tiles.
 struct Span {
@@ -379,29 +338,6 @@ __device__ __forceinline__ void tiles_before(const AttnArgs& a, int b, int lane,
 __device__ __forceinline__ int share_of(const AttnArgs& a, int tiles, int items_per_seq) {
   const int total = tiles * items_per_seq, r = (total + a.n_shares - 1) / a.n_shares;
   return (r + kAttnWaves - 1) / kAttnWaves * kAttnWaves;
-}
-
-// Two e4m3 codes (the low or high half of a word) as two 16-bit values.
-template <int ACT, bool HI>
-__device__ __forceinline__ uint32_t widen2(uint32_t c) {
-  if constexpr (ACT == PW_BF16)
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, HI));
-  else
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, 1.0f, HI));
-}
-template <int ACT>
-__device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi) {
-  return u32x4{widen2<ACT, false>(lo), widen2<ACT, true>(lo), widen2<ACT, false>(hi), widen2<ACT, true>(hi)};
-}
-
-// Largest value of a column (lanes l, l + 16, l + 32, l + 48), in each of its
-// lanes. (Rows 0 and 1, 2 and 3 trade places, then the halves.)
-__device__ __forceinline__ float column_max(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const uint32_t t = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
-  const auto b = __builtin_amdgcn_permlane32_swap(t, t, false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // Block number of a tile of sequence b (counted from position 0); -1 past max_len.

@@ -54,6 +54,72 @@ struct AppendArgs {
   int T;
 };
 
+struct Rotate {
+  const double* inv_freq;  // [R / 2], radians a position
+  const int32_t* positions;
+  int64_t offset;          // added to each
+  int R, interleaved;
+  float amplitude;
+};
+
+struct HeadsArgs {
+  Rotate rot;
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;       // strides as k; with a cache
+  const uint16_t* q_weight;
+  const uint16_t* k_weight;
+  uint16_t* q_out;
+  uint16_t* k_out;         // without one
+  int64_t ldq, ldqh, ldk, ldkh, ldqo, ldqoh, ldko, ldkoh;
+  int n_q, n_k, T, D, act, norm;
+  float eps;
+  KvArgs kv;
+  const int64_t* slots;    // nullptr: no cache
+};
+
+struct KeepArgs {
+  KvArgs kv;
+  const int32_t* starts;
+  const int32_t* table;
+  int64_t ld_table;
+  const int32_t* lens;
+  const int64_t* chosen;   // [B][words]
+  int32_t* new_lens;
+  int B, max_len, words;
+};
+
+// Attention of several rows per sequence. An item is a sequence, a key head and a
+// group of col_tiles x 16 columns: column c of a sequence is query head c mod g of
+// the key head's g, of row c / g.
+struct RowsArgs {
+  KvArgs kv;
+  const uint16_t* q;
+  int64_t ldq, ldqh;
+  int n_q_heads;
+  const int32_t* starts;
+  const int32_t* table;
+  int64_t ld_table;
+  const int32_t* lens;
+  const int64_t* masks;    // [T][words], nullptr: causal
+  int words;
+  int B, T, max_len, window;
+  float scale;
+  uint16_t* out;
+  float* lse;
+  int n_splits, split_tiles;
+  float* part_o;           // [items][splits][columns][D], not normalised
+  float* part_ml;          // [the same][2]: maximum (base 2), sum
+};
+
+struct RowsPlan {
+  int col_tiles;           // of a wave
+  int n_splits, split_tiles;
+  int64_t items;           // at most
+  size_t slots;            // rows of head_dim + 2 floats of the workspace
+};
+RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int bits, int max_len, int window);
+
 // A sequence's attended positions are cut into tiles of 32 tokens, at multiples
 // of 32.
 struct AttnArgs {
@@ -102,6 +168,9 @@ hipError_t launch_pack8(const uint8_t* w, int64_t ldw, int N, int K, uint8_t* pa
 hipError_t launch_gemm8(const Gemm8Args& a, hipStream_t st);
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st);
 hipError_t launch_attn(const AttnArgs& a, hipStream_t st);
+hipError_t launch_heads(const HeadsArgs& a, hipStream_t st);
+hipError_t launch_kv_keep(const KeepArgs& a, hipStream_t st);
+hipError_t launch_attn_rows(const RowsArgs& a, const RowsPlan& p, hipStream_t st);
 hipError_t launch_route_grouped(const RouteArgs& a, hipStream_t st);
 
 }  // namespace pw

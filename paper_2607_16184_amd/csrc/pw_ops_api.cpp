@@ -58,6 +58,40 @@ const char* attn_fault(const pw_kv_cache* c, int B, int n_q_heads, int max_len, 
 }
 bool attn_too_wide(int B, int n_q_heads) { return B > 65535 || n_q_heads > 65535 || static_cast<int64_t>(B) * n_q_heads >= (int64_t(1) << 23); }
 
+// What is wrong with a rotation or the heads that it goes over, or nullptr.
+const char* heads_fault(const pw_rotation* r, int head_dim, int T, int n_q, int n_k, int norm, float eps) {
+  if (T < 0 || n_q < 0 || n_k < 0) return "need T, n_q and n_k >= 0";
+  if (r && (r->dims < 0 || r->dims % 16 != 0 || r->dims > head_dim)) return "rotated channels must be a multiple of 16, at most head_dim";
+  if (r && !std::isfinite(r->amplitude)) return "the amplitude must be finite";
+  if (norm && (!(eps >= 0.0f) || std::isinf(eps))) return "eps must be finite and not negative";
+  return nullptr;
+}
+constexpr const char* kTooManyHeads = "T must stay below 2^25, T times the heads below 2^30: split the batch";
+bool heads_too_many(int T, int n_q, int n_k) {
+  return T >= (1 << 25) || static_cast<int64_t>(T) * (static_cast<int64_t>(n_q) + n_k) >= (int64_t(1) << 30);
+}
+pw::Rotate rotate_args(const pw_rotation* r, const int32_t* positions, int offset) {
+  if (!r || r->dims == 0) return {nullptr, nullptr, 0, 0, 0, 1.0f};
+  return {r->inv_freq, positions, offset, r->dims, r->interleaved != 0, r->amplitude};
+}
+// Whether the heads of an output [T, n] of strides ld, ldh are apart, rows or heads
+// outermost.
+bool apart(int64_t T, int64_t n, int64_t D, int64_t ld, int64_t ldh) {
+  if (T == 1) return n == 1 || ldh >= D;
+  if (n == 1) return ld >= D;
+  if (ld > (int64_t(1) << 40) || ldh > (int64_t(1) << 40)) return false;
+  return (ldh >= D && ld >= (n - 1) * ldh + D) || (ld >= D && ldh >= (T - 1) * ld + D);
+}
+bool same_rows(int T, int n, int64_t ld, int64_t ldh, int64_t ld2, int64_t ldh2) {
+  return (T == 1 || ld == ld2) && (n == 1 || ldh == ldh2);
+}
+constexpr int kMostWords = 1024;
+constexpr const char* kTooManyRows = "B must stay below 65536, T * n_q_heads and the groups of columns below 2^23: split the batch";
+bool rows_too_many(const pw_kv_cache* c, int B, int T, int n_q_heads) {
+  return B > 65535 || static_cast<int64_t>(T) * n_q_heads >= (int64_t(1) << 23) ||
+         static_cast<int64_t>(B < T ? B : T) * c->n_kv_heads >= (int64_t(1) << 21);
+}
+
 }  // namespace
 
 extern "C" {
@@ -204,6 +238,180 @@ pw_status pw_attn_decode(const pw_kv_cache* c, const void* q, int64_t ldq, int64
   a.part_o = static_cast<float*>(ws);
   a.part_ml = a.part_o + p.ws_bytes / sizeof(float) / (c->head_dim + 2) * c->head_dim;
   return launched(pw::launch_attn(a, static_cast<hipStream_t>(stream)), "attention launch");
+}
+
+pw_status pw_heads_norm_rotate(const pw_rotation* rot, const int32_t* positions, int offset, const void* q, int64_t ldq,
+                               int64_t ldqh, int n_q, const void* k, int64_t ldk, int64_t ldkh, int n_k,
+                               const void* q_weight, const void* k_weight, int norm, float eps, int T, int head_dim, int act,
+                               void* q_out, int64_t ldqo, int64_t ldqoh, void* k_out, int64_t ldko, int64_t ldkoh,
+                               void* stream) {
+  if (head_dim < 16 || head_dim > 256 || head_dim % 16 != 0)
+    return set_error(PW_EINVAL, "head_dim must be a multiple of 16, 16 to 256");
+  if (!act_ok(act)) return set_error(PW_EINVAL, "act must be PW_F16 or PW_BF16");
+  if (const char* f = heads_fault(rot, head_dim, T, n_q, n_k, norm, eps)) return set_error(PW_EINVAL, f);
+  if (heads_too_many(T, n_q, n_k)) return set_error(PW_EUNSUPPORTED, kTooManyHeads);
+  if (ldq % 8 != 0 || ldqh % 8 != 0 || ldk % 8 != 0 || ldkh % 8 != 0 || ldqo % 8 != 0 || ldqoh % 8 != 0 || ldko % 8 != 0 ||
+      ldkoh % 8 != 0)
+    return set_error(PW_EINVAL, "strides must be multiples of 8");
+  if (T == 0 || n_q + n_k == 0) return PW_OK;
+  if ((n_q && (!q || !q_out)) || (n_k && (!k || !k_out)) || (rot && rot->dims && (!rot->inv_freq || !positions)))
+    return set_error(PW_EINVAL, "null argument");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_weight, 16) || !aligned(k_weight, 16) || !aligned(q_out, 16) ||
+      !aligned(k_out, 16) || !aligned(positions, 4) || (rot && !aligned(rot->inv_freq, 8)))
+    return set_error(PW_EINVAL, "heads and weights must be 16-byte aligned, frequencies 8-byte, positions 4-byte");
+  if ((n_q && !apart(T, n_q, head_dim, ldqo, ldqoh)) || (n_k && !apart(T, n_k, head_dim, ldko, ldkoh)))
+    return set_error(PW_EINVAL, "heads of an output lie over each other");
+  if ((n_q && q_out == q && !same_rows(T, n_q, ldq, ldqh, ldqo, ldqoh)) ||
+      (n_k && k_out == k && !same_rows(T, n_k, ldk, ldkh, ldko, ldkoh)))
+    return set_error(PW_EINVAL, "an output over its input needs that one's strides");
+  if (n_q && n_k && (q_out == k || k_out == q || q_out == k_out))
+    return set_error(PW_EINVAL, "queries and keys need output buffers of their own");
+  pw::HeadsArgs a{};
+  a.rot = rotate_args(rot, positions, offset);
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.q_weight = static_cast<const uint16_t*>(norm ? q_weight : nullptr);
+  a.k_weight = static_cast<const uint16_t*>(norm ? k_weight : nullptr);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.ldq = ldq;
+  a.ldqh = ldqh;
+  a.ldk = ldk;
+  a.ldkh = ldkh;
+  a.ldqo = ldqo;
+  a.ldqoh = ldqoh;
+  a.ldko = ldko;
+  a.ldkoh = ldkoh;
+  a.n_q = n_q;
+  a.n_k = n_k;
+  a.T = T;
+  a.D = head_dim;
+  a.act = act;
+  a.norm = norm;
+  a.eps = eps;
+  return launched(pw::launch_heads(a, static_cast<hipStream_t>(stream)), "head norm launch");
+}
+
+pw_status pw_kv_append_rotated(const pw_kv_cache* c, const pw_rotation* rot, const int32_t* positions, int offset,
+                               const void* q, int64_t ldq, int64_t ldqh, int n_q, const void* k, const void* v, int64_t ld,
+                               int64_t ldh, const void* q_weight, const void* k_weight, int norm, float eps,
+                               const int64_t* slots, int T, void* q_out, int64_t ldqo, int64_t ldqoh, void* stream) {
+  if (const char* f = kv_fault(c)) return set_error(PW_EINVAL, f);
+  if (const char* f = kv_memory_fault(c)) return set_error(PW_EINVAL, f);
+  if (const char* f = heads_fault(rot, c->head_dim, T, n_q, c->n_kv_heads, norm, eps)) return set_error(PW_EINVAL, f);
+  if (heads_too_many(T, n_q, 2 * c->n_kv_heads)) return set_error(PW_EUNSUPPORTED, kTooManyHeads);
+  if (ldq % 8 != 0 || ldqh % 8 != 0 || ld % 8 != 0 || ldh % 8 != 0 || ldqo % 8 != 0 || ldqoh % 8 != 0)
+    return set_error(PW_EINVAL, "strides must be multiples of 8");
+  if (T == 0) return PW_OK;
+  if (!k || !v || !slots || (n_q && (!q || !q_out)) || (rot && rot->dims && (!rot->inv_freq || !positions)))
+    return set_error(PW_EINVAL, "null argument");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_weight, 16) || !aligned(k_weight, 16) ||
+      !aligned(q_out, 16) || !aligned(positions, 4) || !aligned(slots, 8) || (rot && !aligned(rot->inv_freq, 8)))
+    return set_error(PW_EINVAL, "heads and weights must be 16-byte aligned, frequencies and slots 8-byte, positions 4-byte");
+  if (n_q && !apart(T, n_q, c->head_dim, ldqo, ldqoh)) return set_error(PW_EINVAL, "heads of an output lie over each other");
+  if (n_q && q_out == q && !same_rows(T, n_q, ldq, ldqh, ldqo, ldqoh))
+    return set_error(PW_EINVAL, "an output over its input needs that one's strides");
+  if (n_q && (q_out == k || q_out == v)) return set_error(PW_EINVAL, "queries need an output buffer of their own");
+  pw::HeadsArgs a{};
+  a.rot = rotate_args(rot, positions, offset);
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.q_weight = static_cast<const uint16_t*>(norm ? q_weight : nullptr);
+  a.k_weight = static_cast<const uint16_t*>(norm ? k_weight : nullptr);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.ldq = ldq;
+  a.ldqh = ldqh;
+  a.ldk = ld;
+  a.ldkh = ldh;
+  a.ldqo = ldqo;
+  a.ldqoh = ldqoh;
+  a.n_q = n_q;
+  a.n_k = c->n_kv_heads;
+  a.T = T;
+  a.D = c->head_dim;
+  a.act = c->act;
+  a.norm = norm;
+  a.eps = eps;
+  a.kv = kv_args(c);
+  a.slots = slots;
+  return launched(pw::launch_heads(a, static_cast<hipStream_t>(stream)), "rotated append launch");
+}
+
+pw_status pw_kv_keep(const pw_kv_cache* c, const int32_t* starts, const int32_t* block_table, int64_t ld_table,
+                     const int32_t* seq_lens, int B, int max_len, const int64_t* chosen, int words, int32_t* new_lens,
+                     void* stream) {
+  if (const char* f = kv_fault(c)) return set_error(PW_EINVAL, f);
+  if (const char* f = kv_memory_fault(c)) return set_error(PW_EINVAL, f);
+  if (B < 0 || max_len < 0 || max_len > INT32_MAX - 256) return set_error(PW_EINVAL, "need B >= 0 and 0 <= max_len < 2^31 - 256");
+  if (words < 1 || words > kMostWords) return set_error(PW_EINVAL, "need 1 <= words <= 1024");
+  if (B > 65535) return set_error(PW_EUNSUPPORTED, "B must stay below 65536");
+  const int64_t blocks = (static_cast<int64_t>(max_len) + c->block_tokens - 1) / c->block_tokens;
+  if (ld_table < blocks) return set_error(PW_EINVAL, "the block table's rows are shorter than max_len");
+  if (B == 0) return PW_OK;
+  if (!starts || !seq_lens || !chosen || !new_lens || (max_len > 0 && !block_table)) return set_error(PW_EINVAL, "null argument");
+  if (!aligned(starts, 4) || !aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(new_lens, 4) || !aligned(chosen, 8))
+    return set_error(PW_EINVAL, "buffers must be aligned to their elements");
+  if (new_lens == seq_lens) return set_error(PW_EINVAL, "new_lens needs a buffer of its own");
+  const pw::KeepArgs a{kv_args(c), starts, block_table, ld_table, seq_lens, chosen, new_lens, B, max_len, words};
+  return launched(pw::launch_kv_keep(a, static_cast<hipStream_t>(stream)), "keep launch");
+}
+
+pw_status pw_attn_rows_workspace(const pw_kv_cache* c, int B, int T, int n_q_heads, int max_len, int window, size_t* ws_bytes) {
+  if (const char* f = attn_fault(c, B, n_q_heads, max_len, window)) return set_error(PW_EINVAL, f);
+  if (T < 0) return set_error(PW_EINVAL, "need T >= 0");
+  if (!ws_bytes) return set_error(PW_EINVAL, "null argument");
+  if (rows_too_many(c, B, T, n_q_heads)) return set_error(PW_EUNSUPPORTED, kTooManyRows);
+  *ws_bytes = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window).slots * (c->head_dim + 2) * 4;
+  return PW_OK;
+}
+
+pw_status pw_attn_rows(const pw_kv_cache* c, const void* q, int64_t ldq, int64_t ldqh, int n_q_heads, const int32_t* starts,
+                       int T, const int64_t* masks, int words, const int32_t* block_table, int64_t ld_table,
+                       const int32_t* seq_lens, int B, int max_len, float scale, int window, void* out, float* lse, void* ws,
+                       size_t ws_bytes, void* stream) {
+  if (const char* f = attn_fault(c, B, n_q_heads, max_len, window)) return set_error(PW_EINVAL, f);
+  if (const char* f = kv_memory_fault(c)) return set_error(PW_EINVAL, f);
+  if (T < 0) return set_error(PW_EINVAL, "need T >= 0");
+  if (masks && (words < 1 || words > kMostWords)) return set_error(PW_EINVAL, "need 1 <= words <= 1024");
+  if (rows_too_many(c, B, T, n_q_heads)) return set_error(PW_EUNSUPPORTED, kTooManyRows);
+  if (ldq % 8 != 0 || ldqh % 8 != 0) return set_error(PW_EINVAL, "strides must be multiples of 8");
+  if (!std::isfinite(scale)) return set_error(PW_EINVAL, "scale must be finite");
+  const int64_t blocks = (static_cast<int64_t>(max_len) + c->block_tokens - 1) / c->block_tokens;
+  if (ld_table < blocks) return set_error(PW_EINVAL, "the block table's rows are shorter than max_len");
+  if (B == 0 || T == 0) return PW_OK;
+  if (!q || !starts || !seq_lens || !out || (max_len > 0 && !block_table)) return set_error(PW_EINVAL, "null argument");
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(masks, 8) || !aligned(starts, 4) || !aligned(block_table, 4) ||
+      !aligned(seq_lens, 4) || !aligned(lse, 4))
+    return set_error(PW_EINVAL, "q and out must be 16-byte aligned, masks 8-byte, the other buffers 4-byte");
+  const pw::RowsPlan p = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window);
+  const size_t need = p.slots * (c->head_dim + 2) * sizeof(float);
+  if (need && (!ws || ws_bytes < need)) return set_error(PW_ENOMEM, "workspace too small (pw_attn_rows_workspace)");
+  if (need && !aligned(ws, 16)) return set_error(PW_EINVAL, "the workspace must be 16-byte aligned");
+  pw::RowsArgs a{};
+  a.kv = kv_args(c);
+  a.q = static_cast<const uint16_t*>(q);
+  a.ldq = ldq;
+  a.ldqh = ldqh;
+  a.n_q_heads = n_q_heads;
+  a.starts = starts;
+  a.table = block_table;
+  a.ld_table = ld_table;
+  a.lens = seq_lens;
+  a.masks = masks;
+  a.words = masks ? words : 0;
+  a.B = B;
+  a.T = T;
+  a.max_len = max_len;
+  a.window = window;
+  a.scale = scale;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.n_splits = p.n_splits;
+  a.split_tiles = p.split_tiles;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = a.part_o + p.slots * c->head_dim;
+  return launched(pw::launch_attn_rows(a, p, static_cast<hipStream_t>(stream)), "attention launch");
 }
 
 pw_status pw_route_grouped(const void* logits, int logit_type, const float* bias, int T, int E, int K, int score,

@@ -1,0 +1,613 @@
+// Attention of several new tokens per sequence over the paged KV cache, gfx950:
+// trees of drafted tokens and prompt chunks (k_attn_rows, k_rows_join).
+#include "pw_kv.hpp"
+
+namespace pw {
+namespace {
+
+// Rows and query heads of a key head are the columns of the products that one
+// token's attention (pw_attn.hip) has its query heads for: scores S[token, column]
+// = K q^T, outputs O[channel, column] += V^T P^T, a lane holding tokens 4 g .. 4 g
+// + 3 of either half of a 32-token tile for column lane mod 16. What a column sees
+// of a tile is 32 bits: a range of positions, and for trees the row's mask shifted
+// to the tile. Tiles that all columns see whole are taken without them.
+
+constexpr int kRowsWaves = 4;
+
+struct Item {
+  int b, h;
+  int row0, n;             // first row of the sequence, its rows
+  int col0, n_col;         // first column of the group, columns
+  int ctx;                 // positions before the rows' own
+  int lo, hi;              // positions that some column sees lie in [lo, hi)
+  int t0, tiles;
+};
+
+__device__ __forceinline__ int clamp64(int64_t v, int lo, int hi) {
+  return static_cast<int>(v < lo ? lo : v > hi ? hi : v);
+}
+
+// The item's sequence, columns and span; false past the last one. (Starts that are
+// not in order give other items, never rows outside 0 .. T - 1.)
+__device__ __forceinline__ bool item_at(const RowsArgs& a, int64_t item, int h, int cols, int lane, Item* it) {
+  const int g = a.n_q_heads / a.kv.n_kv_heads;
+  int64_t before = 0;
+  for (int base = 0; base < a.B; base += 64) {
+    const int b = base + lane;
+    int row0 = 0, n = 0;
+    if (b < a.B) {
+      row0 = clampi(a.starts[b], 0, a.T);
+      n = clampi(a.starts[b + 1], row0, a.T) - row0;
+    }
+    const int groups = (n * g + cols - 1) / cols;
+    int upto = groups;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    if (item < before + all) {
+      const int l = __ffsll(static_cast<long long>(__ballot(before + upto > item))) - 1;
+      if (l < 0) return false;
+      it->b = base + l;
+      it->h = h;
+      it->row0 = __builtin_amdgcn_readlane(row0, l);
+      it->n = __builtin_amdgcn_readlane(n, l);
+      const int64_t group = item - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(groups, l));
+      if (group < 0 || group * cols >= static_cast<int64_t>(it->n) * g) return false;
+      it->col0 = static_cast<int>(group) * cols;
+      it->n_col = min(cols, it->n * g - it->col0);
+      const int64_t len = a.lens[it->b];
+      it->ctx = clamp64(len - it->n, -(1 << 30), INT32_MAX);
+      const int first = it->col0 / g, last = (it->col0 + it->n_col - 1) / g;
+      if (a.masks) {
+        it->hi = clamp64(len, 0, a.max_len);
+        it->lo = a.window ? clamp64(static_cast<int64_t>(it->ctx) - a.window, 0, it->hi) : 0;
+      } else {
+        it->hi = clamp64(static_cast<int64_t>(it->ctx) + last + 1, 0, a.max_len);
+        it->lo = a.window ? clamp64(static_cast<int64_t>(it->ctx) + first + 1 - a.window, 0, it->hi) : 0;
+      }
+      it->t0 = it->lo / kTile;
+      it->tiles = it->hi > it->lo ? (it->hi + kTile - 1) / kTile - it->t0 : 0;
+      return true;
+    }
+    before += all;
+  }
+  return false;
+}
+
+// What column c (row i, one of the lane's) sees: positions [lo, hi), and of a tree
+// the drafted tokens in its mask.
+struct Column {
+  int lo, hi;
+  int row;                 // of q and the masks; -1: no column
+};
+__device__ __forceinline__ Column column_at(const RowsArgs& a, const Item& it, int c, int g) {
+  Column x{0, 0, -1};
+  if (c >= it.n_col) return x;
+  const int i = (it.col0 + c) / g;
+  x.row = it.row0 + i;
+  if (a.masks) {
+    x.hi = clampi(it.ctx, 0, a.max_len);
+    if (a.window) {
+      int64_t seen = 0;
+      for (int w = 0; w < a.words && 64 * w < it.n; ++w) {
+        uint64_t m = static_cast<uint64_t>(a.masks[static_cast<int64_t>(x.row) * a.words + w]);
+        if (it.n - 64 * w < 64) m &= (1ull << (it.n - 64 * w)) - 1ull;
+        seen += __popcll(m);
+      }
+      x.lo = clamp64(it.ctx + seen - a.window, 0, x.hi);
+    }
+  } else {
+    x.hi = clamp64(static_cast<int64_t>(it.ctx) + i + 1, 0, a.max_len);
+    x.lo = a.window ? clamp64(static_cast<int64_t>(it.ctx) + i + 1 - a.window, 0, x.hi) : 0;
+  }
+  return x;
+}
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : (1u << n) - 1u; }
+// Bit i: the column sees position t + i.
+__device__ __forceinline__ uint32_t seen_of(const RowsArgs& a, const Item& it, const Column& x, int t) {
+  uint32_t s = first_bits(clamp64(static_cast<int64_t>(x.hi) - t, 0, 32)) & ~first_bits(clamp64(static_cast<int64_t>(x.lo) - t, 0, 32));
+  if (a.masks && x.row >= 0 && t + kTile > it.ctx) {
+    const int64_t j = static_cast<int64_t>(t) - it.ctx;          // drafted token of bit 0, above -32
+    const int64_t* m = a.masks + static_cast<int64_t>(x.row) * a.words;
+    uint64_t d = 0;
+    if (j < 0) {
+      d = static_cast<uint64_t>(m[0]) << -j;
+    } else if (j < 64 * static_cast<int64_t>(a.words)) {
+      const int w = static_cast<int>(j >> 6), sh = static_cast<int>(j & 63);
+      d = static_cast<uint64_t>(m[w]) >> sh;
+      if (sh > 32 && w + 1 < a.words) d |= static_cast<uint64_t>(m[w + 1]) << (64 - sh);
+    }
+    s |= static_cast<uint32_t>(d) & first_bits(clamp64(static_cast<int64_t>(it.hi) - t, 0, 32));
+  }
+  return s;
+}
+
+// Values that are no numbers would enter columns that do not see them (0 x NaN), so
+// in tiles that some columns see in part they are taken out of the product, and
+// added one by one to the columns that do. Where all columns see an infinity, the
+// product of a weight in two terms is none (inf - inf): a wave whose outputs are not
+// all numbers goes through its tiles once more, with that done in all of them.
+template <int BITS, int PV>
+__device__ __forceinline__ uint32_t odd_parts(uint32_t w) {      // ones over the parts of a word that are no numbers
+  if constexpr (BITS == 8) {
+    const uint32_t z = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    return (z >> 7) * 0xFFu;
+  } else {
+    constexpr uint32_t kExp = PV == PW_BF16 ? 0x7F80u : 0x7C00u;
+    return ((w & kExp) == kExp ? 0xFFFFu : 0u) | (((w >> 16) & kExp) == kExp ? 0xFFFF0000u : 0u);
+  }
+}
+
+template <int D>
+struct RowsLds {
+  float o[kRowsWaves][16][D + 4];
+  float m[kRowsWaves][16], l[kRowsWaves][16];
+};
+
+// Tiles [begin, end) of the item's span, by the workgroup's waves in turn; C x 16
+// columns a wave, the same for all. whole: no other workgroup has tiles of the item,
+// the result goes to the output; else to slot `slot`.
+template <int ACT, int BITS, int D, int C>
+__device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, const Item& it, int begin, int end, bool whole,
+                                            int64_t slot) {
+  constexpr int W = kRowsWaves;
+  constexpr int kPv = BITS == 8 ? PW_BF16 : ACT;      // 16-bit type of the second product
+  constexpr bool kByTile = kPv == PW_F16;             // exponentials against the tile's maximum
+  constexpr int kLoads = D * BITS / 8 * 16 / 1024;    // 1 KB loads of 16 tokens' keys
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
+  const int col = lane & 15, lg = lane >> 4;
+  const int P = a.kv.block_tokens, h = it.h;
+  const int first = begin + wave;                                // the wave's tiles: first, first + W, ...
+  const int n_my = first < end ? (end - first + W - 1) / W : 0;
+  const int g = a.n_q_heads / a.kv.n_kv_heads;
+
+  Column x[C];
+  u32x4 q[C][D / 32];
+  int all_lo = 0, all_hi = INT32_MAX;                            // all columns see [all_lo, all_hi)
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int cc = 16 * c + col;
+    x[c] = column_at(a, it, cc, g);
+    if (x[c].row >= 0) {
+      all_lo = max(all_lo, x[c].lo);
+      all_hi = min(all_hi, x[c].hi);
+    }
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      q[c][i] = u32x4{0u, 0u, 0u, 0u};
+      if (x[c].row >= 0)
+        q[c][i] = ld16(reinterpret_cast<const uint8_t*>(a.q + static_cast<int64_t>(x[c].row) * a.ldq +
+                                                        (h * g + (it.col0 + cc) % g) * a.ldqh + 32 * i + 8 * lg));
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    all_lo = max(all_lo, __shfl_xor(all_lo, o));
+    all_hi = min(all_hi, __shfl_xor(all_hi, o));
+  }
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+
+  // The tiles in blocks of the pool, one after the other (tiles in other blocks
+  // are left out): bits of the 64 numbers at hand, then the next 64.
+  const auto block_of = [&](int i) {                             // of the wave's tile i
+    if (i >= n_my) return -1;
+    const int64_t t = static_cast<int64_t>(it.t0 + first + W * i) * kTile;
+    return static_cast<int>(a.table[it.b * a.ld_table + (t >> __builtin_ctz(P))]);
+  };
+  int ids, chunk;
+  uint64_t todo;
+  int next_t = -1, next_id = 0;                                  // first token of the next tile (-1: none), its block
+  const auto advance = [&] {
+    while (todo == 0 && chunk + 64 < n_my) {
+      chunk += 64;
+      ids = block_of(chunk + lane);
+      todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
+    }
+    next_t = -1;
+    if (todo) {
+      const int l = __ffsll(static_cast<long long>(todo)) - 1;
+      todo &= todo - 1;
+      next_id = __builtin_amdgcn_readlane(ids, l);
+      next_t = (it.t0 + first + W * (chunk + l)) * kTile;
+    }
+  };
+  const size_t head_off = static_cast<size_t>(2 * h) * P * D * (BITS / 8);
+  const size_t v_off = static_cast<size_t>(P) * D * (BITS / 8);
+  const size_t sc_off = static_cast<size_t>(2) * a.kv.n_kv_heads * P * D + static_cast<size_t>(h) * P * 4;
+  const size_t vs_off = static_cast<size_t>(a.kv.n_kv_heads) * P * 4;
+  const float scale2 = a.scale * kLog2e;
+
+  u32x4 k[2][kLoads], v[2 * kLoads];
+  f32x4 ks[2], vs[2];
+  const auto values_at = [&](int id, int t) {                    // of the tile, in memory
+    return a.kv.pool + static_cast<int64_t>(id) * a.kv.block_stride + head_off + v_off +
+           static_cast<size_t>(t & (P - 1)) * D * (BITS / 8);
+  };
+  const auto load_k = [&] {
+    const int t = next_t & (P - 1);                              // in the block
+    const uint8_t* blk = a.kv.pool + static_cast<int64_t>(next_id) * a.kv.block_stride;
+    const uint8_t* p = blk + head_off + static_cast<size_t>(t) * D * (BITS / 8) + 16 * lane;
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) k[r][j] = ld16(p + (r * kLoads + j) * 1024);
+    if constexpr (BITS == 8) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) ks[r] = *reinterpret_cast<const f32x4*>(blk + sc_off + 4 * t + 16 * lg + 64 * r);
+    }
+  };
+  const auto load_v = [&] {
+    const int t = next_t & (P - 1);
+    const uint8_t* p = values_at(next_id, next_t) + 16 * lane;
+#pragma unroll
+    for (int j = 0; j < 2 * kLoads; ++j) v[j] = ld16(p + j * 1024);
+    if constexpr (BITS == 8) {
+      const uint8_t* blk = a.kv.pool + static_cast<int64_t>(next_id) * a.kv.block_stride;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) vs[r] = *reinterpret_cast<const f32x4*>(blk + sc_off + vs_off + 4 * t + 16 * lg + 64 * r);
+    }
+  };
+
+  f32x4 o[C][D / 16];
+  float m[C], l[C];
+  for (bool careful = false;; careful = true) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) o[c][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      m[c] = kNoMax;
+      l[c] = 0.0f;
+    }
+
+    ids = block_of(lane);
+    chunk = 0;
+    todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
+    advance();
+    if (next_t >= 0) {
+      load_k();
+      load_v();
+    }
+    while (next_t >= 0) {
+      const int t = next_t, id = next_id;
+      f32x4 s[C][2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) s[c][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+          u32x4 kk;
+          if constexpr (BITS == 16) kk = k[r][j];
+          else kk = widen8<ACT>(k[r][j / 2][2 * (j & 1)], k[r][j / 2][2 * (j & 1) + 1]);
+#pragma unroll
+          for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(kk, q[c][j], s[c][r]);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[c][r][e] *= BITS == 8 ? scale2 * ks[r][e] : scale2;
+      const bool part = t < all_lo || t + kTile > all_hi;          // some column does not see all of it
+      bool odd = false;
+      if (part || careful) {
+        // what no column may see is left out, whatever its bits
+        uint32_t keep[2][2];                                       // of four tokens' 8 or 16 bits
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          keep[r][0] = keep[r][1] = 0u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = t + 16 * r + 4 * lg + e;
+            const bool in = tok >= it.lo && tok < it.hi;
+            if constexpr (BITS == 8) {
+              vs[r][e] = in ? vs[r][e] : 0.0f;
+              keep[r][0] |= in ? 0xFFu << (8 * e) : 0u;
+            } else {
+              keep[r][e / 2] |= in ? 0xFFFFu << (16 * (e & 1)) : 0u;
+            }
+          }
+        }
+        uint32_t any = 0u;
+#pragma unroll
+        for (int j = 0; j < 2 * kLoads; ++j)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            v[j][w] &= BITS == 8 ? keep[w & 1][0] : keep[w / 2][w & 1];
+            const uint32_t z = odd_parts<BITS, kPv>(v[j][w]);
+            any |= z;
+            v[j][w] &= ~z;
+          }
+        odd = __any(any != 0u);
+      }
+      advance();
+      if (next_t >= 0) load_k();
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        uint32_t seen = ~0u;
+        if (part) {
+          seen = seen_of(a, it, x[c], t);
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[c][r][e] = (seen >> (16 * r + 4 * lg + e)) & 1u ? s[c][r][e] : -INFINITY;
+        }
+        float top = s[c][0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, s[c][e / 4][e & 3]);
+        float base = m[c];                                         // probabilities are exp2(s - base)
+        float f = 1.0f, share = 1.0f;                              // factors of what is there and of this tile
+        bool raise;
+        if constexpr (kByTile) {
+          top = fmaxf(column_max(top), kNoMax);                    // (a number, whatever the scores)
+          raise = __any(top > m[c]);
+          const float m_new = fmaxf(m[c], top);
+          f = __builtin_amdgcn_exp2f(m[c] - m_new);
+          share = __builtin_amdgcn_exp2f(top - m_new);
+          base = top;
+          m[c] = m_new;
+        } else {
+          raise = __any(top > m[c] + kSlack);
+          if (raise) {
+            const float m_new = fmaxf(m[c], column_max(top));
+            f = __builtin_amdgcn_exp2f(m[c] - m_new);
+            base = m[c] = m_new;
+          }
+        }
+        if (raise) {
+          l[c] *= f;
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][j][e] *= f;
+        }
+        float sum = 0.0f, pr[8];
+        u32x4 p_hi, p_lo;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          float p[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = w / 2, y = 2 * (w & 1) + e;
+            pr[2 * w + e] = p[e] = __builtin_amdgcn_exp2f(s[c][r][y] - base);
+            sum += p[e];
+            if constexpr (BITS == 8) {
+              p[e] *= vs[r][y];
+              if (part) p[e] = (seen >> (16 * r + 4 * lg + y)) & 1u ? p[e] : 0.0f;
+            }
+            if constexpr (kByTile) p[e] *= kLift;
+          }
+          p_hi[w] = pack16<kPv>(p[0], p[1]);
+          p[0] -= val16(p_hi[w] & 0xFFFFu, kPv);
+          p[1] -= val16(p_hi[w] >> 16, kPv);
+          p_lo[w] = kByTile ? pack16<kPv>(p[0] * kLow, p[1] * kLow) : pack16<kPv>(p[0], p[1]);
+        }
+        l[c] = fmaf(share, sum, l[c]);
+        if (odd) {
+          const uint8_t* vm = values_at(id, t);
+          for (int i = 0; i < kTile; ++i) {
+            const int at = 4 * (i / 16) + i % 4;                   // token i's place in lanes 16 (i / 4 mod 4) ..
+            float p = pr[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) p = at == e ? pr[e] : p;
+            p = __shfl(p, 16 * (i / 4 % 4) + col) * share;
+            const bool on = (seen >> i) & 1u;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int place = 16 * (16 * (i / 4 % 4) + 4 * lg + e);
+                float y = 0.0f;
+                if constexpr (BITS == 16) {
+                  const uint32_t w = *reinterpret_cast<const uint16_t*>(vm + j * 1024 + place + 2 * (4 * (i / 16) + i % 4));
+                  if (odd_parts<16, kPv>(w) & 0xFFFFu) y = val16(w, kPv);
+                } else {
+                  const uint32_t w = vm[(j / 2) * 1024 + place + 8 * (j & 1) + 4 * (i / 16) + i % 4];
+                  if ((w & 0x7Fu) == 0x7Fu) y = __builtin_nanf("");
+                }
+                if (on && y != 0.0f) o[c][j][e] = fmaf(p, y, o[c][j][e]);
+              }
+          }
+        }
+        if constexpr (kByTile) share *= 1.0f / kLift;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          u32x4 vv;
+          if constexpr (BITS == 16) vv = v[j];
+          else vv = widen8<kPv>(v[j / 2][2 * (j & 1)], v[j / 2][2 * (j & 1) + 1]);
+          if constexpr (kByTile) {
+            const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f}, hi = mma<kPv>(vv, p_hi, zero), lo = mma<kPv>(vv, p_lo, zero);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][j][e] = fmaf(share, fmaf(lo[e], 1.0f / kLow, hi[e]), o[c][j][e]);
+            asm volatile("" : "+v"(o[c][j]));                      // (not all products before all sums: registers)
+          } else {
+            o[c][j] = mma<kPv>(vv, p_hi, o[c][j]);
+            o[c][j] = mma<kPv>(vv, p_lo, o[c][j]);
+          }
+        }
+      }
+      if (next_t >= 0) load_v();
+    }
+    bool bad = false;
+    if constexpr (BITS == 16) {                                  // (an 8-bit NaN gives one, however often it is added)
+      if (!careful) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad |= !(fabsf(o[c][j][e]) < INFINITY);
+      }
+    }
+    if (!__any(bad)) break;
+  }
+
+  // join the waves, 16 columns at a time
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int n_col = min(16, it.n_col - 16 * c);                // (uniform)
+    if (n_col <= 0) break;
+    if (c) __syncthreads();                                      // what was joined before is read
+    float sum_l = l[c];
+    sum_l += __shfl_xor(sum_l, 16);
+    sum_l += __shfl_xor(sum_l, 32);
+    if (col < n_col) {
+      if (lg == 0) {
+        lds.m[wave][col] = m[c];
+        lds.l[wave][col] = sum_l;
+      }
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) *reinterpret_cast<f32x4*>(&lds.o[wave][col][16 * j + 4 * lg]) = o[c][j];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < n_col * (D / 4); e += 64 * W) {
+      const int y = e / (D / 4), d = 4 * (e % (D / 4));
+      float mx = lds.m[0][y];
+#pragma unroll
+      for (int w = 1; w < W; ++w) mx = fmaxf(mx, lds.m[w][y]);
+      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float f = __builtin_amdgcn_exp2f(lds.m[w][y] - mx);
+        sum = fmaf(f, lds.l[w][y], sum);
+        const f32x4 z = *reinterpret_cast<const f32x4*>(&lds.o[w][y][d]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = fmaf(f, z[j], acc[j]);
+      }
+      const int cc = 16 * c + y;
+      if (whole) {
+        const int row = it.row0 + (it.col0 + cc) / g, hq = h * g + (it.col0 + cc) % g;
+        const int64_t at = static_cast<int64_t>(row) * a.n_q_heads + hq;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<u32x2*>(a.out + at * D + d) =
+            u32x2{pack16<ACT>(acc[0] * inv, acc[1] * inv), pack16<ACT>(acc[2] * inv, acc[3] * inv)};
+        if (a.lse && d == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
+      } else {
+        const int64_t at = slot * (16 * C) + cc;
+        *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = acc;
+        if (d == 0) {
+          a.part_ml[2 * at] = mx;
+          a.part_ml[2 * at + 1] = sum;
+        }
+      }
+    }
+  }
+}
+
+// Vector registers of a wave, for what the kernel holds from tile to tile.
+constexpr bool rows_two_waves(int bits, int D, int C) {
+  return C * (D / 8 + D / 4 + 8) + D / 4 * bits / 16 * 2 + 48 <= 224;
+}
+
+template <int ACT, int BITS, int D, int C>
+__global__ __launch_bounds__(64 * kRowsWaves, rows_two_waves(BITS, D, C) ? 2 : 1) void k_attn_rows(RowsArgs a) {
+  __shared__ RowsLds<D> lds;
+  const int h = blockIdx.x % a.kv.n_kv_heads;
+  const int64_t rest = blockIdx.x / a.kv.n_kv_heads;
+  const int split = static_cast<int>(rest % a.n_splits);
+  const int64_t item = rest / a.n_splits;
+  Item it;
+  if (!item_at(a, item, h, 16 * C, lane_id(), &it)) return;
+  const int n_act = (it.tiles + a.split_tiles - 1) / a.split_tiles;
+  if (split > 0 && split >= n_act) return;
+  const int begin = split * a.split_tiles, end = min(begin + a.split_tiles, it.tiles);
+  attend_rows<ACT, BITS, D, C>(a, lds, it, begin, end, n_act <= 1, (item * a.kv.n_kv_heads + h) * a.n_splits + split);
+}
+
+// Joins the parts of four columns of an item, a wave for each, in a fixed order.
+template <int ACT, int D>
+__global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols) {
+  constexpr int kC = D / 64;
+  const int lane = lane_id(), c = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int h = blockIdx.x % a.kv.n_kv_heads;
+  const int64_t item = blockIdx.x / a.kv.n_kv_heads;
+  Item it;
+  if (!item_at(a, item, h, cols, lane, &it) || c >= it.n_col) return;
+  const int n = (it.tiles + a.split_tiles - 1) / a.split_tiles;
+  if (n <= 1) return;
+  const int64_t at = (item * a.kv.n_kv_heads + h) * a.n_splits * cols + c;
+  float mx = kNoMax;
+  for (int s = lane; s < n; s += 64) mx = fmaxf(mx, a.part_ml[2 * (at + static_cast<int64_t>(s) * cols)]);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  float acc[kC] = {}, sum = 0.0f;
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const int64_t y = at + static_cast<int64_t>(s) * cols;
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * y] - mx);
+    sum = fmaf(f, a.part_ml[2 * y + 1], sum);
+#pragma unroll
+    for (int j = 0; j < kC; ++j) acc[j] = fmaf(f, a.part_o[y * D + 64 * j + lane], acc[j]);
+  }
+  const int g = a.n_q_heads / a.kv.n_kv_heads;
+  const int64_t row = static_cast<int64_t>(it.row0 + (it.col0 + c) / g) * a.n_q_heads + h * g + (it.col0 + c) % g;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int j = 0; j < kC; ++j) a.out[row * D + 64 * j + lane] = static_cast<uint16_t>(pack16<ACT>(acc[j] * inv, 0.0f));
+  if (a.lse && lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
+}
+
+template <int ACT, int BITS, int D>
+hipError_t launch_d(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
+  const int64_t grid = p.items * a.kv.n_kv_heads * p.n_splits;
+  if (grid >= (1 << 23)) return hipErrorInvalidConfiguration;
+  const uint32_t n = static_cast<uint32_t>(grid);
+  if (p.col_tiles == 1) k_attn_rows<ACT, BITS, D, 1><<<n, 64 * kRowsWaves, 0, st>>>(a);
+  else if (D > 128 || p.col_tiles == 2) k_attn_rows<ACT, BITS, D, 2><<<n, 64 * kRowsWaves, 0, st>>>(a);
+  else if constexpr (D <= 128) k_attn_rows<ACT, BITS, D, 4><<<n, 64 * kRowsWaves, 0, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.n_splits == 1) return e;
+  const int cols = 16 * p.col_tiles;
+  k_rows_join<ACT, D><<<dim3(static_cast<uint32_t>(p.items * a.kv.n_kv_heads), cols / 4), 256, 0, st>>>(a, cols);
+  return hipGetLastError();
+}
+
+template <int ACT, int BITS>
+hipError_t launch_bits(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
+  switch (a.kv.head_dim) {
+    case 64: return launch_d<ACT, BITS, 64>(a, p, st);
+    case 128: return launch_d<ACT, BITS, 128>(a, p, st);
+    case 192: return launch_d<ACT, BITS, 192>(a, p, st);
+    case 256: return launch_d<ACT, BITS, 256>(a, p, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int bits, int max_len, int window) {
+  RowsPlan p{1, 1, 1, 0, 0};
+  if (B == 0 || T == 0) return p;
+  const int64_t g = n_q_heads / n_kv_heads, cols = g * ((static_cast<int64_t>(T) + B - 1) / B);
+  p.col_tiles = cols <= 16 ? 1 : cols <= 32 || head_dim > 128 ? 2 : 4;
+  const int64_t group = 16 * p.col_tiles;
+  p.items = g * T / group + (B < T ? B : T);
+  int64_t tiles = (static_cast<int64_t>(max_len) + kTile - 1) / kTile;
+  if (window > 0) {
+    const int64_t w = (static_cast<int64_t>(window) + T + 2 * kTile - 2) / kTile;
+    tiles = w < tiles ? w : tiles;
+  }
+  if (tiles == 0) tiles = 1;
+  const int64_t most = (tiles + 31) / 32, want = (1024 + p.items * n_kv_heads - 1) / (p.items * n_kv_heads);
+  int64_t n = want < most ? want : most;
+  const int64_t per = ((tiles + n - 1) / n + kRowsWaves - 1) / kRowsWaves * kRowsWaves;
+  n = (tiles + per - 1) / per;
+  p.n_splits = static_cast<int>(n);
+  p.split_tiles = static_cast<int>(per);
+  if (n > 1) p.slots = static_cast<size_t>(p.items * n_kv_heads * n) * group;
+  return p;
+}
+
+hipError_t launch_attn_rows(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
+  if (a.kv.act == PW_BF16)
+    return a.kv.bits == 16 ? launch_bits<PW_BF16, 16>(a, p, st) : launch_bits<PW_BF16, 8>(a, p, st);
+  return a.kv.bits == 16 ? launch_bits<PW_F16, 16>(a, p, st) : launch_bits<PW_F16, 8>(a, p, st);
+}
+
+}  // namespace pw

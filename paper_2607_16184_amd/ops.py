@@ -179,6 +179,77 @@ class Linear8:
 
 
 # ---------------------------------------------------------------------------
+# Heads of queries and keys
+# ---------------------------------------------------------------------------
+
+class Rotation:
+    """A position rotation of the first ``dims`` channels of a head (pw_rotation):
+    pair i by position * inv_freq[i], by default base^(-2 i / dims); pairs (i, i +
+    dims / 2), or neighbours where ``interleaved``."""
+
+    def __init__(self, dims: int, base: float = 10000.0, inv_freq: torch.Tensor = None, amplitude: float = 1.0,
+                 interleaved: bool = False, device="cuda"):
+        _need(dims >= 0 and dims % 16 == 0, "dims must be a multiple of 16")
+        if inv_freq is None:
+            inv_freq = (base ** (-torch.arange(0, dims, 2, dtype=torch.float64) / max(dims, 1))).to(device)
+        _need(inv_freq.shape == (dims // 2,), "inv_freq must be [dims / 2]")
+        self.inv_freq = inv_freq.to(torch.float64).contiguous()
+        self.dev = self.inv_freq.get_device()
+        _need(self.dev >= 0, "inv_freq must lie on the device")
+        self.dims, self.interleaved, self.amplitude = dims, interleaved, amplitude
+        self.desc = pw.pw_rotation(self.inv_freq.data_ptr(), dims, int(interleaved), amplitude)
+
+
+def _rows(t: Optional[torch.Tensor], T: int, D: int, act: torch.dtype, dev: int, name: str):
+    """(address, heads, row stride, head stride) of heads [T, n, D]; nothing for None."""
+    if t is None:
+        return 0, 0, 0, 0
+    if not (t.dim() == 3 and t.shape[0] == T and t.shape[2] == D and t.dtype is act and t.get_device() == dev):
+        raise ValueError("%s must be [%d, heads, %d], %s, on device %d" % (name, T, D, act, dev))
+    ld, ldh, inner = t.stride()
+    _need(inner == 1, name + " must have contiguous channels")
+    n = t.shape[1]
+    return t.data_ptr(), n, ld if T > 1 else 0, ldh if n > 1 else 0   # a single row, or head, may have any stride
+
+
+def _turned(rotation: Optional[Rotation], positions: Optional[torch.Tensor], T: int, dev: int):
+    """The library's rotation and the positions' address."""
+    if rotation is None or rotation.dims == 0:
+        _packed(positions, (T,), torch.int32, dev, "positions")
+        return None, 0
+    _need(rotation.dev == dev, "the rotation lies on another device")
+    _need(positions is not None, "a rotation needs positions")
+    _packed(positions, (T,), torch.int32, dev, "positions")
+    return rotation.desc, positions.data_ptr()
+
+
+def norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional[torch.Tensor], rotation: Optional[Rotation],
+                q_weight: torch.Tensor = None, k_weight: torch.Tensor = None, *, norm: bool = True, eps: float = 1e-6,
+                offset: int = 0, out=None, stream=None):
+    """Queries [T, heads, head_dim] and keys (or None) normed by head where
+    ``norm``, then turned by positions [T] int32 + offset: (q, k) in new tensors or
+    those of ``out``, which may be q and k themselves (pw_heads_norm_rotate)."""
+    T, n, D = q.shape
+    act, dev = q.dtype, q.get_device()
+    _need((act is torch.bfloat16 or act is torch.float16) and dev >= 0, "q must be 16-bit heads on the device")
+    rot, pos = _turned(rotation, positions, T, dev)
+    q_ptr, n_q, ldq, ldqh = _rows(q, T, D, act, dev, "q")
+    k_ptr, n_k, ldk, ldkh = _rows(k, T, D, act, dev, "k")
+    _packed(q_weight, (D,), act, dev, "q_weight")
+    _packed(k_weight, (D,), act, dev, "k_weight")
+    if out is None:
+        out = (_empty(q.shape, act, q.device, stream), None if k is None else _empty(k.shape, act, q.device, stream))
+    qo, ko = out
+    _need(qo.shape == q.shape and (ko is None) == (k is None) and (k is None or ko.shape == k.shape),
+          "out must have the shapes of q and k")
+    qo_ptr, _, ldqo, ldqoh = _rows(qo, T, D, act, dev, "out")
+    ko_ptr, _, ldko, ldkoh = _rows(ko, T, D, act, dev, "out")
+    _call(dev, pw.pw_heads_norm_rotate, rot, pos, offset, q_ptr, ldq, ldqh, n_q, k_ptr, ldk, ldkh, n_k, _ptr(q_weight),
+          _ptr(k_weight), int(norm), eps, T, D, _TYPE[act], qo_ptr, ldqo, ldqoh, ko_ptr, ldko, ldkoh, _on(dev, stream))
+    return qo, ko
+
+
+# ---------------------------------------------------------------------------
 # KV cache
 # ---------------------------------------------------------------------------
 
@@ -248,6 +319,85 @@ class KVCache:
                 lens.data_ptr(), B, max_len, D ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse))
         self._ws.run(dev, stream, pw.pw_attn_decode, args,
                      lambda: pw.pw_attn_workspace(self.desc, B, heads, max_len, window))
+        return out
+
+
+    def append_rotated(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor],
+                       rotation: Optional[Rotation], q: torch.Tensor = None, q_weight: torch.Tensor = None,
+                       k_weight: torch.Tensor = None, *, norm: bool = True, eps: float = 1e-6, offset: int = 0,
+                       q_out: torch.Tensor = None, stream=None) -> Optional[torch.Tensor]:
+        """``norm_rotate`` of q [T, heads, head_dim] (or None) and k, with k and v
+        written to the slots as ``append`` does: q in a new tensor or in ``q_out``,
+        which may be q itself (pw_kv_append_rotated)."""
+        T, D, dev, act = k.shape[0], self.head_dim, self.dev, self.act
+        k_ptr, n_k, ld, ldh = _rows(k, T, D, act, dev, "k")
+        v_ptr, n_v, ldv, ldvh = _rows(v, T, D, act, dev, "v")
+        _need(n_k == self.kv_heads and n_v == n_k and ld == ldv and ldh == ldvh,
+              "k and v must be [T, kv_heads, head_dim] with equal strides")
+        _packed(slots, (T,), torch.int64, dev, "slots")
+        rot, pos = _turned(rotation, positions, T, dev)
+        _packed(q_weight, (D,), act, dev, "q_weight")
+        _packed(k_weight, (D,), act, dev, "k_weight")
+        if q is not None and q_out is None:
+            q_out = _empty(q.shape, act, q.device, stream)
+        _need((q is None) == (q_out is None) and (q is None or q_out.shape == q.shape), "q_out must have q's shape")
+        q_ptr, n_q, ldq, ldqh = _rows(q, T, D, act, dev, "q")
+        qo_ptr, _, ldqo, ldqoh = _rows(q_out, T, D, act, dev, "q_out")
+        _call(dev, pw.pw_kv_append_rotated, self.desc, rot, pos, offset, q_ptr, ldq, ldqh, n_q, k_ptr, v_ptr, ld, ldh,
+              _ptr(q_weight), _ptr(k_weight), int(norm), eps, slots.data_ptr(), T, qo_ptr, ldqo, ldqoh, _on(dev, stream))
+        return q_out
+
+    def _table(self, block_table: torch.Tensor, B: int, max_len: int):
+        """(address, row stride) of a block table."""
+        rows, blocks = block_table.shape
+        _need(block_table.dtype is torch.int32 and rows == B and block_table.get_device() == self.dev
+              and (block_table.stride(1) == 1 or blocks <= 1), "block_table must be [B, blocks] int32 on the cache's device")
+        _need(blocks * self.block_tokens >= max_len, "the block table is shorter than max_len")
+        return block_table.data_ptr(), block_table.stride(0) if B > 1 else blocks
+
+    def attend_rows(self, q: torch.Tensor, starts: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, max_len: int,
+                    masks: torch.Tensor = None, scale: float = None, window: int = 0, out: torch.Tensor = None,
+                    lse: torch.Tensor = None, stream=None) -> torch.Tensor:
+        """Attention of several new tokens per sequence: rows starts[b] .. starts[b
+        + 1] - 1 of q [T, heads, head_dim] are the last of the lens[b] cached tokens
+        of the blocks block_table[b]. Each sees the tokens up to itself, or with
+        ``masks`` [T, words] int64 the context and the new tokens whose bits are set
+        -> [T, heads, head_dim]; rows of no sequence are not written
+        (pw_attn_rows)."""
+        T, heads, D = q.shape
+        dev, B = self.dev, lens.shape[0]
+        q_ptr, _, ldq, ldqh = _rows(q, T, self.head_dim, self.act, dev, "q")
+        _packed(starts, (B + 1,), torch.int32, dev, "starts")
+        _packed(lens, (B,), torch.int32, dev, "lens")
+        words = 0 if masks is None else masks.shape[1]
+        _packed(masks, (T, words), torch.int64, dev, "masks")
+        table, ld_table = self._table(block_table, B, max_len)
+        if out is None:
+            out = _empty((T, heads, D), self.act, q.device, stream)
+        _packed(out, (T, heads, D), self.act, dev, "out")
+        _packed(lse, (T, heads), torch.float32, dev, "lse")
+        args = (self.desc, q_ptr, ldq, ldqh, heads, starts.data_ptr(), T, _ptr(masks), words, table, ld_table, lens.data_ptr(), B,
+                max_len, D ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse))
+        self._ws.run(dev, stream, pw.pw_attn_rows, args,
+                     lambda: pw.pw_attn_rows_workspace(self.desc, B, T, heads, max_len, window))
+        return out
+
+    def keep(self, starts: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, max_len: int, chosen: torch.Tensor,
+             out: torch.Tensor = None, stream=None) -> torch.Tensor:
+        """Of each sequence's new tokens (as in ``attend_rows``) move the chosen
+        ones, by bits [B, words] int64, together behind the context -> the new
+        lengths [B] int32 (pw_kv_keep)."""
+        dev, B = self.dev, lens.shape[0]
+        _packed(starts, (B + 1,), torch.int32, dev, "starts")
+        _packed(lens, (B,), torch.int32, dev, "lens")
+        words = chosen.shape[1]
+        _packed(chosen, (B, words), torch.int64, dev, "chosen")
+        table, ld_table = self._table(block_table, B, max_len)
+        if out is None:
+            out = _empty((B,), torch.int32, lens.device, stream)
+        _packed(out, (B,), torch.int32, dev, "out")
+        _call(dev, pw.pw_kv_keep, self.desc, starts.data_ptr(), table, ld_table, lens.data_ptr(), B, max_len, chosen.data_ptr(),
+              words, out.data_ptr(), _on(dev, stream))
         return out
 
 

@@ -68,6 +68,11 @@ class pw_kv_cache(ctypes.Structure):
                 ("head_dim", ctypes.c_int), ("act", ctypes.c_int), ("bits", ctypes.c_int)]
 
 
+class pw_rotation(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("dims", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("amplitude", ctypes.c_float)]
+
+
 class PWError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__("%s: %s" % (_status_name(status), msg))
@@ -142,6 +147,14 @@ def _load():
         "pw_kv_append": (i32, [P(pw_kv_cache), vp, vp, i64, i64, vp, i32, vp]),
         "pw_attn_workspace": (i32, [P(pw_kv_cache), i32, i32, i32, i32, P(sz)]),
         "pw_attn_decode": (i32, [P(pw_kv_cache), vp, i64, i64, i32, vp, i64, vp, i32, i32, f32, i32, vp, vp, vp, sz, vp]),
+        "pw_heads_norm_rotate": (i32, [P(pw_rotation), vp, i32, vp, i64, i64, i32, vp, i64, i64, i32, vp, vp, i32, f32, i32, i32, i32,
+                                       vp, i64, i64, vp, i64, i64, vp]),
+        "pw_kv_append_rotated": (i32, [P(pw_kv_cache), P(pw_rotation), vp, i32, vp, i64, i64, i32, vp, vp, i64, i64, vp, vp, i32, f32,
+                                       vp, i32, vp, i64, i64, vp]),
+        "pw_kv_keep": (i32, [P(pw_kv_cache), vp, vp, i64, vp, i32, i32, vp, i32, vp, vp]),
+        "pw_attn_rows_workspace": (i32, [P(pw_kv_cache), i32, i32, i32, i32, i32, P(sz)]),
+        "pw_attn_rows": (i32, [P(pw_kv_cache), vp, i64, i64, i32, vp, i32, vp, i32, vp, i64, vp, i32, i32, f32, i32, vp, vp, vp, sz,
+                               vp]),
         "pw_route_grouped": (i32, [vp, i32, vp, i32, i32, i32, i32, i32, i32, i32, i32, f32, i32, vp, vp, vp, vp, vp, vp,
                                    vp]),
         "pw_last_error": (ctypes.c_char_p, []),
@@ -525,6 +538,47 @@ def pw_attn_decode(cache: pw_kv_cache, q_ptr: int, ldq: int, ldqh: int, n_q_head
                    ws_bytes: int, stream: int):
     _check(_lib.pw_attn_decode(ctypes.byref(cache), q_ptr, ldq, ldqh, n_q_heads, table_ptr, ld_table, lens_ptr, B, max_len,
                                scale, window, out_ptr, lse_ptr, ws_ptr, ws_bytes, stream))
+
+
+def _rotation(rot):
+    return None if rot is None else ctypes.byref(rot)
+
+
+def pw_heads_norm_rotate(rot, positions_ptr: int, offset: int, q_ptr: int, ldq: int, ldqh: int, n_q: int, k_ptr: int, ldk: int,
+                         ldkh: int, n_k: int, q_weight_ptr: int, k_weight_ptr: int, norm: int, eps: float, T: int, head_dim: int,
+                         act: int, q_out_ptr: int, ldqo: int, ldqoh: int, k_out_ptr: int, ldko: int, ldkoh: int, stream: int):
+    """rot: a pw_rotation, or None."""
+    _check(_lib.pw_heads_norm_rotate(_rotation(rot), positions_ptr, offset, q_ptr, ldq, ldqh, n_q, k_ptr, ldk, ldkh, n_k,
+                                     q_weight_ptr, k_weight_ptr, norm, eps, T, head_dim, act, q_out_ptr, ldqo, ldqoh, k_out_ptr,
+                                     ldko, ldkoh, stream))
+
+
+def pw_kv_append_rotated(cache: pw_kv_cache, rot, positions_ptr: int, offset: int, q_ptr: int, ldq: int, ldqh: int, n_q: int,
+                         k_ptr: int, v_ptr: int, ld: int, ldh: int, q_weight_ptr: int, k_weight_ptr: int, norm: int, eps: float,
+                         slots_ptr: int, T: int, q_out_ptr: int, ldqo: int, ldqoh: int, stream: int):
+    """rot: a pw_rotation, or None."""
+    _check(_lib.pw_kv_append_rotated(ctypes.byref(cache), _rotation(rot), positions_ptr, offset, q_ptr, ldq, ldqh, n_q, k_ptr,
+                                     v_ptr, ld, ldh, q_weight_ptr, k_weight_ptr, norm, eps, slots_ptr, T, q_out_ptr, ldqo, ldqoh,
+                                     stream))
+
+
+def pw_kv_keep(cache: pw_kv_cache, starts_ptr: int, table_ptr: int, ld_table: int, lens_ptr: int, B: int, max_len: int,
+               chosen_ptr: int, words: int, new_lens_ptr: int, stream: int):
+    _check(_lib.pw_kv_keep(ctypes.byref(cache), starts_ptr, table_ptr, ld_table, lens_ptr, B, max_len, chosen_ptr, words,
+                           new_lens_ptr, stream))
+
+
+def pw_attn_rows_workspace(cache: pw_kv_cache, B: int, T: int, n_q_heads: int, max_len: int, window: int) -> int:
+    out = ctypes.c_size_t()
+    _check(_lib.pw_attn_rows_workspace(ctypes.byref(cache), B, T, n_q_heads, max_len, window, ctypes.byref(out)))
+    return out.value
+
+
+def pw_attn_rows(cache: pw_kv_cache, q_ptr: int, ldq: int, ldqh: int, n_q_heads: int, starts_ptr: int, T: int, masks_ptr: int,
+                 words: int, table_ptr: int, ld_table: int, lens_ptr: int, B: int, max_len: int, scale: float, window: int,
+                 out_ptr: int, lse_ptr: int, ws_ptr: int, ws_bytes: int, stream: int):
+    _check(_lib.pw_attn_rows(ctypes.byref(cache), q_ptr, ldq, ldqh, n_q_heads, starts_ptr, T, masks_ptr, words, table_ptr,
+                             ld_table, lens_ptr, B, max_len, scale, window, out_ptr, lse_ptr, ws_ptr, ws_bytes, stream))
 
 
 def pw_route_grouped(logits_ptr: int, logit_type: int, bias_ptr: int, T: int, E: int, K: int, score: int, n_groups: int,
