@@ -754,7 +754,10 @@ pw_status pw_kv_append_rotated(const pw_kv_cache* cache, const pw_rotation* rot,
  * has are not written. Rows that see nothing give zeros and an lse of -infinity.
  * What lies in the cache at positions that a row does not see is not used for it,
  * NaN and infinities included. Scores, exponentials and sums are in fp32; weights
- * enter the product with the values as in pw_attn_decode.
+ * enter the product with the values as in pw_attn_decode where T * (n_q_heads /
+ * n_kv_heads) <= 64 B, above that rounded once to 16 bits: to bf16 with bf16 and 8-bit
+ * caches, off by at most 2^-8 of themselves; with fp16 caches by at most 2^-11 and
+ * 2^-52 of the row's largest weight.
  * Constraints: B, T >= 0; n_q_heads a multiple of n_kv_heads; 1 <= words <= 1024;
  * 0 <= max_len < 2^31 - 256; window >= 0; scale finite (PW_EINVAL otherwise); B <
  * 65536, T * n_q_heads < 2^23, min(B, T) * n_kv_heads < 2^21 (PW_EUNSUPPORTED: split

@@ -107,18 +107,21 @@ struct RowsArgs {
   float scale;
   uint16_t* out;
   float* lse;
-  int n_splits, split_tiles;
-  float* part_o;           // [items][splits][columns][D], not normalised
+  int64_t whole;           // items that are not split, the first ones
+  int n_splits, split_tiles;   // of the others
+  float* part_o;           // [items from there on][splits][columns][D], not normalised
   float* part_ml;          // [the same][2]: maximum (base 2), sum
 };
 
 struct RowsPlan {
+  int many;                // waves with columns of their own, else tiles of their own
   int col_tiles;           // of a wave
   int n_splits, split_tiles;
-  int64_t items;           // at most
+  int64_t items, whole;    // at most; of them not split
   size_t slots;            // rows of head_dim + 2 floats of the workspace
 };
-RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int bits, int max_len, int window);
+RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int act, int bits, int max_len,
+                   int window);
 
 // A sequence's attended positions are cut into tiles of 32 tokens, at multiples
 // of 32.

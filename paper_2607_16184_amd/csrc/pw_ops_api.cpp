@@ -362,7 +362,7 @@ pw_status pw_attn_rows_workspace(const pw_kv_cache* c, int B, int T, int n_q_hea
   if (T < 0) return set_error(PW_EINVAL, "need T >= 0");
   if (!ws_bytes) return set_error(PW_EINVAL, "null argument");
   if (rows_too_many(c, B, T, n_q_heads)) return set_error(PW_EUNSUPPORTED, kTooManyRows);
-  *ws_bytes = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window).slots * (c->head_dim + 2) * 4;
+  *ws_bytes = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->act, c->bits, max_len, window).slots * (c->head_dim + 2) * 4;
   return PW_OK;
 }
 
@@ -384,7 +384,7 @@ pw_status pw_attn_rows(const pw_kv_cache* c, const void* q, int64_t ldq, int64_t
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(masks, 8) || !aligned(starts, 4) || !aligned(block_table, 4) ||
       !aligned(seq_lens, 4) || !aligned(lse, 4))
     return set_error(PW_EINVAL, "q and out must be 16-byte aligned, masks 8-byte, the other buffers 4-byte");
-  const pw::RowsPlan p = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->bits, max_len, window);
+  const pw::RowsPlan p = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->act, c->bits, max_len, window);
   const size_t need = p.slots * (c->head_dim + 2) * sizeof(float);
   if (need && (!ws || ws_bytes < need)) return set_error(PW_ENOMEM, "workspace too small (pw_attn_rows_workspace)");
   if (need && !aligned(ws, 16)) return set_error(PW_EINVAL, "the workspace must be 16-byte aligned");
@@ -407,6 +407,7 @@ pw_status pw_attn_rows(const pw_kv_cache* c, const void* q, int64_t ldq, int64_t
   a.scale = scale;
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
+  a.whole = p.whole;
   a.n_splits = p.n_splits;
   a.split_tiles = p.split_tiles;
   a.part_o = static_cast<float*>(ws);

@@ -1,6 +1,7 @@
 // Attention of several new tokens per sequence over the paged KV cache, gfx950:
 // trees of drafted tokens and prompt chunks (k_attn_rows, k_rows_join).
 #include "pw_kv.hpp"
+#include "pw_lds.hpp"
 
 namespace pw {
 namespace {
@@ -54,7 +55,8 @@ __device__ __forceinline__ bool item_at(const RowsArgs& a, int64_t item, int h, 
       it->h = h;
       it->row0 = __builtin_amdgcn_readlane(row0, l);
       it->n = __builtin_amdgcn_readlane(n, l);
-      const int64_t group = item - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(groups, l));
+      // the last rows first: of a prompt's chunk they have the longest spans
+      const int64_t group = before + __builtin_amdgcn_readlane(upto, l) - 1 - item;
       if (group < 0 || group * cols >= static_cast<int64_t>(it->n) * g) return false;
       it->col0 = static_cast<int>(group) * cols;
       it->n_col = min(cols, it->n * g - it->col0);
@@ -520,18 +522,404 @@ __global__ __launch_bounds__(64 * kRowsWaves, rows_two_waves(BITS, D, C) ? 2 : 1
   attend_rows<ACT, BITS, D, C>(a, lds, it, begin, end, n_act <= 1, (item * a.kv.n_kv_heads + h) * a.n_splits + split);
 }
 
+// ---------------------------------------------------------------------------
+// Many columns
+// ---------------------------------------------------------------------------
+//
+// A workgroup's four waves have columns of their own, C x 16 each, and share the
+// tiles: those come into LDS by direct loads, kStages - 1 tiles ahead, in the order
+// in which they lie in the cache, which is the one that the matrix instructions take
+// them in: 1 KB per instruction, without bank conflicts.
+
+constexpr int kStages = 3;
+template <int BITS, int D>
+constexpr int stage_bytes() { return 64 * D * BITS / 8 + (BITS == 8 ? 256 : 0); }
+
+template <int ACT, int BITS, int D, int C>
+__device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, const Item& it, int begin, int end, bool whole,
+                                             int64_t slot) {
+  constexpr int kPv = BITS == 8 ? PW_BF16 : ACT;
+  constexpr bool kByTile = kPv == PW_F16;
+  constexpr int kLoads = D * BITS / 8 * 16 / 1024;    // 1 KB pieces of 16 tokens' keys
+  constexpr int kMine = kLoads + (BITS == 8 ? 1 : 0); // loads of a wave for a tile: a quarter of the pieces, the scales
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
+  const int col = lane & 15, lg = lane >> 4;
+  const int P = a.kv.block_tokens, h = it.h;
+  const int g = a.n_q_heads / a.kv.n_kv_heads;
+  const int my0 = 16 * C * wave;                                 // the wave's first column
+  const bool busy = my0 < it.n_col;
+  const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;       // queries of the other sign: maxima stay maxima
+  const float scale2 = fabsf(a.scale) * kLog2e;
+
+  Column x[C];
+  u32x4 q[C][D / 32];
+  int all_lo = 0, all_hi = INT32_MAX;                            // all columns of the wave see [all_lo, all_hi)
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int cc = my0 + 16 * c + col;
+    x[c] = column_at(a, it, cc, g);
+    if (x[c].row >= 0) {
+      all_lo = max(all_lo, x[c].lo);
+      all_hi = min(all_hi, x[c].hi);
+    }
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      q[c][i] = u32x4{0u, 0u, 0u, 0u};
+      if (x[c].row >= 0)
+        q[c][i] = ld16(reinterpret_cast<const uint8_t*>(a.q + static_cast<int64_t>(x[c].row) * a.ldq +
+                                                        (h * g + (it.col0 + cc) % g) * a.ldqh + 32 * i + 8 * lg));
+#pragma unroll
+      for (int w = 0; w < 4; ++w) q[c][i][w] ^= flip;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    all_lo = max(all_lo, __shfl_xor(all_lo, o));
+    all_hi = min(all_hi, __shfl_xor(all_hi, o));
+  }
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+
+  // tiles in blocks of the pool, in order; the same for all waves
+  const int n_my = end - begin;
+  const auto block_of = [&](int i) {
+    if (i >= n_my) return -1;
+    const int64_t t = static_cast<int64_t>(it.t0 + begin + i) * kTile;
+    return static_cast<int>(a.table[it.b * a.ld_table + (t >> __builtin_ctz(P))]);
+  };
+  int ids = block_of(lane), chunk = 0;
+  uint64_t todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
+  const size_t head_off = static_cast<size_t>(2 * h) * P * D * (BITS / 8);
+  const size_t v_off = static_cast<size_t>(P) * D * (BITS / 8);
+  const size_t sc_off = static_cast<size_t>(2) * a.kv.n_kv_heads * P * D + static_cast<size_t>(h) * P * 4;
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_u8_t)lds));
+  const uint32_t sc_lane = (lane & 31) * 4 + (lane >= 32 ? static_cast<uint32_t>(a.kv.n_kv_heads) * P * 4 : 0u);
+  // the next tile's loads into a stage; its first token, -1 where there is none
+  const auto fetch = [&](int stage) {
+    while (todo == 0 && chunk + 64 < n_my) {
+      chunk += 64;
+      ids = block_of(chunk + lane);
+      todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
+    }
+    if (todo == 0) return -1;
+    const int l = __ffsll(static_cast<long long>(todo)) - 1;
+    todo &= todo - 1;
+    const int id = __builtin_amdgcn_readlane(ids, l);
+    const int t = (it.t0 + begin + chunk + l) * kTile;
+    const uint8_t* blk = a.kv.pool + static_cast<int64_t>(id) * a.kv.block_stride;
+    const uint8_t* src = uniform_ptr(blk + head_off + static_cast<size_t>(t & (P - 1)) * D * (BITS / 8));
+    const uint32_t dst = lds0 + stage * stage_bytes<BITS, D>();
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int piece = 4 * i + wave;                            // the keys' 2 kLoads, then the values'
+      const bool is_v = piece >= 2 * kLoads;
+      lds_load16(dst + piece * 1024, 16 * lane, uniform_ptr(src + (is_v ? v_off : 0) + (piece - (is_v ? 2 * kLoads : 0)) * 1024));
+    }
+    if constexpr (BITS == 8)                                     // (each wave the same ones)
+      lds_load4(dst + 4 * kLoads * 1024, sc_lane, uniform_ptr(blk + sc_off + 4 * (t & (P - 1))));
+    return t;
+  };
+
+  f32x4 o[C][D / 16];
+  float m[C], l[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) o[c][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    m[c] = kNoMax;
+    l[c] = 0.0f;
+  }
+  int t = fetch(0), t1 = t < 0 ? -1 : fetch(1);
+  int stage = 0;
+  while (t >= 0) {
+    if (t1 >= 0) wait_vm<kMine>();
+    else wait_vm<0>();
+    wg_barrier();                                                // the stage is there, the one before it is read
+    const int t2 = t1 < 0 ? -1 : fetch(stage >= 1 ? stage - 1 : kStages - 1);
+    if (busy) {
+      const uint8_t* sk = lds + stage * stage_bytes<BITS, D>() + 16 * lane;
+      const uint8_t* sv = sk + 2 * kLoads * 1024;
+      const float* sc = reinterpret_cast<const float*>(lds + stage * stage_bytes<BITS, D>() + 4 * kLoads * 1024) + 4 * lg;
+      f32x4 s[C][2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) s[c][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          const u32x4 kk = ld16(sk + (r * kLoads + j) * 1024);
+          if constexpr (BITS == 16) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(kk, q[c][j], s[c][r]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const u32x4 w = widen8<ACT>(kk[2 * e], kk[2 * e + 1]);
+#pragma unroll
+              for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(w, q[c][2 * j + e], s[c][r]);
+            }
+          }
+        }
+      }
+      f32x4 vs[2];
+      if constexpr (BITS == 8) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 16 * r);
+          vs[r] = *reinterpret_cast<const f32x4*>(sc + 32 + 16 * r);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float f = scale2 * ks[e];
+#pragma unroll
+            for (int c = 0; c < C; ++c) s[c][r][e] *= f;
+          }
+        }
+      }
+      const bool part = t < all_lo || t + kTile > all_hi;        // some column does not see all of it
+      uint32_t seen[C];
+      float mul = BITS == 8 ? 1.0f : scale2;                     // of the scores as they are
+      if (part) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          seen[c] = seen_of(a, it, x[c], t) >> (4 * lg);
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[c][r][e] = (seen[c] >> (16 * r + e)) & 1u ? s[c][r][e] * mul : -INFINITY;
+        }
+        mul = 1.0f;
+      }
+      u32x4 p_hi[C];
+      float share[C], base[C], top[C];
+      bool low = false;                                          // fp16: weights that one term does not hold
+      bool raise = false;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        top[c] = s[c][0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top[c] = fmaxf(top[c], s[c][e / 4][e & 3]);
+        top[c] *= mul;
+        if constexpr (kByTile) {
+          top[c] = fmaxf(column_max(top[c]), kNoMax);
+          raise |= top[c] > m[c];
+        } else {
+          raise |= top[c] > m[c] + kSlack;
+        }
+      }
+      if (__any(raise)) {                                        // (all columns at once: what follows is one piece)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const float m_new = fmaxf(m[c], kByTile ? top[c] : column_max(top[c]));
+          const float f = __builtin_amdgcn_exp2f(m[c] - m_new);
+          m[c] = m_new;
+          l[c] *= f;
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][j][e] *= f;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        base[c] = kByTile ? top[c] : m[c];
+        share[c] = kByTile ? __builtin_amdgcn_exp2f(top[c] - m[c]) : 1.0f;
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          float p[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = w / 2, y = 2 * (w & 1) + e;
+            p[e] = __builtin_amdgcn_exp2f(fmaf(s[c][r][y], mul, -base[c]));
+            sum += p[e];
+            if constexpr (BITS == 8) {
+              p[e] *= vs[r][y];
+              if (part) p[e] = (seen[c] >> (16 * r + y)) & 1u ? p[e] : 0.0f;
+            }
+            if constexpr (kByTile) {
+              p[e] *= kLift;
+              low |= p[e] < 0x1p-14f;
+              s[c][r][y] = p[e];
+            }
+          }
+          p_hi[c][w] = pack16<kPv>(p[0], p[1]);
+        }
+        l[c] = fmaf(share[c], sum, l[c]);
+        if constexpr (kByTile) share[c] *= 1.0f / kLift;
+      }
+      uint32_t keep[2][2], any = 0u;
+      if (part) {
+        // values that no column may see are left out, whatever their bits, and those
+        // that are no numbers for now
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          keep[r][0] = keep[r][1] = 0u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = t + 16 * r + 4 * lg + e;
+            const bool in = tok >= it.lo && tok < it.hi;
+            if constexpr (BITS == 8) keep[r][0] |= in ? 0xFFu << (8 * e) : 0u;
+            else keep[r][e / 2] |= in ? 0xFFFFu << (16 * (e & 1)) : 0u;
+          }
+        }
+      }
+      const auto values = [&](int j) {                           // the 1 KB piece j of the values
+        u32x4 v = ld16(sv + j * 1024);
+        if (part) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            v[w] &= BITS == 8 ? keep[w & 1][0] : keep[w / 2][w & 1];
+            const uint32_t z = odd_parts<BITS, kPv>(v[w]);
+            any |= z;
+            v[w] &= ~z;
+          }
+        }
+        return v;
+      };
+      if constexpr (kByTile) {
+        const bool two = __any(low);
+        u32x4 p_lo[C];
+        if (two) {
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              p_lo[c][w] = pack16<kPv>((s[c][w / 2][2 * (w & 1)] - val16(p_hi[c][w] & 0xFFFFu, kPv)) * kLow,
+                                       (s[c][w / 2][2 * (w & 1) + 1] - val16(p_hi[c][w] >> 16, kPv)) * kLow);
+        }
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          const u32x4 v = values(j);
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+            f32x4 hi = mma<kPv>(v, p_hi[c], zero);
+            if (two) {
+              const f32x4 lo = mma<kPv>(v, p_lo[c], zero);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) hi[e] = fabsf(hi[e]) < INFINITY ? fmaf(lo[e], 1.0f / kLow, hi[e]) : hi[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][j][e] = fmaf(share[c], hi[e], o[c][j][e]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2 * kLoads; ++j) {
+          const u32x4 v = values(j);
+          if constexpr (BITS == 16) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c][j] = mma<kPv>(v, p_hi[c], o[c][j]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const u32x4 w = widen8<kPv>(v[2 * e], v[2 * e + 1]);
+#pragma unroll
+              for (int c = 0; c < C; ++c) o[c][2 * j + e] = mma<kPv>(w, p_hi[c], o[c][2 * j + e]);
+            }
+          }
+        }
+      }
+      if (part && __any(any != 0u)) {
+        // one by one, to the columns that see them
+        const uint8_t* vm = lds + stage * stage_bytes<BITS, D>() + 2 * kLoads * 1024;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          for (int i = 0; i < kTile; ++i) {
+            uint32_t w = p_hi[c][0];
+            const int at = 2 * (i / 16) + i % 4 / 2;             // token i's word in lanes 16 (i / 4 mod 4) ..
+#pragma unroll
+            for (int e = 1; e < 4; ++e) w = at == e ? p_hi[c][e] : w;
+            w = static_cast<uint32_t>(__shfl(static_cast<int>(w), 16 * (i / 4 % 4) + col));
+            const uint32_t on = static_cast<uint32_t>(__shfl(static_cast<int>(seen[c]), col)) >> i & 1u;   // (bits of lane group 0: all)
+            const float p = val16(w >> (16 * (i & 1)), kPv) * share[c];
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int place = 16 * (16 * (i / 4 % 4) + 4 * lg + e);
+                float y = 0.0f;
+                if constexpr (BITS == 16) {
+                  const uint32_t b = *reinterpret_cast<const any_u16*>(vm + j * 1024 + place + 2 * (4 * (i / 16) + i % 4));
+                  if (odd_parts<16, kPv>(b) & 0xFFFFu) y = val16(b, kPv);
+                } else {
+                  const uint32_t b = vm[(j / 2) * 1024 + place + 8 * (j & 1) + 4 * (i / 16) + i % 4];
+                  if ((b & 0x7Fu) == 0x7Fu) y = __builtin_nanf("");
+                }
+                if (on && y != 0.0f) o[c][j][e] = fmaf(p, y, o[c][j][e]);
+              }
+          }
+        }
+      }
+    }
+    t = t1;
+    t1 = t2;
+    stage = stage + 1 < kStages ? stage + 1 : 0;
+  }
+  if (!busy) return;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    float sum = l[c];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    const int cc = my0 + 16 * c + col;
+    if (cc >= it.n_col) continue;
+    if (whole) {
+      const int64_t at = static_cast<int64_t>(x[c].row) * a.n_q_heads + h * g + (it.col0 + cc) % g;
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+        *reinterpret_cast<u32x2*>(a.out + at * D + 16 * j + 4 * lg) =
+            u32x2{pack16<ACT>(o[c][j][0] * inv, o[c][j][1] * inv), pack16<ACT>(o[c][j][2] * inv, o[c][j][3] * inv)};
+      if (a.lse && lg == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (m[c] + log2f(sum)) * kLn2;
+    } else {
+      // (the lanes of a column may hold different maxima only where it has seen nothing)
+      const int64_t at = slot * (64 * C) + cc;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) *reinterpret_cast<f32x4*>(a.part_o + at * D + 16 * j + 4 * lg) = o[c][j];
+      if (lg == 0) {
+        a.part_ml[2 * at] = m[c];
+        a.part_ml[2 * at + 1] = sum;
+      }
+    }
+  }
+}
+
+// Workgroups of k_attn_tiles on a CU, by its registers (fp16 caches: more of them)
+// and LDS.
+constexpr int tiles_resident(int act, int bits, int D) {
+  return D <= 64 ? 4 : D <= 128 ? (act == PW_F16 && bits == 16 ? 2 : 3) : D <= 192 ? 2 : 1;
+}
+
+template <int ACT, int BITS, int D, int C>
+__global__ __launch_bounds__(256, tiles_resident(ACT, BITS, D)) void k_attn_tiles(RowsArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * stage_bytes<BITS, D>()];
+  const int h = blockIdx.x % a.kv.n_kv_heads;
+  const int64_t rest = blockIdx.x / a.kv.n_kv_heads;
+  const bool all = rest < a.whole;                               // the first items are not split
+  const int split = all ? 0 : static_cast<int>((rest - a.whole) % a.n_splits);
+  const int64_t item = all ? rest : a.whole + (rest - a.whole) / a.n_splits;
+  Item it;
+  if (!item_at(a, item, h, 64 * C, lane_id(), &it)) return;
+  const int per = all ? it.tiles : a.split_tiles, n_act = all ? 1 : (it.tiles + per - 1) / per;
+  if (split > 0 && split >= n_act) return;
+  const int begin = split * per, end = min(begin + per, it.tiles);
+  attend_tiles<ACT, BITS, D, C>(a, lds, it, begin, end, n_act <= 1,
+                                ((item - a.whole) * a.kv.n_kv_heads + h) * a.n_splits + split);
+}
+
 // Joins the parts of four columns of an item, a wave for each, in a fixed order.
 template <int ACT, int D>
 __global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols) {
   constexpr int kC = D / 64;
   const int lane = lane_id(), c = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int h = blockIdx.x % a.kv.n_kv_heads;
-  const int64_t item = blockIdx.x / a.kv.n_kv_heads;
+  const int64_t item = a.whole + blockIdx.x / a.kv.n_kv_heads;
   Item it;
   if (!item_at(a, item, h, cols, lane, &it) || c >= it.n_col) return;
   const int n = (it.tiles + a.split_tiles - 1) / a.split_tiles;
   if (n <= 1) return;
-  const int64_t at = (item * a.kv.n_kv_heads + h) * a.n_splits * cols + c;
+  const int64_t at = ((item - a.whole) * a.kv.n_kv_heads + h) * a.n_splits * cols + c;
   float mx = kNoMax;
   for (int s = lane; s < n; s += 64) mx = fmaxf(mx, a.part_ml[2 * (at + static_cast<int64_t>(s) * cols)]);
 #pragma unroll
@@ -553,18 +941,21 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols) {
   if (a.lse && lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
 }
 
+constexpr int kTileCols = 2;          // column tiles of a wave of k_attn_tiles
+
 template <int ACT, int BITS, int D>
 hipError_t launch_d(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
-  const int64_t grid = p.items * a.kv.n_kv_heads * p.n_splits;
+  const int64_t grid = (p.whole + (p.items - p.whole) * p.n_splits) * a.kv.n_kv_heads;
   if (grid >= (1 << 23)) return hipErrorInvalidConfiguration;
   const uint32_t n = static_cast<uint32_t>(grid);
-  if (p.col_tiles == 1) k_attn_rows<ACT, BITS, D, 1><<<n, 64 * kRowsWaves, 0, st>>>(a);
+  if (p.many) k_attn_tiles<ACT, BITS, D, kTileCols><<<n, 256, 0, st>>>(a);
+  else if (p.col_tiles == 1) k_attn_rows<ACT, BITS, D, 1><<<n, 64 * kRowsWaves, 0, st>>>(a);
   else if (D > 128 || p.col_tiles == 2) k_attn_rows<ACT, BITS, D, 2><<<n, 64 * kRowsWaves, 0, st>>>(a);
   else if constexpr (D <= 128) k_attn_rows<ACT, BITS, D, 4><<<n, 64 * kRowsWaves, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.n_splits == 1) return e;
-  const int cols = 16 * p.col_tiles;
-  k_rows_join<ACT, D><<<dim3(static_cast<uint32_t>(p.items * a.kv.n_kv_heads), cols / 4), 256, 0, st>>>(a, cols);
+  if (e != hipSuccess || p.slots == 0) return e;
+  const int cols = (p.many ? 64 : 16) * p.col_tiles;
+  k_rows_join<ACT, D><<<dim3(static_cast<uint32_t>((p.items - p.whole) * a.kv.n_kv_heads), cols / 4), 256, 0, st>>>(a, cols);
   return hipGetLastError();
 }
 
@@ -581,12 +972,13 @@ hipError_t launch_bits(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
 
 }  // namespace
 
-RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int bits, int max_len, int window) {
-  RowsPlan p{1, 1, 1, 0, 0};
+RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int act, int bits, int max_len, int window) {
+  RowsPlan p{0, 1, 1, 1, 0, 0, 0};
   if (B == 0 || T == 0) return p;
-  const int64_t g = n_q_heads / n_kv_heads, cols = g * ((static_cast<int64_t>(T) + B - 1) / B);
-  p.col_tiles = cols <= 16 ? 1 : cols <= 32 || head_dim > 128 ? 2 : 4;
-  const int64_t group = 16 * p.col_tiles;
+  const int64_t g = n_q_heads / n_kv_heads, rows = (static_cast<int64_t>(T) + B - 1) / B, cols = g * rows;
+  p.many = g * T > 64 * static_cast<int64_t>(B);
+  p.col_tiles = p.many ? kTileCols : cols <= 16 ? 1 : cols <= 32 || head_dim > 128 ? 2 : 4;
+  const int64_t group = (p.many ? 64 : 16) * p.col_tiles;
   p.items = g * T / group + (B < T ? B : T);
   int64_t tiles = (static_cast<int64_t>(max_len) + kTile - 1) / kTile;
   if (window > 0) {
@@ -594,13 +986,42 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
     tiles = w < tiles ? w : tiles;
   }
   if (tiles == 0) tiles = 1;
-  const int64_t most = (tiles + 31) / 32, want = (1024 + p.items * n_kv_heads - 1) / (p.items * n_kv_heads);
-  int64_t n = want < most ? want : most;
+  const int64_t items = p.items * n_kv_heads;
+  int64_t n = 1;
+  if (p.many) {
+    const int64_t resident = 256 * tiles_resident(act, bits, head_dim);
+    const double unit = 0.5 * tiles_resident(act, bits, head_dim) * head_dim / 128;   // us a tile
+    const double part = 128.0 * (head_dim + 2) * 8 / 4e6;        // us to write and read a part
+    const int64_t tri = rows / kTile < tiles ? rows / kTile : tiles;
+    double best = 0.0;
+    for (int64_t k = 1; k <= 32 && (k == 1 || tiles / k >= 8); ++k)
+      for (int64_t whole = 0; whole <= (k > 1 && tri < tiles / 4 ? items / resident : 0); whole += items / resident > 0 ? items / resident : 1) {
+        const int64_t left = items - whole * resident;
+        if (left < 0) continue;
+        const int64_t rounds = (left * k + resident - 1) / resident;
+        double t = static_cast<double>(whole) * (tiles + 3) + rounds * (static_cast<double>(tiles) / k + 3);
+        if (tri >= tiles / 4) {
+          const double mean = (tiles - 0.5 * tri) * items / resident, longest = static_cast<double>(tiles) / k;
+          t = (mean > longest ? mean : longest) + 3 * rounds;
+        }
+        t *= unit;
+        if (k > 1) t += 5.0 + left * k * part;
+        if (best == 0.0 || t < best) {
+          best = t;
+          n = k;
+          p.whole = whole * resident / n_kv_heads;
+        }
+      }
+    if (n == 1) p.whole = 0;
+  } else {
+    const int64_t most = (tiles + 31) / 32, want = (1024 + items - 1) / items;
+    n = want < most ? want : most;
+  }
   const int64_t per = ((tiles + n - 1) / n + kRowsWaves - 1) / kRowsWaves * kRowsWaves;
   n = (tiles + per - 1) / per;
   p.n_splits = static_cast<int>(n);
   p.split_tiles = static_cast<int>(per);
-  if (n > 1) p.slots = static_cast<size_t>(p.items * n_kv_heads * n) * group;
+  if (n > 1) p.slots = static_cast<size_t>((p.items - p.whole) * n_kv_heads * n) * group;
   return p;
 }
 

@@ -7,7 +7,7 @@ import torch
 import ops_ref as R
 import rows_ref as RR
 from test_gpu_ops import BF, FP, _cache, _gen, _ops, _same, _within
-from test_gpu_rows import _bound, _tree
+from test_gpu_rows import _bound, _once, _tree
 
 pytestmark = pytest.mark.gpu
 
@@ -118,7 +118,7 @@ def test_a_drafting_loop(act, bits):
             # keys of 16-bit caches as the definition rounds them: a code that lies
             # beside it is one step off
             step = R.U[act] if bits == 16 else 2 * R.U[R.F8]
-            ds, bound = _bound(act, D, len(k64), size, o, mass)
+            ds, bound = _bound(act, D, len(k64), size, o, mass, _once(len(out), B, n_q // H, act, bits))
             _within(out[at:at + n], o, bound + (2 * step * size[..., None] + step) * mass, "sequence %d" % b)
             at += n
 
