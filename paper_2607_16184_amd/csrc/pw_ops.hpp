@@ -107,18 +107,23 @@ struct RowsArgs {
   float scale;
   uint16_t* out;
   float* lse;
-  int64_t whole;           // items that are not split, the first ones
+  uint32_t over_g;         // floor(2^32 / g), for g = 1 the largest number
+  int64_t whole;           // splits: items that are not split, the first ones
   int n_splits, split_tiles;   // of the others
-  float* part_o;           // [items from there on][splits][columns][D], not normalised
+  int n_shares, least;     // shares per key head (0: splits), tiles of one at least
+  int64_t items;           // at most
+  float* part_o;           // [key heads][shares + items][columns][D], not normalised
   float* part_ml;          // [the same][2]: maximum (base 2), sum
+  int32_t* meta;           // [key heads][items][2]: first slot, parts
 };
 
 struct RowsPlan {
   int many;                // waves with columns of their own, else tiles of their own
   int col_tiles;           // of a wave
-  int n_splits, split_tiles;
-  int64_t items, whole;    // at most; of them not split
-  size_t slots;            // rows of head_dim + 2 floats of the workspace
+  int64_t items, whole, n_shares;
+  int n_splits, split_tiles, least;
+  int64_t slots;           // rows of head_dim + 2 floats of the workspace
+  size_t ws_bytes;
 };
 RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int act, int bits, int max_len,
                    int window);

@@ -362,7 +362,7 @@ pw_status pw_attn_rows_workspace(const pw_kv_cache* c, int B, int T, int n_q_hea
   if (T < 0) return set_error(PW_EINVAL, "need T >= 0");
   if (!ws_bytes) return set_error(PW_EINVAL, "null argument");
   if (rows_too_many(c, B, T, n_q_heads)) return set_error(PW_EUNSUPPORTED, kTooManyRows);
-  *ws_bytes = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->act, c->bits, max_len, window).slots * (c->head_dim + 2) * 4;
+  *ws_bytes = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->act, c->bits, max_len, window).ws_bytes;
   return PW_OK;
 }
 
@@ -385,7 +385,7 @@ pw_status pw_attn_rows(const pw_kv_cache* c, const void* q, int64_t ldq, int64_t
       !aligned(seq_lens, 4) || !aligned(lse, 4))
     return set_error(PW_EINVAL, "q and out must be 16-byte aligned, masks 8-byte, the other buffers 4-byte");
   const pw::RowsPlan p = pw::rows_plan(B, T, n_q_heads, c->n_kv_heads, c->head_dim, c->act, c->bits, max_len, window);
-  const size_t need = p.slots * (c->head_dim + 2) * sizeof(float);
+  const size_t need = p.ws_bytes;
   if (need && (!ws || ws_bytes < need)) return set_error(PW_ENOMEM, "workspace too small (pw_attn_rows_workspace)");
   if (need && !aligned(ws, 16)) return set_error(PW_EINVAL, "the workspace must be 16-byte aligned");
   pw::RowsArgs a{};
@@ -407,11 +407,17 @@ pw_status pw_attn_rows(const pw_kv_cache* c, const void* q, int64_t ldq, int64_t
   a.scale = scale;
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
+  const uint32_t g = static_cast<uint32_t>(n_q_heads / c->n_kv_heads);
+  a.over_g = g == 1 ? UINT32_MAX : static_cast<uint32_t>((uint64_t(1) << 32) / g);
   a.whole = p.whole;
   a.n_splits = p.n_splits;
   a.split_tiles = p.split_tiles;
+  a.n_shares = static_cast<int>(p.n_shares);
+  a.least = p.least;
+  a.items = p.items;
   a.part_o = static_cast<float*>(ws);
   a.part_ml = a.part_o + p.slots * c->head_dim;
+  a.meta = reinterpret_cast<int32_t*>(a.part_ml + 2 * p.slots);
   return launched(pw::launch_attn_rows(a, p, static_cast<hipStream_t>(stream)), "attention launch");
 }
 

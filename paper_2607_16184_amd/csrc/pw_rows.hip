@@ -28,55 +28,186 @@ __device__ __forceinline__ int clamp64(int64_t v, int lo, int hi) {
   return static_cast<int>(v < lo ? lo : v > hi ? hi : v);
 }
 
-// The item's sequence, columns and span; false past the last one. (Starts that are
-// not in order give other items, never rows outside 0 .. T - 1.)
+// How the work is cut.
+//   splits (a.n_shares 0): the first a.whole items go to a workgroup each, the others to
+//     a.n_splits, each of which takes a.split_tiles tiles of the item. Workgroups that
+//     run together then read the same tiles for other columns, from the L2.
+//   shares: each head's items form a line of tiles, cut into equal shares, one per
+//     workgroup, wherever the items end: sequences of unlike lengths leave no workgroup
+//     with more than another. Workgroups that run together read other tiles, so this
+//     is for sequences of few groups of columns.
+// A part of an item that is not all of it goes to a slot of the workspace: split s of
+// item i to slot (i - whole) n_splits + s, share s's part of item i to slot s + i (one
+// of the two grows from part to part); k_rows_join adds them up. Lengths are read on
+// the device, and nothing else decides.
+
+// Sequence b's rows; none outside 0 .. T - 1, whatever the starts are.
+__device__ __forceinline__ void rows_of(const RowsArgs& a, int b, int* row0, int* n) {
+  *row0 = clampi(a.starts[b], 0, a.T);
+  *n = clampi(a.starts[b + 1], *row0, a.T) - *row0;
+}
+// x / g for 0 <= x < 2^31 by the reciprocal m = floor(2^32 / g), which gives it or one
+// less.
+__device__ __forceinline__ int over(int x, int g, uint32_t m) {
+  const int q = static_cast<int>(__umulhi(static_cast<uint32_t>(x), m));
+  return x - q * g >= g ? q + 1 : q;
+}
+// Group gi of a sequence's columns.
+__device__ __forceinline__ Item item_of(const RowsArgs& a, int b, int h, int row0, int n, int64_t len, int gi, int cols, int g) {
+  Item it;
+  it.b = b;
+  it.h = h;
+  it.row0 = row0;
+  it.n = n;
+  it.col0 = gi * cols;
+  it.n_col = min(cols, n * g - it.col0);
+  it.ctx = clamp64(len - n, -(1 << 30), INT32_MAX);
+  if (a.masks) {
+    it.hi = clamp64(len, 0, a.max_len);
+    it.lo = a.window ? clamp64(static_cast<int64_t>(it.ctx) - a.window, 0, it.hi) : 0;
+  } else {
+    const int first = over(it.col0, g, a.over_g), last = over(it.col0 + it.n_col - 1, g, a.over_g);
+    it.hi = clamp64(static_cast<int64_t>(it.ctx) + last + 1, 0, a.max_len);
+    it.lo = a.window ? clamp64(static_cast<int64_t>(it.ctx) + first + 1 - a.window, 0, it.hi) : 0;
+  }
+  it.t0 = it.lo / kTile;
+  it.tiles = it.hi > it.lo ? (it.hi + kTile - 1) / kTile - it.t0 : 0;
+  return it;
+}
+__device__ __forceinline__ int scan64(int x, int lane) {         // sums of the lanes up to this one
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+// Item `item` in the order of sequences and groups; false past the last one.
 __device__ __forceinline__ bool item_at(const RowsArgs& a, int64_t item, int h, int cols, int lane, Item* it) {
   const int g = a.n_q_heads / a.kv.n_kv_heads;
   int64_t before = 0;
   for (int base = 0; base < a.B; base += 64) {
-    const int b = base + lane;
     int row0 = 0, n = 0;
-    if (b < a.B) {
-      row0 = clampi(a.starts[b], 0, a.T);
-      n = clampi(a.starts[b + 1], row0, a.T) - row0;
-    }
-    const int groups = (n * g + cols - 1) / cols;
-    int upto = groups;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(upto, o);
-      if (lane >= o) upto += x;
-    }
+    if (base + lane < a.B) rows_of(a, base + lane, &row0, &n);
+    const int groups = (n * g + cols - 1) / cols, upto = scan64(groups, lane);
     const int all = __builtin_amdgcn_readlane(upto, 63);
     if (item < before + all) {
       const int l = __ffsll(static_cast<long long>(__ballot(before + upto > item))) - 1;
       if (l < 0) return false;
-      it->b = base + l;
-      it->h = h;
-      it->row0 = __builtin_amdgcn_readlane(row0, l);
-      it->n = __builtin_amdgcn_readlane(n, l);
-      // the last rows first: of a prompt's chunk they have the longest spans
-      const int64_t group = before + __builtin_amdgcn_readlane(upto, l) - 1 - item;
-      if (group < 0 || group * cols >= static_cast<int64_t>(it->n) * g) return false;
-      it->col0 = static_cast<int>(group) * cols;
-      it->n_col = min(cols, it->n * g - it->col0);
-      const int64_t len = a.lens[it->b];
-      it->ctx = clamp64(len - it->n, -(1 << 30), INT32_MAX);
-      const int first = it->col0 / g, last = (it->col0 + it->n_col - 1) / g;
-      if (a.masks) {
-        it->hi = clamp64(len, 0, a.max_len);
-        it->lo = a.window ? clamp64(static_cast<int64_t>(it->ctx) - a.window, 0, it->hi) : 0;
-      } else {
-        it->hi = clamp64(static_cast<int64_t>(it->ctx) + last + 1, 0, a.max_len);
-        it->lo = a.window ? clamp64(static_cast<int64_t>(it->ctx) + first + 1 - a.window, 0, it->hi) : 0;
-      }
-      it->t0 = it->lo / kTile;
-      it->tiles = it->hi > it->lo ? (it->hi + kTile - 1) / kTile - it->t0 : 0;
+      n = __builtin_amdgcn_readlane(n, l);
+      const int64_t gi = item - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(groups, l));
+      if (gi < 0 || gi * cols >= static_cast<int64_t>(n) * g) return false;
+      *it = item_of(a, base + l, h, __builtin_amdgcn_readlane(row0, l), n, a.lens[base + l], static_cast<int>(gi), cols, g);
       return true;
     }
     before += all;
   }
   return false;
+}
+// Tiles of a sequence's items.
+__device__ __forceinline__ int tiles_of(const RowsArgs& a, int row0, int n, int64_t len, int cols, int g) {
+  const int groups = (n * g + cols - 1) / cols;
+  int sum = 0;
+  if (a.masks && groups > 0) return groups * item_of(a, 0, 0, row0, n, len, 0, cols, g).tiles;   // one span for all
+  for (int gi = 0; gi < groups; ++gi) sum += item_of(a, 0, 0, row0, n, len, gi, cols, g).tiles;
+  return sum;
+}
+
+// The workgroup's items, or parts of them, one after the other.
+struct Walk {
+  int pos, stop;           // its tiles of the line, from the next part on
+  int start, index;        // of the item that `pos` lies in: first tile, number
+  int b, gi, r;            // its sequence and group; tiles of a share
+};
+struct Part {
+  int begin, end;          // tiles of the item's span
+  bool whole;
+  int64_t slot;
+};
+// The workgroup's split of an item; false where there is none.
+__device__ __forceinline__ bool split_of(const RowsArgs& a, int cols, int lane, Item* it, Part* p) {
+  const int H = a.kv.n_kv_heads, h = blockIdx.x % H, w = blockIdx.x / H;
+  const bool all = w < a.whole;
+  const int rest = static_cast<int>(a.items - a.whole), y = w - static_cast<int>(a.whole);
+  const int split = all ? 0 : y / rest, item = all ? w : static_cast<int>(a.whole) + y % rest;
+  // (the last rows first: of a prompt's chunk they have the longest spans)
+  if (!item_at(a, a.items - 1 - item, h, cols, lane, it)) return false;
+  const int per = all ? max(it->tiles, 1) : a.split_tiles, n_act = (it->tiles + per - 1) / per;
+  if (split > 0 && split >= n_act) return false;
+  *p = Part{split * per, min(split * per + per, it->tiles), n_act <= 1,
+            (h * static_cast<int64_t>(rest) + item - a.whole) * a.n_splits + split};
+  return true;
+}
+// The first of its parts of the line; false where there is none.
+__device__ __forceinline__ bool walk_begin(const RowsArgs& a, int cols, int lane, Walk* k) {
+  const int H = a.kv.n_kv_heads, w = blockIdx.x / H, g = a.n_q_heads / H;
+  // tiles of all sequences (the sums stay below 2^31: checked on the host for max_len)
+  int total = 0;
+  for (int base = 0; base < a.B; base += 64) {
+    int row0 = 0, n = 0, x = 0;
+    if (base + lane < a.B) {
+      rows_of(a, base + lane, &row0, &n);
+      x = tiles_of(a, row0, n, a.lens[base + lane], cols, g);
+    }
+    total += __builtin_amdgcn_readlane(scan64(x, lane), 63);
+  }
+  const int r = (total + a.n_shares - 1) / a.n_shares;
+  k->r = max((r + kRowsWaves - 1) / kRowsWaves * kRowsWaves, a.least);
+  const int64_t pos = static_cast<int64_t>(w) * k->r;
+  if (pos >= total) return false;
+  k->pos = static_cast<int>(pos);
+  k->stop = min(total - k->pos, k->r) + k->pos;
+  k->start = k->index = k->b = k->gi = 0;
+  for (int base = 0; base < a.B; base += 64) {
+    int row0 = 0, n = 0, x = 0;
+    if (base + lane < a.B) {
+      rows_of(a, base + lane, &row0, &n);
+      x = tiles_of(a, row0, n, a.lens[base + lane], cols, g);
+    }
+    const int groups = (n * g + cols - 1) / cols, x_upto = scan64(x, lane), g_upto = scan64(groups, lane);
+    const int l = __ffsll(static_cast<long long>(__ballot(k->start + x_upto > k->pos))) - 1;
+    if (l >= 0) {
+      k->b = base + l;
+      k->start += __builtin_amdgcn_readlane(x_upto, l) - __builtin_amdgcn_readlane(x, l);
+      k->index += __builtin_amdgcn_readlane(g_upto, l) - __builtin_amdgcn_readlane(groups, l);
+      return true;
+    }
+    k->start += __builtin_amdgcn_readlane(x_upto, 63);
+    k->index += __builtin_amdgcn_readlane(g_upto, 63);
+  }
+  return false;                                                  // (only if a length changes meanwhile)
+}
+// The part at `pos`, which is moved past it.
+__device__ __forceinline__ bool walk_on(const RowsArgs& a, int cols, Walk* k, Item* it, Part* p) {
+  const int H = a.kv.n_kv_heads, h = blockIdx.x % H, w = blockIdx.x / H;
+  const int g = a.n_q_heads / H;
+  if (k->pos >= k->stop) return false;
+  while (true) {
+    int row0, n;
+    rows_of(a, k->b, &row0, &n);
+    const int64_t len = a.lens[k->b];
+    while (k->gi * static_cast<int64_t>(cols) < static_cast<int64_t>(n) * g) {
+      *it = item_of(a, k->b, h, row0, n, len, k->gi, cols, g);
+      if (k->start + it->tiles > k->pos) {
+        const int begin = k->pos - k->start, end = min(it->tiles, begin + k->stop - k->pos);
+        const int first = k->start / k->r, parts = (k->start + it->tiles - 1) / k->r - first + 1;
+        if (k->index >= a.items) return false;                   // (only if a length changes meanwhile)
+        if (begin == 0 && threadIdx.x == 0) {
+          int32_t* meta = a.meta + 2 * (h * a.items + k->index);
+          meta[0] = first + k->index;
+          meta[1] = parts;
+        }
+        *p = Part{begin, end, parts == 1, h * (a.n_shares + a.items) + w + k->index};
+        k->pos += end - begin;
+        return true;
+      }
+      k->start += it->tiles;
+      ++k->index;
+      ++k->gi;
+    }
+    k->gi = 0;
+    if (++k->b >= a.B) return false;                             // (the same)
+  }
 }
 
 // What column c (row i, one of the lane's) sees: positions [lo, hi), and of a tree
@@ -502,24 +633,27 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
   }
 }
 
-// Vector registers of a wave, for what the kernel holds from tile to tile.
-constexpr bool rows_two_waves(int bits, int D, int C) {
-  return C * (D / 8 + D / 4 + 8) + D / 4 * bits / 16 * 2 + 48 <= 224;
+// Workgroups on a CU, by what the kernel holds in registers from tile to tile.
+constexpr int rows_resident(int bits, int D, int C) {
+  return C * (D / 8 + D / 4 + 8) + D / 4 * bits / 16 * 2 + 48 <= 224 ? 2 : 1;
 }
 
-template <int ACT, int BITS, int D, int C>
-__global__ __launch_bounds__(64 * kRowsWaves, rows_two_waves(BITS, D, C) ? 2 : 1) void k_attn_rows(RowsArgs a) {
+template <int ACT, int BITS, int D, int C, bool LINE>
+__global__ __launch_bounds__(64 * kRowsWaves, rows_resident(BITS, D, C)) void k_attn_rows(RowsArgs a) {
   __shared__ RowsLds<D> lds;
-  const int h = blockIdx.x % a.kv.n_kv_heads;
-  const int64_t rest = blockIdx.x / a.kv.n_kv_heads;
-  const int split = static_cast<int>(rest % a.n_splits);
-  const int64_t item = rest / a.n_splits;
   Item it;
-  if (!item_at(a, item, h, 16 * C, lane_id(), &it)) return;
-  const int n_act = (it.tiles + a.split_tiles - 1) / a.split_tiles;
-  if (split > 0 && split >= n_act) return;
-  const int begin = split * a.split_tiles, end = min(begin + a.split_tiles, it.tiles);
-  attend_rows<ACT, BITS, D, C>(a, lds, it, begin, end, n_act <= 1, (item * a.kv.n_kv_heads + h) * a.n_splits + split);
+  Part p;
+  if constexpr (!LINE) {
+    if (split_of(a, 16 * C, lane_id(), &it, &p)) attend_rows<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
+  } else {
+    Walk k;
+    if (!walk_begin(a, 16 * C, lane_id(), &k) || !walk_on(a, 16 * C, &k, &it, &p)) return;
+    while (true) {
+      attend_rows<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
+      if (!walk_on(a, 16 * C, &k, &it, &p)) return;
+      __syncthreads();                                           // the part's LDS is read
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -891,71 +1025,92 @@ constexpr int tiles_resident(int act, int bits, int D) {
   return D <= 64 ? 4 : D <= 128 ? (act == PW_F16 && bits == 16 ? 2 : 3) : D <= 192 ? 2 : 1;
 }
 
-template <int ACT, int BITS, int D, int C>
+template <int ACT, int BITS, int D, int C, bool LINE>
 __global__ __launch_bounds__(256, tiles_resident(ACT, BITS, D)) void k_attn_tiles(RowsArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * stage_bytes<BITS, D>()];
-  const int h = blockIdx.x % a.kv.n_kv_heads;
-  const int64_t rest = blockIdx.x / a.kv.n_kv_heads;
-  const bool all = rest < a.whole;                               // the first items are not split
-  const int split = all ? 0 : static_cast<int>((rest - a.whole) % a.n_splits);
-  const int64_t item = all ? rest : a.whole + (rest - a.whole) / a.n_splits;
   Item it;
-  if (!item_at(a, item, h, 64 * C, lane_id(), &it)) return;
-  const int per = all ? it.tiles : a.split_tiles, n_act = all ? 1 : (it.tiles + per - 1) / per;
-  if (split > 0 && split >= n_act) return;
-  const int begin = split * per, end = min(begin + per, it.tiles);
-  attend_tiles<ACT, BITS, D, C>(a, lds, it, begin, end, n_act <= 1,
-                                ((item - a.whole) * a.kv.n_kv_heads + h) * a.n_splits + split);
+  Part p;
+  if constexpr (!LINE) {
+    if (split_of(a, 64 * C, lane_id(), &it, &p)) attend_tiles<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
+  } else {
+    Walk k;
+    if (!walk_begin(a, 64 * C, lane_id(), &k) || !walk_on(a, 64 * C, &k, &it, &p)) return;
+    while (true) {
+      attend_tiles<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
+      if (!walk_on(a, 64 * C, &k, &it, &p)) return;
+      __syncthreads();                                           // the part's LDS is read
+    }
+  }
 }
 
-// Joins the parts of four columns of an item, a wave for each, in a fixed order.
+// Joins the parts of 16 columns of an item, four a wave, in a fixed order, and writes
+// the rows of items that no share has.
 template <int ACT, int D>
 __global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols) {
   constexpr int kC = D / 64;
-  const int lane = lane_id(), c = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int h = blockIdx.x % a.kv.n_kv_heads;
-  const int64_t item = a.whole + blockIdx.x / a.kv.n_kv_heads;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int H = a.kv.n_kv_heads, h = blockIdx.x % H, item = blockIdx.x / H, g = a.n_q_heads / H;
   Item it;
-  if (!item_at(a, item, h, cols, lane, &it) || c >= it.n_col) return;
-  const int n = (it.tiles + a.split_tiles - 1) / a.split_tiles;
-  if (n <= 1) return;
-  const int64_t at = ((item - a.whole) * a.kv.n_kv_heads + h) * a.n_splits * cols + c;
-  float mx = kNoMax;
-  for (int s = lane; s < n; s += 64) mx = fmaxf(mx, a.part_ml[2 * (at + static_cast<int64_t>(s) * cols)]);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-  float acc[kC] = {}, sum = 0.0f;
-#pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const int64_t y = at + static_cast<int64_t>(s) * cols;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * y] - mx);
-    sum = fmaf(f, a.part_ml[2 * y + 1], sum);
-#pragma unroll
-    for (int j = 0; j < kC; ++j) acc[j] = fmaf(f, a.part_o[y * D + 64 * j + lane], acc[j]);
+  int n = 0;
+  int64_t at0 = 0;
+  if (a.n_shares == 0) {
+    const int rest = static_cast<int>(a.items - a.whole);
+    if (!item_at(a, rest - 1 - item, h, cols, lane, &it)) return;
+    n = (it.tiles + a.split_tiles - 1) / a.split_tiles;
+    if (n <= 1) return;
+    at0 = (h * static_cast<int64_t>(rest) + item) * a.n_splits * cols;
+  } else if (!item_at(a, item, h, cols, lane, &it)) {
+    return;
+  } else if (it.tiles > 0) {
+    const int32_t* meta = a.meta + 2 * (static_cast<int64_t>(h) * a.items + item);
+    n = meta[1];
+    if (n <= 1) return;
+    at0 = (static_cast<int64_t>(h) * (a.n_shares + a.items) + meta[0]) * cols;
   }
-  const int g = a.n_q_heads / a.kv.n_kv_heads;
-  const int64_t row = static_cast<int64_t>(it.row0 + (it.col0 + c) / g) * a.n_q_heads + h * g + (it.col0 + c) % g;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  for (int c = 16 * blockIdx.y + wave; c < 16 * static_cast<int>(blockIdx.y) + 16 && c < it.n_col; c += 4) {
+    const int64_t at = at0 + c;
+    float mx = kNoMax;
+    for (int s = lane; s < n; s += 64) mx = fmaxf(mx, a.part_ml[2 * (at + static_cast<int64_t>(s) * cols)]);
 #pragma unroll
-  for (int j = 0; j < kC; ++j) a.out[row * D + 64 * j + lane] = static_cast<uint16_t>(pack16<ACT>(acc[j] * inv, 0.0f));
-  if (a.lse && lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
+    for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    float acc[kC] = {}, sum = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < n; ++s) {
+      const int64_t y = at + static_cast<int64_t>(s) * cols;
+      const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * y] - mx);
+      sum = fmaf(f, a.part_ml[2 * y + 1], sum);
+#pragma unroll
+      for (int j = 0; j < kC; ++j) acc[j] = fmaf(f, a.part_o[y * D + 64 * j + lane], acc[j]);
+    }
+    const int64_t row = static_cast<int64_t>(it.row0 + (it.col0 + c) / g) * a.n_q_heads + h * g + (it.col0 + c) % g;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+    for (int j = 0; j < kC; ++j) a.out[row * D + 64 * j + lane] = static_cast<uint16_t>(pack16<ACT>(acc[j] * inv, 0.0f));
+    if (a.lse && lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
+  }
 }
 
 constexpr int kTileCols = 2;          // column tiles of a wave of k_attn_tiles
 
+template <int ACT, int BITS, int D, bool LINE>
+void launch_kernel(const RowsArgs& a, const RowsPlan& p, uint32_t n, hipStream_t st) {
+  if (p.many) k_attn_tiles<ACT, BITS, D, kTileCols, LINE><<<n, 256, 0, st>>>(a);
+  else if (p.col_tiles == 1) k_attn_rows<ACT, BITS, D, 1, LINE><<<n, 64 * kRowsWaves, 0, st>>>(a);
+  else if (D > 128 || p.col_tiles == 2) k_attn_rows<ACT, BITS, D, 2, LINE><<<n, 64 * kRowsWaves, 0, st>>>(a);
+  else if constexpr (D <= 128) k_attn_rows<ACT, BITS, D, 4, LINE><<<n, 64 * kRowsWaves, 0, st>>>(a);
+}
+
 template <int ACT, int BITS, int D>
 hipError_t launch_d(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
-  const int64_t grid = (p.whole + (p.items - p.whole) * p.n_splits) * a.kv.n_kv_heads;
-  if (grid >= (1 << 23)) return hipErrorInvalidConfiguration;
+  const int64_t rest = p.items - p.whole, grid = (p.n_shares ? p.n_shares : p.whole + rest * p.n_splits) * a.kv.n_kv_heads;
+  if (grid >= (1 << 23) || p.items * a.kv.n_kv_heads >= (1 << 23)) return hipErrorInvalidConfiguration;
   const uint32_t n = static_cast<uint32_t>(grid);
-  if (p.many) k_attn_tiles<ACT, BITS, D, kTileCols><<<n, 256, 0, st>>>(a);
-  else if (p.col_tiles == 1) k_attn_rows<ACT, BITS, D, 1><<<n, 64 * kRowsWaves, 0, st>>>(a);
-  else if (D > 128 || p.col_tiles == 2) k_attn_rows<ACT, BITS, D, 2><<<n, 64 * kRowsWaves, 0, st>>>(a);
-  else if constexpr (D <= 128) k_attn_rows<ACT, BITS, D, 4><<<n, 64 * kRowsWaves, 0, st>>>(a);
+  if (p.n_shares) launch_kernel<ACT, BITS, D, true>(a, p, n, st);
+  else launch_kernel<ACT, BITS, D, false>(a, p, n, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 0) return e;
   const int cols = (p.many ? 64 : 16) * p.col_tiles;
-  k_rows_join<ACT, D><<<dim3(static_cast<uint32_t>((p.items - p.whole) * a.kv.n_kv_heads), cols / 4), 256, 0, st>>>(a, cols);
+  k_rows_join<ACT, D><<<dim3(static_cast<uint32_t>(rest * a.kv.n_kv_heads), cols / 16), 256, 0, st>>>(a, cols);
   return hipGetLastError();
 }
 
@@ -973,7 +1128,8 @@ hipError_t launch_bits(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
 }  // namespace
 
 RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, int act, int bits, int max_len, int window) {
-  RowsPlan p{0, 1, 1, 1, 0, 0, 0};
+  RowsPlan p{};
+  p.col_tiles = p.n_splits = p.split_tiles = 1;
   if (B == 0 || T == 0) return p;
   const int64_t g = n_q_heads / n_kv_heads, rows = (static_cast<int64_t>(T) + B - 1) / B, cols = g * rows;
   p.many = g * T > 64 * static_cast<int64_t>(B);
@@ -986,18 +1142,23 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
     tiles = w < tiles ? w : tiles;
   }
   if (tiles == 0) tiles = 1;
+  p.split_tiles = static_cast<int>(tiles);
   const int64_t items = p.items * n_kv_heads;
-  int64_t n = 1;
-  if (p.many) {
-    const int64_t resident = 256 * tiles_resident(act, bits, head_dim);
-    const double unit = 0.5 * tiles_resident(act, bits, head_dim) * head_dim / 128;   // us a tile
-    const double part = 128.0 * (head_dim + 2) * 8 / 4e6;        // us to write and read a part
+  const int per_cu = p.many ? tiles_resident(act, bits, head_dim) : rows_resident(bits, head_dim, p.col_tiles);
+  const int64_t resident = 256 * per_cu;
+  p.least = p.many ? 8 : 32;
+  if (cols <= 4 * group && items * 2 < resident * 3 && tiles >= 3 * p.least && p.items * tiles < (int64_t(1) << 31) - (1 << 20)) {
+    p.n_shares = resident / n_kv_heads > 0 ? resident / n_kv_heads : 1;
+    p.slots = (p.n_shares + p.items) * n_kv_heads * group;
+  } else if (tiles >= 3 * p.least) {
+    const double unit = 0.5 * per_cu * head_dim / 128 * p.col_tiles / 2;   // us a tile
+    const double part = group * (head_dim + 2) * 8 / 4e6;        // us to write and read a part
     const int64_t tri = rows / kTile < tiles ? rows / kTile : tiles;
+    int64_t n = 1;
     double best = 0.0;
-    for (int64_t k = 1; k <= 32 && (k == 1 || tiles / k >= 8); ++k)
+    for (int64_t k = 1; k <= 32 && (k == 1 || tiles / k >= p.least); ++k)
       for (int64_t whole = 0; whole <= (k > 1 && tri < tiles / 4 ? items / resident : 0); whole += items / resident > 0 ? items / resident : 1) {
         const int64_t left = items - whole * resident;
-        if (left < 0) continue;
         const int64_t rounds = (left * k + resident - 1) / resident;
         double t = static_cast<double>(whole) * (tiles + 3) + rounds * (static_cast<double>(tiles) / k + 3);
         if (tri >= tiles / 4) {
@@ -1012,16 +1173,15 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
           p.whole = whole * resident / n_kv_heads;
         }
       }
+    const int64_t per = ((tiles + n - 1) / n + kRowsWaves - 1) / kRowsWaves * kRowsWaves;
+    n = (tiles + per - 1) / per;
     if (n == 1) p.whole = 0;
-  } else {
-    const int64_t most = (tiles + 31) / 32, want = (1024 + items - 1) / items;
-    n = want < most ? want : most;
+    p.n_splits = static_cast<int>(n);
+    p.split_tiles = static_cast<int>(per);
+    if (n > 1) p.slots = (p.items - p.whole) * n_kv_heads * n * group;
   }
-  const int64_t per = ((tiles + n - 1) / n + kRowsWaves - 1) / kRowsWaves * kRowsWaves;
-  n = (tiles + per - 1) / per;
-  p.n_splits = static_cast<int>(n);
-  p.split_tiles = static_cast<int>(per);
-  if (n > 1) p.slots = static_cast<size_t>((p.items - p.whole) * n_kv_heads * n) * group;
+  if (p.slots)
+    p.ws_bytes = static_cast<size_t>(p.slots) * (head_dim + 2) * sizeof(float) + static_cast<size_t>(p.items) * n_kv_heads * 8;
   return p;
 }
 
