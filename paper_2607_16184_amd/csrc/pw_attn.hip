@@ -1,6 +1,6 @@
 // Paged KV cache, gfx950: writing new tokens into it (k_kv_append) and the
 // attention of one new token per sequence over it (k_attn, k_attn_join).
-#include "pw_kv.hpp"
+#include "pw_turn.hpp"
 
 namespace pw {
 namespace {
@@ -63,13 +63,69 @@ constexpr int kAppendWaves = 4;
 constexpr int kAppendMany = 512;          // tokens
 constexpr int kRunItems16 = 6144, kRunItems8 = 16384;   // tokens x heads
 constexpr int kMinRun = 8;
-template <int ACT, int BITS, int D>
-__global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArgs a) {
+
+// The values of place c's token (at row `tok`, channels 32 i + 8 lg .. of its key x) as
+// heads_wave has them; a pair's other half lies in the same lane.
+template <int ACT, int D>
+__device__ __forceinline__ void turned_key(const HeadsArgs& t, const u32x4 (&x)[D / 32], int64_t tok, int lg, float (&f)[D / 32][8]) {
+  float sq = 0.0f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    unpack8<ACT>(x[i], f[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sq = fmaf(f[i][j], f[i][j], sq);
+  }
+  if (t.norm) {
+    sq += __shfl_xor(sq, 16);
+    sq += __shfl_xor(sq, 32);
+    const float inv = 1.0f / sqrtf(sq / static_cast<float>(D) + t.eps);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      float w[8];
+      if (t.k_weight) unpack8<ACT>(ld16(reinterpret_cast<const uint8_t*>(t.k_weight + 32 * i + 8 * lg)), w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] *= t.k_weight ? inv * w[j] : inv;
+    }
+  }
+  const double pos = t.rot.R > 0 ? position_of(t.rot, tok) : 0.0;
+  if (t.rot.interleaved) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      if (32 * i + 8 * lg >= t.rot.R) continue;
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {
+        float co, si;
+        angle_of(t.rot, pos, 16 * i + 4 * lg + j / 2, &co, &si);
+        const float y = f[i][j], z = f[i][j + 1];
+        f[i][j] = fmaf(y, co, z * -si);
+        f[i][j + 1] = fmaf(z, co, y * si);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int by = 1; by <= D / 64; ++by) {                       // R = 64 by
+      if (t.rot.R != 64 * by) continue;
+#pragma unroll
+      for (int i = 0; i < by; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float co, si;
+          angle_of(t.rot, pos, 32 * i + 8 * lg + j, &co, &si);
+          const float y = f[i][j], z = f[i + by][j];
+          f[i][j] = fmaf(y, co, z * -si);
+          f[i + by][j] = fmaf(z, co, y * si);
+        }
+    }
+  }
+}
+
+// Window, head and side `unit` of a.T tokens, by one wave with `mine` of LDS. TURN: keys
+// normed and turned (t).
+template <int ACT, int BITS, int D, bool TURN>
+__device__ __forceinline__ void append_window(const AppendArgs& a, const HeadsArgs& t_args, int64_t unit, uint8_t* mine) {
   constexpr int kE = BITS / 8, kPitch = D * kE + 4;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kAppendWaves][32 * kPitch];
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
+  const int lane = lane_id();
   const int H = a.kv.n_kv_heads, P = a.kv.block_tokens;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kAppendWaves + wave;
   const int is_v = static_cast<int>(unit & 1), h = static_cast<int>((unit >> 1) % H);
   const int64_t first = (unit >> 1) / H * 32;                    // first token of the window
   if (first >= a.T) return;                                      // (wave-uniform; no barrier follows)
@@ -119,9 +175,18 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
       for (int i = 0; i < D / 32; ++i)
         x[u][i] = in(16 * u + c) ? ld16(reinterpret_cast<const uint8_t*>(src + 32 * i)) : u32x4{0u, 0u, 0u, 0u};
     }
-    uint8_t* mine = lds[wave];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      float kf[D / 32][8];                                       // TURN: the keys
+      if constexpr (TURN) {
+        if (!is_v) {
+          turned_key<ACT, D>(t_args, x[u], in(16 * u + c) ? n0 + 16 * u + c : n0 + t0, lg, kf);
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[u][i][w] = pack16<ACT>(kf[i][2 * w], kf[i][2 * w + 1]);
+        }
+      }
       uint8_t* row = mine + (16 * u + c) * kPitch + 8 * lg * kE;
       const bool here = in(16 * u + c);
       if constexpr (BITS == 16) {
@@ -139,7 +204,8 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(val16(x[u][i][j / 2] >> (16 * (j & 1)), ACT)));
+          for (int j = 0; j < 8; ++j)
+            m = fmaxf(m, fabsf(TURN && !is_v ? kf[i][j] : val16(x[u][i][j / 2] >> (16 * (j & 1)), ACT)));
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         const float s = f8_scale(m);
@@ -148,7 +214,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
         for (int i = 0; i < D / 32; ++i) {
           float f[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = val16(x[u][i][j / 2] >> (16 * (j & 1)), ACT);
+          for (int j = 0; j < 8; ++j) f[j] = TURN && !is_v ? kf[i][j] : val16(x[u][i][j / 2] >> (16 * (j & 1)), ACT);
           q[i] = f8_codes8(f, s);
         }
         if (lg == 0 && here) {
@@ -248,9 +314,53 @@ __global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArg
     for (int j = 0; j < kTurns; ++j) {
       const int n = j * kAtOnce + lane / G;
       const int64_t slot = shfl64(sa, 32 + n);
+      if constexpr (TURN) {
+        if (!is_v) {
+          const int by = t_args.rot.R / 16, cp = c < by ? c + by : c < 2 * by ? c - by : c;
+          const uint32_t one2 = ACT == PW_BF16 ? 0x3F803F80u : 0x3C003C00u;
+          u32x4 w{one2, one2, one2, one2}, wp = w;
+          if (t_args.k_weight && 8 * c < D) {
+            w = ld16(reinterpret_cast<const uint8_t*>(t_args.k_weight + 8 * c));
+            wp = ld16(reinterpret_cast<const uint8_t*>(t_args.k_weight + 8 * cp));
+          }
+          Turn tn;
+          turn_of(t_args.rot, min(first + n, static_cast<int64_t>(a.T) - 1), c, &tn);
+          float f[8];
+          head_values<ACT>(t_args, raw[j], w, wp, tn, c, G, f);
+          if ((single >> n) & 1ull) {
+            if constexpr (BITS == 16) {
+              u32x4 y;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[i] = pack16<ACT>(f[2 * i], f[2 * i + 1]);
+              put16(a.kv, y, slot, h, 0, c);
+            } else {
+              put8(a.kv, f, slot, h, 0, c, G);
+            }
+          }
+          continue;
+        }
+      }
       if ((single >> n) & 1ull) append_one<ACT, BITS>(a, raw[j], slot, h, is_v, c, G);
     }
   }
+}
+
+template <int ACT, int BITS, int D>
+__global__ __launch_bounds__(64 * kAppendWaves) void k_kv_append_tiles(AppendArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kAppendWaves][32 * (D * (BITS / 8) + 4)];
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  append_window<ACT, BITS, D, false>(a, HeadsArgs{}, static_cast<int64_t>(blockIdx.x) * kAppendWaves + wave, lds[wave]);
+}
+
+// The rotated append of many tokens: keys and values by windows, first (they take
+// longest), the queries by tokens (k, without keys).
+template <int ACT, int BITS, int D>
+__global__ __launch_bounds__(64 * kAppendWaves) void k_append_runs(AppendArgs a, HeadsArgs t, HeadsCut k, int64_t window_blocks) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kAppendWaves][32 * (D * (BITS / 8) + 4)];
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int64_t block = blockIdx.x;
+  if (block < window_blocks) append_window<ACT, BITS, D, true>(a, t, block * kAppendWaves + wave, lds[wave]);
+  else heads_wave<ACT, 0>(t, (block - window_blocks) * kAppendWaves + wave, k.G, k.steps, k.parts);
 }
 
 // ---------------------------------------------------------------------------
@@ -844,7 +954,38 @@ hipError_t append(const AppendArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int ACT, int BITS>
+hipError_t append_runs(const HeadsArgs& t, hipStream_t st) {
+  const AppendArgs a{t.kv, t.k, t.v, t.ldk, t.ldkh, t.slots, t.T};
+  HeadsArgs q = t;                                               // the queries alone
+  q.n_k = 0;
+  const HeadsCut k = heads_cut(t.T, t.D, t.n_q);
+  const int64_t windows = ((static_cast<int64_t>(t.T) + 31) / 32 * t.n_k * 2 + kAppendWaves - 1) / kAppendWaves;
+  const int64_t grid = windows + (t.n_q ? k.blocks : 0);
+  if (grid >= (1 << 24)) return hipErrorInvalidConfiguration;
+  const dim3 g(static_cast<uint32_t>(grid)), b(64 * kAppendWaves);
+  switch (t.D) {
+    case 64: k_append_runs<ACT, BITS, 64><<<g, b, 0, st>>>(a, q, k, windows); break;
+    case 128: k_append_runs<ACT, BITS, 128><<<g, b, 0, st>>>(a, q, k, windows); break;
+    case 192: k_append_runs<ACT, BITS, 192><<<g, b, 0, st>>>(a, q, k, windows); break;
+    case 256: k_append_runs<ACT, BITS, 256><<<g, b, 0, st>>>(a, q, k, windows); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
 }  // namespace
+
+// By runs where pw_kv_append goes by them, and a pair lies in one lane there.
+bool append_by_runs(const HeadsArgs& a) {
+  return a.T >= kAppendMany && static_cast<int64_t>(a.T) * a.n_k >= (a.kv.bits == 16 ? kRunItems16 : kRunItems8) &&
+         (a.rot.interleaved || a.rot.R % 64 == 0);
+}
+
+hipError_t launch_append_runs(const HeadsArgs& a, hipStream_t st) {
+  if (a.act == PW_BF16) return a.kv.bits == 16 ? append_runs<PW_BF16, 16>(a, st) : append_runs<PW_BF16, 8>(a, st);
+  return a.kv.bits == 16 ? append_runs<PW_F16, 16>(a, st) : append_runs<PW_F16, 8>(a, st);
+}
 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st) {
   if (a.kv.act == PW_BF16) return a.kv.bits == 16 ? append<PW_BF16, 16>(a, st) : append<PW_BF16, 8>(a, st);

@@ -177,6 +177,8 @@ hipError_t launch_gemm8(const Gemm8Args& a, hipStream_t st);
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t st);
 hipError_t launch_attn(const AttnArgs& a, hipStream_t st);
 hipError_t launch_heads(const HeadsArgs& a, hipStream_t st);
+bool append_by_runs(const HeadsArgs& a);
+hipError_t launch_append_runs(const HeadsArgs& a, hipStream_t st);
 hipError_t launch_kv_keep(const KeepArgs& a, hipStream_t st);
 hipError_t launch_attn_rows(const RowsArgs& a, const RowsPlan& p, hipStream_t st);
 hipError_t launch_route_grouped(const RouteArgs& a, hipStream_t st);

@@ -87,9 +87,12 @@ __device__ __forceinline__ bool item_at(const RowsArgs& a, int64_t item, int h, 
   const int g = a.n_q_heads / a.kv.n_kv_heads;
   int64_t before = 0;
   for (int base = 0; base < a.B; base += 64) {
-    int row0 = 0, n = 0;
-    if (base + lane < a.B) rows_of(a, base + lane, &row0, &n);
-    const int groups = (n * g + cols - 1) / cols, upto = scan64(groups, lane);
+    int row0 = 0, n = 0, len = 0;
+    if (base + lane < a.B) {
+      rows_of(a, base + lane, &row0, &n);
+      len = a.lens[base + lane];
+    }
+    const int groups = (n * g + cols - 1) / cols, upto = a.B > 1 ? scan64(groups, lane) : __builtin_amdgcn_readlane(groups, 0);
     const int all = __builtin_amdgcn_readlane(upto, 63);
     if (item < before + all) {
       const int l = __ffsll(static_cast<long long>(__ballot(before + upto > item))) - 1;
@@ -97,7 +100,8 @@ __device__ __forceinline__ bool item_at(const RowsArgs& a, int64_t item, int h, 
       n = __builtin_amdgcn_readlane(n, l);
       const int64_t gi = item - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(groups, l));
       if (gi < 0 || gi * cols >= static_cast<int64_t>(n) * g) return false;
-      *it = item_of(a, base + l, h, __builtin_amdgcn_readlane(row0, l), n, a.lens[base + l], static_cast<int>(gi), cols, g);
+      *it = item_of(a, base + l, h, __builtin_amdgcn_readlane(row0, l), n, __builtin_amdgcn_readlane(len, l),
+                    static_cast<int>(gi), cols, g);
       return true;
     }
     before += all;
@@ -215,14 +219,16 @@ __device__ __forceinline__ bool walk_on(const RowsArgs& a, int cols, Walk* k, It
 struct Column {
   int lo, hi;
   int row;                 // of q and the masks; -1: no column
+  uint64_t word0;          // of its mask
 };
 __device__ __forceinline__ Column column_at(const RowsArgs& a, const Item& it, int c, int g) {
-  Column x{0, 0, -1};
+  Column x{0, 0, -1, 0};
   if (c >= it.n_col) return x;
   const int i = (it.col0 + c) / g;
   x.row = it.row0 + i;
   if (a.masks) {
     x.hi = clampi(it.ctx, 0, a.max_len);
+    x.word0 = static_cast<uint64_t>(a.masks[static_cast<int64_t>(x.row) * a.words]);
     if (a.window) {
       int64_t seen = 0;
       for (int w = 0; w < a.words && 64 * w < it.n; ++w) {
@@ -247,10 +253,10 @@ __device__ __forceinline__ uint32_t seen_of(const RowsArgs& a, const Item& it, c
     const int64_t* m = a.masks + static_cast<int64_t>(x.row) * a.words;
     uint64_t d = 0;
     if (j < 0) {
-      d = static_cast<uint64_t>(m[0]) << -j;
+      d = x.word0 << -j;
     } else if (j < 64 * static_cast<int64_t>(a.words)) {
       const int w = static_cast<int>(j >> 6), sh = static_cast<int>(j & 63);
-      d = static_cast<uint64_t>(m[w]) >> sh;
+      d = (w == 0 ? x.word0 : static_cast<uint64_t>(m[w])) >> sh;
       if (sh > 32 && w + 1 < a.words) d |= static_cast<uint64_t>(m[w + 1]) << (64 - sh);
     }
     s |= static_cast<uint32_t>(d) & first_bits(clamp64(static_cast<int64_t>(it.hi) - t, 0, 32));
@@ -462,6 +468,7 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
       if (next_t >= 0) load_k();
 #pragma unroll
       for (int c = 0; c < C; ++c) {
+        if (16 * c >= it.n_col) break;                           // (uniform)
         uint32_t seen = ~0u;
         if (part) {
           seen = seen_of(a, it, x[c], t);
@@ -1157,11 +1164,11 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
     int64_t n = 1;
     double best = 0.0;
     for (int64_t k = 1; k <= 32 && (k == 1 || tiles / k >= p.least); ++k)
-      for (int64_t whole = 0; whole <= (k > 1 && tri < tiles / 4 ? items / resident : 0); whole += items / resident > 0 ? items / resident : 1) {
+      for (int64_t whole = 0; whole <= (k > 1 && tri <= tiles / 2 ? items / resident : 0); whole += items / resident > 0 ? items / resident : 1) {
         const int64_t left = items - whole * resident;
         const int64_t rounds = (left * k + resident - 1) / resident;
         double t = static_cast<double>(whole) * (tiles + 3) + rounds * (static_cast<double>(tiles) / k + 3);
-        if (tri >= tiles / 4) {
+        if (tri > tiles / 2) {                                   // spans of all lengths: short ones fill the gaps
           const double mean = (tiles - 0.5 * tri) * items / resident, longest = static_cast<double>(tiles) / k;
           t = (mean > longest ? mean : longest) + 3 * rounds;
         }
