@@ -87,15 +87,18 @@ __device__ __forceinline__ void turned_key(const HeadsArgs& t, const u32x4 (&x)[
       for (int j = 0; j < 8; ++j) f[i][j] *= t.k_weight ? inv * w[j] : inv;
     }
   }
-  const double pos = t.rot.R > 0 ? position_of(t.rot, tok) : 0.0;
+  const double quarters = t.rot.R > 0 ? quarters_of(t.rot, tok) : 0.0;
   if (t.rot.interleaved) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       if (32 * i + 8 * lg >= t.rot.R) continue;
+      double freq[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) freq[j] = t.rot.inv_freq[16 * i + 4 * lg + j];
 #pragma unroll
       for (int j = 0; j < 8; j += 2) {
         float co, si;
-        angle_of(t.rot, pos, 16 * i + 4 * lg + j / 2, &co, &si);
+        angle_of(t.rot, quarters, freq[j / 2], &co, &si);
         const float y = f[i][j], z = f[i][j + 1];
         f[i][j] = fmaf(y, co, z * -si);
         f[i][j + 1] = fmaf(z, co, y * si);
@@ -106,16 +109,37 @@ __device__ __forceinline__ void turned_key(const HeadsArgs& t, const u32x4 (&x)[
     for (int by = 1; by <= D / 64; ++by) {                       // R = 64 by
       if (t.rot.R != 64 * by) continue;
 #pragma unroll
-      for (int i = 0; i < by; ++i)
+      for (int i = 0; i < by; ++i) {
+        double freq[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) freq[j] = t.rot.inv_freq[32 * i + 8 * lg + j];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           float co, si;
-          angle_of(t.rot, pos, 32 * i + 8 * lg + j, &co, &si);
+          angle_of(t.rot, quarters, freq[j], &co, &si);
           const float y = f[i][j], z = f[i + by][j];
           f[i][j] = fmaf(y, co, z * -si);
           f[i + by][j] = fmaf(z, co, y * si);
         }
+      }
     }
+  }
+}
+
+// turn_of for a token per lane group.
+__device__ __forceinline__ void own_turn(const Rotate& r, int64_t tok, int c, Turn* t) {
+  const int half = r.R / 2;
+  const bool hi = 8 * c >= half;
+  const double quarters = r.R > 0 ? quarters_of(r, tok) : 0.0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    t->cs[j] = 1.0f;
+    t->sn[j] = 0.0f;
+    if (8 * c >= r.R) continue;
+    float co, si;
+    angle_of(r, quarters, r.inv_freq[r.interleaved ? 4 * c + j / 2 : 8 * c + j - (hi ? half : 0)], &co, &si);
+    t->cs[j] = co;
+    t->sn[j] = (r.interleaved ? j & 1 : hi) ? si : -si;
   }
 }
 
@@ -324,7 +348,7 @@ __device__ __forceinline__ void append_window(const AppendArgs& a, const HeadsAr
             wp = ld16(reinterpret_cast<const uint8_t*>(t_args.k_weight + 8 * cp));
           }
           Turn tn;
-          turn_of(t_args.rot, min(first + n, static_cast<int64_t>(a.T) - 1), c, &tn);
+          own_turn(t_args.rot, min(first + n, static_cast<int64_t>(a.T) - 1), c, &tn);
           float f[8];
           head_values<ACT>(t_args, raw[j], w, wp, tn, c, G, f);
           if ((single >> n) & 1ull) {
