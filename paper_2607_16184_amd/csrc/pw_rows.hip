@@ -1032,22 +1032,12 @@ constexpr int tiles_resident(int act, int bits, int D) {
   return D <= 64 ? 4 : D <= 128 ? (act == PW_F16 && bits == 16 ? 2 : 3) : D <= 192 ? 2 : 1;
 }
 
-template <int ACT, int BITS, int D, int C, bool LINE>
+template <int ACT, int BITS, int D, int C>
 __global__ __launch_bounds__(256, tiles_resident(ACT, BITS, D)) void k_attn_tiles(RowsArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * stage_bytes<BITS, D>()];
   Item it;
   Part p;
-  if constexpr (!LINE) {
-    if (split_of(a, 64 * C, lane_id(), &it, &p)) attend_tiles<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
-  } else {
-    Walk k;
-    if (!walk_begin(a, 64 * C, lane_id(), &k) || !walk_on(a, 64 * C, &k, &it, &p)) return;
-    while (true) {
-      attend_tiles<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
-      if (!walk_on(a, 64 * C, &k, &it, &p)) return;
-      __syncthreads();                                           // the part's LDS is read
-    }
-  }
+  if (split_of(a, 64 * C, lane_id(), &it, &p)) attend_tiles<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
 }
 
 // Joins the parts of 16 columns of an item, four a wave, in a fixed order, and writes
@@ -1098,22 +1088,19 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols) {
 }
 
 constexpr int kTileCols = 2;          // column tiles of a wave of k_attn_tiles
-
-template <int ACT, int BITS, int D, bool LINE>
-void launch_kernel(const RowsArgs& a, const RowsPlan& p, uint32_t n, hipStream_t st) {
-  if (p.many) k_attn_tiles<ACT, BITS, D, kTileCols, LINE><<<n, 256, 0, st>>>(a);
-  else if (p.col_tiles == 1) k_attn_rows<ACT, BITS, D, 1, LINE><<<n, 64 * kRowsWaves, 0, st>>>(a);
-  else if (D > 128 || p.col_tiles == 2) k_attn_rows<ACT, BITS, D, 2, LINE><<<n, 64 * kRowsWaves, 0, st>>>(a);
-  else if constexpr (D <= 128) k_attn_rows<ACT, BITS, D, 4, LINE><<<n, 64 * kRowsWaves, 0, st>>>(a);
-}
+constexpr int kPiece = 72;            // tiles of a split in a batch
 
 template <int ACT, int BITS, int D>
 hipError_t launch_d(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
   const int64_t rest = p.items - p.whole, grid = (p.n_shares ? p.n_shares : p.whole + rest * p.n_splits) * a.kv.n_kv_heads;
   if (grid >= (1 << 23) || p.items * a.kv.n_kv_heads >= (1 << 23)) return hipErrorInvalidConfiguration;
   const uint32_t n = static_cast<uint32_t>(grid);
-  if (p.n_shares) launch_kernel<ACT, BITS, D, true>(a, p, n, st);
-  else launch_kernel<ACT, BITS, D, false>(a, p, n, st);
+  constexpr int kThreads = 64 * kRowsWaves;
+  if (p.many) k_attn_tiles<ACT, BITS, D, kTileCols><<<n, 256, 0, st>>>(a);
+  else if (p.col_tiles == 1 && p.n_shares) k_attn_rows<ACT, BITS, D, 1, true><<<n, kThreads, 0, st>>>(a);
+  else if (p.col_tiles == 1) k_attn_rows<ACT, BITS, D, 1, false><<<n, kThreads, 0, st>>>(a);
+  else if (p.n_shares) k_attn_rows<ACT, BITS, D, 2, true><<<n, kThreads, 0, st>>>(a);
+  else k_attn_rows<ACT, BITS, D, 2, false><<<n, kThreads, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 0) return e;
   const int cols = (p.many ? 64 : 16) * p.col_tiles;
@@ -1140,9 +1127,11 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
   if (B == 0 || T == 0) return p;
   const int64_t g = n_q_heads / n_kv_heads, rows = (static_cast<int64_t>(T) + B - 1) / B, cols = g * rows;
   p.many = g * T > 64 * static_cast<int64_t>(B);
-  p.col_tiles = p.many ? kTileCols : cols <= 16 ? 1 : cols <= 32 || head_dim > 128 ? 2 : 4;
+  const auto items_of = [&](int64_t group) { return g * T / group + (B < T ? B : T); };
+  if (p.many) p.col_tiles = kTileCols;
+  else p.col_tiles = cols > 16 && bits == 16 && items_of(32) * n_kv_heads >= 256 ? 2 : 1;
   const int64_t group = (p.many ? 64 : 16) * p.col_tiles;
-  p.items = g * T / group + (B < T ? B : T);
+  p.items = items_of(group);
   int64_t tiles = (static_cast<int64_t>(max_len) + kTile - 1) / kTile;
   if (window > 0) {
     const int64_t w = (static_cast<int64_t>(window) + T + 2 * kTile - 2) / kTile;
@@ -1151,36 +1140,45 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
   if (tiles == 0) tiles = 1;
   p.split_tiles = static_cast<int>(tiles);
   const int64_t items = p.items * n_kv_heads;
-  const int per_cu = p.many ? tiles_resident(act, bits, head_dim) : rows_resident(bits, head_dim, p.col_tiles);
-  const int64_t resident = 256 * per_cu;
-  p.least = p.many ? 8 : 32;
-  if (cols <= 4 * group && items * 2 < resident * 3 && tiles >= 3 * p.least && p.items * tiles < (int64_t(1) << 31) - (1 << 20)) {
-    p.n_shares = resident / n_kv_heads > 0 ? resident / n_kv_heads : 1;
-    p.slots = (p.n_shares + p.items) * n_kv_heads * group;
-  } else if (tiles >= 3 * p.least) {
-    const double unit = 0.5 * per_cu * head_dim / 128 * p.col_tiles / 2;   // us a tile
-    const double part = group * (head_dim + 2) * 8 / 4e6;        // us to write and read a part
-    const int64_t tri = rows / kTile < tiles ? rows / kTile : tiles;
+  if (!p.many) {
+    const int64_t resident = 256 * rows_resident(bits, head_dim, p.col_tiles);
+    p.least = 32;
+    if (items * 2 < resident * 3 && tiles >= 3 * p.least && p.items * tiles < (int64_t(1) << 31) - (1 << 20)) {
+      p.n_shares = resident / n_kv_heads > 0 ? resident / n_kv_heads : 1;
+      p.slots = (p.n_shares + p.items) * n_kv_heads * group;
+    }
+  } else if (tiles >= 24) {
+    const int per_cu = tiles_resident(act, bits, head_dim);
+    const int64_t resident = 256 * per_cu, most = tiles / 8;
     int64_t n = 1;
-    double best = 0.0;
-    for (int64_t k = 1; k <= 32 && (k == 1 || tiles / k >= p.least); ++k)
-      for (int64_t whole = 0; whole <= (k > 1 && tri <= tiles / 2 ? items / resident : 0); whole += items / resident > 0 ? items / resident : 1) {
-        const int64_t left = items - whole * resident;
-        const int64_t rounds = (left * k + resident - 1) / resident;
-        double t = static_cast<double>(whole) * (tiles + 3) + rounds * (static_cast<double>(tiles) / k + 3);
-        if (tri > tiles / 2) {                                   // spans of all lengths: short ones fill the gaps
-          const double mean = (tiles - 0.5 * tri) * items / resident, longest = static_cast<double>(tiles) / k;
-          t = (mean > longest ? mean : longest) + 3 * rounds;
+    if (B > 1 && items < 2 * resident) {
+      const int64_t fill = (resident + items - 1) / items;
+      n = (tiles + kPiece - 1) / kPiece;
+      n = n < fill ? fill : n;
+      n = n < most ? n : most;
+    } else {
+      const double unit = 0.5 * per_cu * head_dim / 128;         // us a tile
+      const double part = group * (head_dim + 2) * 8 / 4e6;      // us to write and read a part
+      const int64_t tri = rows / kTile < tiles ? rows / kTile : tiles;
+      double best = 0.0;
+      for (int64_t k = 1; k <= 32 && k <= most; ++k)
+        for (int64_t whole = 0; whole <= (k > 1 && tri <= tiles / 2 ? items / resident : 0); whole += items / resident > 0 ? items / resident : 1) {
+          const int64_t left = items - whole * resident, rounds = (left * k + resident - 1) / resident;
+          double t = static_cast<double>(whole) * (tiles + 3) + rounds * (static_cast<double>(tiles) / k + 3);
+          if (tri > tiles / 2) {                                 // spans of all lengths: short ones fill the gaps
+            const double mean = (tiles - 0.5 * tri) * items / resident, longest = static_cast<double>(tiles) / k;
+            t = (mean > longest ? mean : longest) + 3 * rounds;
+          }
+          t *= unit;
+          if (k > 1) t += 5.0 + left * k * part;
+          if (best == 0.0 || t < best) {
+            best = t;
+            n = k;
+            p.whole = whole * resident / n_kv_heads;
+          }
         }
-        t *= unit;
-        if (k > 1) t += 5.0 + left * k * part;
-        if (best == 0.0 || t < best) {
-          best = t;
-          n = k;
-          p.whole = whole * resident / n_kv_heads;
-        }
-      }
-    const int64_t per = ((tiles + n - 1) / n + kRowsWaves - 1) / kRowsWaves * kRowsWaves;
+    }
+    const int64_t per = (tiles + n - 1) / n;
     n = (tiles + per - 1) / per;
     if (n == 1) p.whole = 0;
     p.n_splits = static_cast<int>(n);
