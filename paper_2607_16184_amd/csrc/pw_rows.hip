@@ -219,16 +219,14 @@ __device__ __forceinline__ bool walk_on(const RowsArgs& a, int cols, Walk* k, It
 struct Column {
   int lo, hi;
   int row;                 // of q and the masks; -1: no column
-  uint64_t word0;          // of its mask
 };
 __device__ __forceinline__ Column column_at(const RowsArgs& a, const Item& it, int c, int g) {
-  Column x{0, 0, -1, 0};
+  Column x{0, 0, -1};
   if (c >= it.n_col) return x;
   const int i = (it.col0 + c) / g;
   x.row = it.row0 + i;
   if (a.masks) {
     x.hi = clampi(it.ctx, 0, a.max_len);
-    x.word0 = static_cast<uint64_t>(a.masks[static_cast<int64_t>(x.row) * a.words]);
     if (a.window) {
       int64_t seen = 0;
       for (int w = 0; w < a.words && 64 * w < it.n; ++w) {
@@ -245,18 +243,21 @@ __device__ __forceinline__ Column column_at(const RowsArgs& a, const Item& it, i
   return x;
 }
 __device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : (1u << n) - 1u; }
-// Bit i: the column sees position t + i.
-__device__ __forceinline__ uint32_t seen_of(const RowsArgs& a, const Item& it, const Column& x, int t) {
+__device__ __forceinline__ uint64_t first_word(const RowsArgs& a, const Column& x) {
+  return a.masks && x.row >= 0 ? static_cast<uint64_t>(a.masks[static_cast<int64_t>(x.row) * a.words]) : 0;
+}
+// Bit i: the column sees position t + i. word0: the first word of its mask.
+__device__ __forceinline__ uint32_t seen_of(const RowsArgs& a, const Item& it, const Column& x, uint64_t word0, int t) {
   uint32_t s = first_bits(clamp64(static_cast<int64_t>(x.hi) - t, 0, 32)) & ~first_bits(clamp64(static_cast<int64_t>(x.lo) - t, 0, 32));
   if (a.masks && x.row >= 0 && t + kTile > it.ctx) {
     const int64_t j = static_cast<int64_t>(t) - it.ctx;          // drafted token of bit 0, above -32
     const int64_t* m = a.masks + static_cast<int64_t>(x.row) * a.words;
     uint64_t d = 0;
     if (j < 0) {
-      d = x.word0 << -j;
+      d = word0 << -j;
     } else if (j < 64 * static_cast<int64_t>(a.words)) {
       const int w = static_cast<int>(j >> 6), sh = static_cast<int>(j & 63);
-      d = (w == 0 ? x.word0 : static_cast<uint64_t>(m[w])) >> sh;
+      d = (w == 0 ? word0 : static_cast<uint64_t>(m[w])) >> sh;
       if (sh > 32 && w + 1 < a.words) d |= static_cast<uint64_t>(m[w + 1]) << (64 - sh);
     }
     s |= static_cast<uint32_t>(d) & first_bits(clamp64(static_cast<int64_t>(it.hi) - t, 0, 32));
@@ -304,12 +305,14 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
   const int g = a.n_q_heads / a.kv.n_kv_heads;
 
   Column x[C];
+  uint64_t word0[C];                                             // (early: otherwise one more load in the chain of the last tiles)
   u32x4 q[C][D / 32];
   int all_lo = 0, all_hi = INT32_MAX;                            // all columns see [all_lo, all_hi)
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int cc = 16 * c + col;
     x[c] = column_at(a, it, cc, g);
+    word0[c] = first_word(a, x[c]);
     if (x[c].row >= 0) {
       all_lo = max(all_lo, x[c].lo);
       all_hi = min(all_hi, x[c].hi);
@@ -471,7 +474,7 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
         if (16 * c >= it.n_col) break;                           // (uniform)
         uint32_t seen = ~0u;
         if (part) {
-          seen = seen_of(a, it, x[c], t);
+          seen = seen_of(a, it, x[c], word0[c], t);
 #pragma unroll
           for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -822,7 +825,7 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
       if (part) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          seen[c] = seen_of(a, it, x[c], t) >> (4 * lg);
+          seen[c] = seen_of(a, it, x[c], first_word(a, x[c]), t) >> (4 * lg);
 #pragma unroll
           for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -1029,7 +1032,8 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
 // Workgroups of k_attn_tiles on a CU, by its registers (fp16 caches: more of them)
 // and LDS.
 constexpr int tiles_resident(int act, int bits, int D) {
-  return D <= 64 ? 4 : D <= 128 ? (act == PW_F16 && bits == 16 ? 2 : 3) : D <= 192 ? 2 : 1;
+  const bool more = act == PW_F16 && bits == 16;
+  return D <= 64 ? (more ? 3 : 4) : D <= 128 ? (more ? 2 : 3) : D <= 192 ? (more ? 1 : 2) : 1;
 }
 
 template <int ACT, int BITS, int D, int C>

@@ -204,11 +204,10 @@ def _rows(t: Optional[torch.Tensor], T: int, D: int, act: torch.dtype, dev: int,
     """(address, heads, row stride, head stride) of heads [T, n, D]; nothing for None."""
     if t is None:
         return 0, 0, 0, 0
-    if not (t.dim() == 3 and t.shape[0] == T and t.shape[2] == D and t.dtype is act and t.get_device() == dev):
-        raise ValueError("%s must be [%d, heads, %d], %s, on device %d" % (name, T, D, act, dev))
+    rows, n, width = t.shape
     ld, ldh, inner = t.stride()
-    _need(inner == 1, name + " must have contiguous channels")
-    n = t.shape[1]
+    if rows != T or width != D or t.dtype is not act or inner != 1 or t.get_device() != dev:
+        raise ValueError("%s must be [%d, heads, %d], %s, on device %d, with contiguous channels" % (name, T, D, act, dev))
     return t.data_ptr(), n, ld if T > 1 else 0, ldh if n > 1 else 0   # a single row, or head, may have any stride
 
 
