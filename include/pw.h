@@ -714,7 +714,7 @@ typedef struct {
  *   positions [T] int32 device, of any sign (not read without a rotation).
  * Constraints: head_dim a multiple of 16, 16 to 256; act PW_F16 or PW_BF16; eps >= 0
  * and finite; strides multiples of 8; heads and weights 16-byte aligned (PW_EINVAL
- * otherwise); T < 2^25, T * (n_q + n_k) < 2^30 (PW_EUNSUPPORTED). T = 0 does
+ * otherwise); T < 2^24, T * (n_q + n_k) < 2^29 (PW_EUNSUPPORTED). T = 0 does
  * nothing.                                                                   */
 pw_status pw_heads_norm_rotate(const pw_rotation* rot, const int32_t* positions, int offset, const void* q, int64_t ldq,
                                int64_t ldqh, int n_q, const void* k, int64_t ldk, int64_t ldkh, int n_k,
@@ -729,7 +729,7 @@ pw_status pw_heads_norm_rotate(const pw_rotation* rot, const int32_t* positions,
  *   k and v [T, cache heads], strides ld and ldh, and slots as in pw_kv_append; n_q
  *   may be 0.
  * Constraints: those of pw_kv_append and pw_heads_norm_rotate; T * (n_q + 2
- * n_kv_heads) < 2^30 (PW_EUNSUPPORTED).                                      */
+ * n_kv_heads) < 2^29 (PW_EUNSUPPORTED).                                      */
 pw_status pw_kv_append_rotated(const pw_kv_cache* cache, const pw_rotation* rot, const int32_t* positions, int offset,
                                const void* q, int64_t ldq, int64_t ldqh, int n_q, const void* k, const void* v,
                                int64_t ld, int64_t ldh, const void* q_weight, const void* k_weight, int norm, float eps,
@@ -755,8 +755,8 @@ pw_status pw_kv_append_rotated(const pw_kv_cache* cache, const pw_rotation* rot,
  * What lies in the cache at positions that a row does not see is not used for it,
  * NaN and infinities included. Scores, exponentials and sums are in fp32; weights
  * enter the product with the values as in pw_attn_decode where T * (n_q_heads /
- * n_kv_heads) <= 64 B, above that rounded once to 16 bits: to bf16 with bf16 and 8-bit
- * caches, off by at most 2^-8 of themselves; with fp16 caches by at most 2^-11 and
+ * n_kv_heads) <= 64 B, and in 8-bit caches with act PW_F16; above that rounded once to
+ * act: to bf16, off by at most 2^-8 of themselves, or to fp16, by at most 2^-11 and
  * 2^-52 of the row's largest weight.
  * Constraints: B, T >= 0; n_q_heads a multiple of n_kv_heads; 1 <= words <= 1024;
  * 0 <= max_len < 2^31 - 256; window >= 0; scale finite (PW_EINVAL otherwise); B <

@@ -66,9 +66,9 @@ const char* heads_fault(const pw_rotation* r, int head_dim, int T, int n_q, int 
   if (norm && (!(eps >= 0.0f) || std::isinf(eps))) return "eps must be finite and not negative";
   return nullptr;
 }
-constexpr const char* kTooManyHeads = "T must stay below 2^25, T times the heads below 2^30: split the batch";
+constexpr const char* kTooManyHeads = "T must stay below 2^24, T times the heads below 2^29: split the batch";
 bool heads_too_many(int T, int n_q, int n_k) {
-  return T >= (1 << 25) || static_cast<int64_t>(T) * (static_cast<int64_t>(n_q) + n_k) >= (int64_t(1) << 30);
+  return T >= (1 << 24) || static_cast<int64_t>(T) * (static_cast<int64_t>(n_q) + n_k) >= (int64_t(1) << 29);
 }
 pw::Rotate rotate_args(const pw_rotation* r, const int32_t* positions, int offset) {
   if (!r || r->dims == 0) return {nullptr, nullptr, 0, 0, 0, 1.0f};

@@ -684,6 +684,7 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
                                              int64_t slot) {
   constexpr int kPv = BITS == 8 ? PW_BF16 : ACT;
   constexpr bool kByTile = kPv == PW_F16;
+  constexpr bool kTwo = BITS == 8 && ACT == PW_F16;   // weights in two terms: fp16 outputs show what one bf16 leaves
   constexpr int kLoads = D * BITS / 8 * 16 / 1024;    // 1 KB pieces of 16 tokens' keys
   constexpr int kMine = kLoads + (BITS == 8 ? 1 : 0); // loads of a wave for a tile: a quarter of the pieces, the scales
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
@@ -833,7 +834,7 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
         }
         mul = 1.0f;
       }
-      u32x4 p_hi[C];
+      u32x4 p_hi[C], p_two[C];
       float share[C], base[C], top[C];
       bool low = false;                                          // fp16: weights that one term does not hold
       bool raise = false;
@@ -887,6 +888,8 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
             }
           }
           p_hi[c][w] = pack16<kPv>(p[0], p[1]);
+          if constexpr (kTwo)
+            p_two[c][w] = pack16<kPv>(p[0] - val16(p_hi[c][w] & 0xFFFFu, kPv), p[1] - val16(p_hi[c][w] >> 16, kPv));
         }
         l[c] = fmaf(share[c], sum, l[c]);
         if constexpr (kByTile) share[c] *= 1.0f / kLift;
@@ -959,7 +962,10 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
             for (int e = 0; e < 2; ++e) {
               const u32x4 w = widen8<kPv>(v[2 * e], v[2 * e + 1]);
 #pragma unroll
-              for (int c = 0; c < C; ++c) o[c][2 * j + e] = mma<kPv>(w, p_hi[c], o[c][2 * j + e]);
+              for (int c = 0; c < C; ++c) {
+                o[c][2 * j + e] = mma<kPv>(w, p_hi[c], o[c][2 * j + e]);
+                if constexpr (kTwo) o[c][2 * j + e] = mma<kPv>(w, p_two[c], o[c][2 * j + e]);
+              }
             }
           }
         }
@@ -1032,8 +1038,8 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
 // Workgroups of k_attn_tiles on a CU, by its registers (fp16 caches: more of them)
 // and LDS.
 constexpr int tiles_resident(int act, int bits, int D) {
-  const bool more = act == PW_F16 && bits == 16;
-  return D <= 64 ? (more ? 3 : 4) : D <= 128 ? (more ? 2 : 3) : D <= 192 ? (more ? 1 : 2) : 1;
+  const bool more = act == PW_F16;
+  return D <= 64 ? (more ? 3 : 4) : D <= 128 ? (more ? 2 : 3) : D <= 192 ? (more && bits == 16 ? 1 : 2) : 1;
 }
 
 template <int ACT, int BITS, int D, int C>

@@ -369,6 +369,7 @@ class KVCache:
         _packed(starts, (B + 1,), torch.int32, dev, "starts")
         _packed(lens, (B,), torch.int32, dev, "lens")
         words = 0 if masks is None else masks.shape[1]
+        _need(masks is None or words > 0, "masks must have at least one word")
         _packed(masks, (T, words), torch.int64, dev, "masks")
         table, ld_table = self._table(block_table, B, max_len)
         if out is None:

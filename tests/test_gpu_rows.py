@@ -40,9 +40,7 @@ def _bound(act, D, n_keys, size, o, mass, once=None):
 
 def _once(T, B, g, act, bits):
     """The type that a call's weights are rounded to, None: two terms."""
-    if T * g <= 64 * B:
-        return None
-    return act if bits == 16 else BF
+    return None if T * g <= 64 * B or (act is FP and bits == 8) else act
 
 
 def _case(seqs, P, H, g, D, act, bits, tree=None, window=0, seed=0, scale=None, missing=(), odd=(), pad_rows=0, max_len=None,

@@ -227,5 +227,17 @@ def test_positions_and_frequencies_are_refused(calls):
     assert not calls
 
 
+def test_masks_without_words_are_refused(calls):
+    with pytest.raises(ValueError):
+        _rows(_make(ROWS_T, 0), masks=_t(0, 3, 0, dtype=I64))
+    assert not calls
+
+
+def test_limits_are_the_ones_stated():
+    _refused(pw.PW_EUNSUPPORTED, _call(pw.pw_heads_norm_rotate, HEADS, HEADS_OK, T=1 << 24))
+    _refused(pw.PW_EUNSUPPORTED, _call(pw.pw_heads_norm_rotate, HEADS, HEADS_OK, T=1 << 23, nq=62, ldqo=62 * 64))
+    _refused(pw.PW_EUNSUPPORTED, _call(pw.pw_kv_append_rotated, APPEND, APPEND_OK, T=1 << 24))
+
+
 def test_structure_matches_the_header():
     assert ctypes.sizeof(pw.pw_rotation) == 24
