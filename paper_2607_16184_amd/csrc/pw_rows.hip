@@ -12,6 +12,20 @@ namespace {
 // + 3 of either half of a 32-token tile for column lane mod 16. What a column sees
 // of a tile is 32 bits: a range of positions, and for trees the row's mask shifted
 // to the tile. Tiles that all columns see whole are taken without them.
+//
+// Two kernels, by the columns that a sequence and key head have on average:
+//   up to 64, k_attn_rows: the waves of a workgroup have the same 16 or 32 columns and
+//     take tiles in turn, keys and values straight to registers, as pw_attn.hip does.
+//     Bound by the cache's bytes and, with 32 columns or fp16, by vector instructions:
+//     64 ragged trees of up to 16 tokens, contexts to 4096, 8 key heads x 4, heads of
+//     128 in 16 bits (509 MB) 135 us, in 8 bits (267 MB) 115; heads of 64 in fp16,
+//     window 1500 (156 MB), 45; 8 tokens after 300 (one sequence) 9.0, a chain of
+//     starts, table, tiles and the join of the waves. 64 columns a wave were slower
+//     everywhere (the first 176 us, the second 186): their registers leave one wave
+//     per SIMD, and groups are rarely full.
+//   above, k_attn_tiles: see there.
+// At 68 columns on average (500 rows beside 31 single ones) the second takes 79 us and
+// the first 96; at 64 (the first case above) 142 and 135.
 
 constexpr int kRowsWaves = 4;
 
@@ -35,7 +49,8 @@ __device__ __forceinline__ int clamp64(int64_t v, int lo, int hi) {
 //   shares: each head's items form a line of tiles, cut into equal shares, one per
 //     workgroup, wherever the items end: sequences of unlike lengths leave no workgroup
 //     with more than another. Workgroups that run together read other tiles, so this
-//     is for sequences of few groups of columns.
+//     is for few groups of columns (with k_attn_tiles 24 sequences of 1152 rows took
+//     1632 us, by splits 1206).
 // A part of an item that is not all of it goes to a slot of the workspace: split s of
 // item i to slot (i - whole) n_splits + s, share s's part of item i to slot s + i (one
 // of the two grows from part to part); k_rows_join adds them up. Lengths are read on
@@ -674,6 +689,22 @@ __global__ __launch_bounds__(64 * kRowsWaves, rows_resident(BITS, D, C)) void k_
 // tiles: those come into LDS by direct loads, kStages - 1 tiles ahead, in the order
 // in which they lie in the cache, which is the one that the matrix instructions take
 // them in: 1 KB per instruction, without bank conflicts.
+// The matrix unit is the bound (busy 382 us of 4096 rows after 12288 tokens, 8 key
+// heads x 4 of 128 in bf16, 0.96 TFLOP), with about as much time of vector
+// instructions (exponentials, maxima, roundings) and of LDS reads beside it: 900 us,
+// 1.07 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches 1.27.
+// What counts is waves per SIMD that are at another of the three: C = 2 has 168
+// registers and three waves, 1155 us (24 sequences of 1152 rows after 2048 tokens); with
+// two waves 1360; C = 3 with two waves 1194; C = 4 spills with two waves (3029) and has
+// one without (2729). All columns' maxima are compared before one branch, so that what
+// follows is one block in which products and exponentials mix: 1244 us before.
+// A weight is rounded once to the 16 bits of its product (a second term, as
+// k_attn_rows has it, is half as many products again): in bf16 that leaves as much as
+// the output's own rounding, 2.3e-3 of the result in norm together against 1.7e-3. fp16
+// outputs would show it, so 8-bit caches then take two terms (several prompts of up to
+// 1111 rows, heads of 64: 64 us, with one 51), and fp16 caches, whose exponentials are
+// against the tile's maximum, two where a tile holds weights below 2^-29 of it.
+// 8-bit codes are widened by each wave (1479 us where 16 bits take 1177).
 
 constexpr int kStages = 3;
 template <int BITS, int D>
@@ -1137,6 +1168,9 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
   if (B == 0 || T == 0) return p;
   const int64_t g = n_q_heads / n_kv_heads, rows = (static_cast<int64_t>(T) + B - 1) / B, cols = g * rows;
   p.many = g * T > 64 * static_cast<int64_t>(B);
+  // 32 columns a wave where there are workgroups for the chip, 16 bits: 64 trees of up
+  // to 16 tokens, as above, 135 us, with 16 columns 143; in 8 bits 128 and 116; one tree
+  // of 16 after 8000 tokens 39 and 33.
   const auto items_of = [&](int64_t group) { return g * T / group + (B < T ? B : T); };
   if (p.many) p.col_tiles = kTileCols;
   else p.col_tiles = cols > 16 && bits == 16 && items_of(32) * n_kv_heads >= 256 ? 2 : 1;
@@ -1153,6 +1187,9 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
   if (!p.many) {
     const int64_t resident = 256 * rows_resident(bits, head_dim, p.col_tiles);
     p.least = 32;
+    // Shares where items are few and long: one tree of 16 after 8000 tokens 33 us, a
+    // workgroup per item 60. With an item and a half for every place on the chip the
+    // second is as fast, and needs no join.
     if (items * 2 < resident * 3 && tiles >= 3 * p.least && p.items * tiles < (int64_t(1) << 31) - (1 << 20)) {
       p.n_shares = resident / n_kv_heads > 0 ? resident / n_kv_heads : 1;
       p.slots = (p.n_shares + p.items) * n_kv_heads * group;
@@ -1161,6 +1198,15 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
     const int per_cu = tiles_resident(act, bits, head_dim);
     const int64_t resident = 256 * per_cu, most = tiles / 8;
     int64_t n = 1;
+    // Splits. In a batch lengths may be unlike: pieces of kPiece tiles, and enough of
+    // them to fill the chip: 16 ragged trees of up to 60 tokens after up to 32768 in 8
+    // bits in 1, 2, 4, 6, 12, 16 splits (us) 1434, 798, 574, 401, 372, 377; 500 rows
+    // beside 31 single ones of up to 3000 tokens in 1, 2, 4, 8 splits 102, 79, 83, 88.
+    // Else the cheapest count by rounds of workgroups over the chip, the first rounds
+    // whole: 4096 rows after 12288 tokens, 1024 workgroups on 768 places, unsplit 1003
+    // us, all in 2, 3, 4 splits 937, 946, 965, the last round alone in 2 splits 919; 512
+    // rows after 3000 tokens in 1, 2, 4, 6, 8 splits 113, 74, 58, 59, 68; 4096 rows from
+    // the beginning, spans of all lengths, 151, in 2 splits 197.
     if (B > 1 && items < 2 * resident) {
       const int64_t fill = (resident + items - 1) / items;
       n = (tiles + kPiece - 1) / kPiece;

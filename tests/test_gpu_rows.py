@@ -301,3 +301,28 @@ def test_runs_twice_the_same_and_on_other_streams():
     third = c.attend_rows(q, *args, 4800)
     side.synchronize()
     assert _same(want, again) and _same(want, third)
+
+
+@pytest.mark.parametrize("act,bits", [(BF, 16), (FP, 16), (BF, 8), (FP, 8)])
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+@pytest.mark.parametrize("tree", [None, 2])
+def test_many_columns_under_windows_bounds_and_missing_blocks(act, bits, D, tree):
+    """What the tests above do with few columns per sequence, with more than a
+    workgroup's 128."""
+    seqs = [(0, 70), (40, 33), (700, 100), (0, 0), (300, 1)]
+    for window in (1, 50, 640):
+        _case(seqs, 32, 1, 4, D, act, bits, tree, window=window, seed=window)
+    _case(seqs, 32, 1, 4, D, act, bits, tree, seed=D, missing=[(0, 0, -1), (0, 1, 1 << 29), (1, 1, -3), (2, 5, -1), (2, 24, -1)])
+    _case(seqs, 64, 2, 5, D, act, bits, tree, pad_rows=9, max_len=760, seed=D)
+    _case(seqs, 32, 1, 4, D, act, bits, tree, max_len=90, empty=True, seed=D, scale=-0.2)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("tree", [None, 1])
+def test_shares_over_missing_blocks_and_odd_values(bits, tree):
+    """Few rows after long contexts: equal shares of all tiles, some of them in no
+    block, one whole sequence without any, one that sees values that are no numbers."""
+    seqs = [(5000, 4), (0, 2), (3300, 6), (96, 1), (4000, 9)]
+    _case(seqs, 64, 2, 2, 128, BF, bits, tree, seed=8, missing=[(0, j, -1) for j in range(10, 60)] + [(1, 0, -1), (3, 0, -1), (3, 1, -1)])
+    _case(seqs, 64, 1, 4, 64, FP, bits, tree, seed=9, odd=[(0, 100, (1, 3, math.inf)), (2, 3303, math.nan), (4, 4004, (1, 9, math.nan))])
+    _case(seqs, 64, 1, 4, 64, BF, bits, tree, seed=9, window=3200, max_len=4003)
