@@ -1081,11 +1081,12 @@ __global__ __launch_bounds__(256, tiles_resident(ACT, BITS, D)) void k_attn_tile
   if (split_of(a, 64 * C, lane_id(), &it, &p)) attend_tiles<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
 }
 
-// Joins the parts of 16 columns of an item, four a wave, in a fixed order, and writes
-// the rows of items that no share has.
+// Joins the parts of 4 `per` columns of an item, `per` a wave, in a fixed order (lanes
+// hold four channels, so that heads of 64 take four parts at once, of 128 two), and
+// writes the rows of items that no share has.
 template <int ACT, int D>
-__global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols) {
-  constexpr int kC = D / 64;
+__global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols, int per) {
+  constexpr int kLanes = D <= 64 ? 16 : D <= 128 ? 32 : 64, kAtOnce = 64 / kLanes;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int H = a.kv.n_kv_heads, h = blockIdx.x % H, item = blockIdx.x / H, g = a.n_q_heads / H;
   Item it;
@@ -1100,30 +1101,44 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols) {
   } else if (!item_at(a, item, h, cols, lane, &it)) {
     return;
   } else if (it.tiles > 0) {
-    const int32_t* meta = a.meta + 2 * (static_cast<int64_t>(h) * a.items + item);
+    const int32_t* meta = a.meta + 2 * (h * a.items + item);
     n = meta[1];
     if (n <= 1) return;
-    at0 = (static_cast<int64_t>(h) * (a.n_shares + a.items) + meta[0]) * cols;
+    at0 = (h * (a.n_shares + a.items) + meta[0]) * cols;
   }
-  for (int c = 16 * blockIdx.y + wave; c < 16 * static_cast<int>(blockIdx.y) + 16 && c < it.n_col; c += 4) {
+  const int sub = lane / kLanes, d = 4 * (lane % kLanes);
+  for (int i = 0; i < per; ++i) {
+    const int c = (blockIdx.y * per + i) * 4 + wave;
+    if (c >= it.n_col) return;
     const int64_t at = at0 + c;
     float mx = kNoMax;
     for (int s = lane; s < n; s += 64) mx = fmaxf(mx, a.part_ml[2 * (at + static_cast<int64_t>(s) * cols)]);
 #pragma unroll
     for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-    float acc[kC] = {}, sum = 0.0f;
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    float sum = 0.0f;
 #pragma unroll 4
-    for (int s = 0; s < n; ++s) {
+    for (int s = sub; s < n; s += kAtOnce) {
       const int64_t y = at + static_cast<int64_t>(s) * cols;
       const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * y] - mx);
       sum = fmaf(f, a.part_ml[2 * y + 1], sum);
+      if (d < D) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + y * D + d);
 #pragma unroll
-      for (int j = 0; j < kC; ++j) acc[j] = fmaf(f, a.part_o[y * D + 64 * j + lane], acc[j]);
+        for (int j = 0; j < 4; ++j) acc[j] = fmaf(f, x[j], acc[j]);
+      }
+    }
+#pragma unroll
+    for (int o = kLanes; o < 64; o <<= 1) {
+      sum += __shfl_xor(sum, o);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], o);
     }
     const int64_t row = static_cast<int64_t>(it.row0 + (it.col0 + c) / g) * a.n_q_heads + h * g + (it.col0 + c) % g;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-    for (int j = 0; j < kC; ++j) a.out[row * D + 64 * j + lane] = static_cast<uint16_t>(pack16<ACT>(acc[j] * inv, 0.0f));
+    if (sub == 0 && d < D)
+      *reinterpret_cast<u32x2*>(a.out + row * D + d) =
+          u32x2{pack16<ACT>(acc[0] * inv, acc[1] * inv), pack16<ACT>(acc[2] * inv, acc[3] * inv)};
     if (a.lse && lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
   }
 }
@@ -1145,7 +1160,9 @@ hipError_t launch_d(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 0) return e;
   const int cols = (p.many ? 64 : 16) * p.col_tiles;
-  k_rows_join<ACT, D><<<dim3(static_cast<uint32_t>(rest * a.kv.n_kv_heads), cols / 16), 256, 0, st>>>(a, cols);
+  // (four columns a wave where there are many: the search for the item is most of it)
+  const int per = p.many ? 4 : 1;
+  k_rows_join<ACT, D><<<dim3(static_cast<uint32_t>(rest * a.kv.n_kv_heads), cols / (4 * per)), 256, 0, st>>>(a, cols, per);
   return hipGetLastError();
 }
 
@@ -1170,7 +1187,7 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
   p.many = g * T > 64 * static_cast<int64_t>(B);
   // 32 columns a wave where there are workgroups for the chip, 16 bits: 64 trees of up
   // to 16 tokens, as above, 135 us, with 16 columns 143; in 8 bits 128 and 116; one tree
-  // of 16 after 8000 tokens 39 and 33.
+  // of 16 after 8000 tokens 39 and 33 (27 since its join takes parts side by side).
   const auto items_of = [&](int64_t group) { return g * T / group + (B < T ? B : T); };
   if (p.many) p.col_tiles = kTileCols;
   else p.col_tiles = cols > 16 && bits == 16 && items_of(32) * n_kv_heads >= 256 ? 2 : 1;
@@ -1187,7 +1204,7 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
   if (!p.many) {
     const int64_t resident = 256 * rows_resident(bits, head_dim, p.col_tiles);
     p.least = 32;
-    // Shares where items are few and long: one tree of 16 after 8000 tokens 33 us, a
+    // Shares where items are few and long: one tree of 16 after 8000 tokens 27 us, a
     // workgroup per item 60. With an item and a half for every place on the chip the
     // second is as fast, and needs no join.
     if (items * 2 < resident * 3 && tiles >= 3 * p.least && p.items * tiles < (int64_t(1) << 31) - (1 << 20)) {
