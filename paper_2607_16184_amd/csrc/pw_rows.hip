@@ -1203,54 +1203,50 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
   const int64_t items = p.items * n_kv_heads;
   if (!p.many) {
     const int64_t resident = 256 * rows_resident(bits, head_dim, p.col_tiles);
-    p.least = 32;
+    p.least = 16;
     // Shares where items are few and long: one tree of 16 after 8000 tokens 27 us, a
     // workgroup per item 60. With an item and a half for every place on the chip the
     // second is as fast, and needs no join.
-    if (items * 2 < resident * 3 && tiles >= 3 * p.least && p.items * tiles < (int64_t(1) << 31) - (1 << 20)) {
+    if (items * 2 < resident * 3 && tiles >= 4 * p.least && p.items * tiles < (int64_t(1) << 31) - (1 << 20)) {
       p.n_shares = resident / n_kv_heads > 0 ? resident / n_kv_heads : 1;
       p.slots = (p.n_shares + p.items) * n_kv_heads * group;
     }
-  } else if (tiles >= 24) {
+  } else if (tiles >= 8) {
     const int per_cu = tiles_resident(act, bits, head_dim);
-    const int64_t resident = 256 * per_cu, most = tiles / 8;
+    const int64_t resident = 256 * per_cu, most = tiles / 4;
     int64_t n = 1;
-    // Splits. In a batch lengths may be unlike: pieces of kPiece tiles, and enough of
-    // them to fill the chip: 16 ragged trees of up to 60 tokens after up to 32768 in 8
+    // Splits. In a batch lengths may be unlike: pieces of kPiece tiles at most: 16 ragged trees of up to 60 tokens after up to 32768 in 8
     // bits in 1, 2, 4, 6, 12, 16 splits (us) 1434, 798, 574, 401, 372, 377; 500 rows
     // beside 31 single ones of up to 3000 tokens in 1, 2, 4, 8 splits 102, 79, 83, 88.
-    // Else the cheapest count by rounds of workgroups over the chip, the first rounds
-    // whole: 4096 rows after 12288 tokens, 1024 workgroups on 768 places, unsplit 1003
+    // Within that the cheapest count by rounds of workgroups over the chip, the first
+    // rounds whole where items are many: 4096 rows after 12288 tokens, 1024 workgroups on 768 places, unsplit 1003
     // us, all in 2, 3, 4 splits 937, 946, 965, the last round alone in 2 splits 919; 512
     // rows after 3000 tokens in 1, 2, 4, 6, 8 splits 113, 74, 58, 59, 68; 4096 rows from
     // the beginning, spans of all lengths, 151, in 2 splits 197.
-    if (B > 1 && items < 2 * resident) {
-      const int64_t fill = (resident + items - 1) / items;
-      n = (tiles + kPiece - 1) / kPiece;
-      n = n < fill ? fill : n;
-      n = n < most ? n : most;
-    } else {
-      const double unit = 0.5 * per_cu * head_dim / 128;         // us a tile
-      const double part = group * (head_dim + 2) * 8 / 4e6;      // us to write and read a part
-      const int64_t tri = rows / kTile < tiles ? rows / kTile : tiles;
-      double best = 0.0;
-      for (int64_t k = 1; k <= 32 && k <= most; ++k)
-        for (int64_t whole = 0; whole <= (k > 1 && tri <= tiles / 2 ? items / resident : 0); whole += items / resident > 0 ? items / resident : 1) {
-          const int64_t left = items - whole * resident, rounds = (left * k + resident - 1) / resident;
-          double t = static_cast<double>(whole) * (tiles + 3) + rounds * (static_cast<double>(tiles) / k + 3);
-          if (tri > tiles / 2) {                                 // spans of all lengths: short ones fill the gaps
-            const double mean = (tiles - 0.5 * tri) * items / resident, longest = static_cast<double>(tiles) / k;
-            t = (mean > longest ? mean : longest) + 3 * rounds;
-          }
-          t *= unit;
-          if (k > 1) t += 5.0 + left * k * part;
-          if (best == 0.0 || t < best) {
-            best = t;
-            n = k;
-            p.whole = whole * resident / n_kv_heads;
-          }
+    // A few rows of one sequence take small pieces, too: 7 rows x 16 heads of 256 after 644
+    // tokens in 8 bits, one workgroup, 59 us whole, 28 in five.
+    const bool pieces = B > 1 && items < 2 * resident;
+    const double unit = (per_cu > 2 ? 0.5 * per_cu : 1.0) * head_dim / 128;   // us a tile
+    const double part = group * (head_dim + 2) * 8 / 4e6;        // us to write and read a part
+    const int64_t tri = rows / kTile < tiles ? rows / kTile : tiles, least = pieces ? (tiles + kPiece - 1) / kPiece : 1;
+    const int64_t whole_step = items / resident > 0 ? items / resident : 1;
+    double best = 0.0;
+    for (int64_t k = least; k <= least + 31 && k <= most; ++k)
+      for (int64_t whole = 0; whole <= (k > 1 && !pieces && tri <= tiles / 2 ? items / resident : 0); whole += whole_step) {
+        const int64_t left = items - whole * resident, rounds = (left * k + resident - 1) / resident;
+        double t = static_cast<double>(whole) * (tiles + 3) + rounds * (static_cast<double>(tiles) / k + 3);
+        if (tri > tiles / 2) {                                   // spans of all lengths: short ones fill the gaps
+          const double mean = (tiles - 0.5 * tri) * items / resident, longest = static_cast<double>(tiles) / k;
+          t = (mean > longest ? mean : longest) + 3 * rounds;
         }
-    }
+        t *= unit;
+        if (k > 1) t += 5.0 + left * k * part;
+        if (best == 0.0 || t < best) {
+          best = t;
+          n = k;
+          p.whole = whole * resident / n_kv_heads;
+        }
+      }
     const int64_t per = (tiles + n - 1) / n;
     n = (tiles + per - 1) / per;
     if (n == 1) p.whole = 0;
