@@ -1228,7 +1228,15 @@ RowsPlan rows_plan(int B, int T, int n_q_heads, int n_kv_heads, int head_dim, in
     const bool pieces = B > 1 && items < 2 * resident;
     const double unit = (per_cu > 2 ? 0.5 * per_cu : 1.0) * head_dim / 128;   // us a tile
     const double part = group * (head_dim + 2) * 8 / 4e6;        // us to write and read a part
-    const int64_t tri = rows / kTile < tiles ? rows / kTile : tiles, least = pieces ? (tiles + kPiece - 1) / kPiece : 1;
+    const int64_t tri = rows / kTile < tiles ? rows / kTile : tiles;
+    int64_t least = 1;
+    if (pieces) {
+      // (not more than eight rounds of them: a bound of the lengths far above the lengths
+      // themselves would cost a workspace of as many parts)
+      const int64_t cap = 8 * resident / items;
+      least = (tiles + kPiece - 1) / kPiece;
+      least = least < cap ? least : cap > 1 ? cap : 1;
+    }
     const int64_t whole_step = items / resident > 0 ? items / resident : 1;
     double best = 0.0;
     for (int64_t k = least; k <= least + 31 && k <= most; ++k)

@@ -100,6 +100,14 @@ def test_rows_workspace():
     _refused(pw.PW_EINVAL, _call(pw.pw_attn_rows, ROWS, ROWS_OK, ws=A + 8, wsb=need, **over))
 
 
+def test_rows_workspace_stays_small_for_long_bounds():
+    """A bound of a million tokens for a batch of trees: the parts of a few rounds of
+    workgroups, not of every piece that such lengths would have."""
+    big = _desc(n_kv_heads=8, head_dim=128, block_stride=1 << 22)
+    for B, T in ((16, 960), (64, 1100), (190, 60 * 190), (1, 64), (1, 4096), (64, 64 * 16)):
+        assert pw.pw_attn_rows_workspace(big, B, T, 32, 1 << 20, 0) < 3 << 30
+
+
 KEEP = "c starts table ldt lens B max_len chosen words new st".split()
 KEEP_OK = dict(c=_desc(), starts=A, table=A, ldt=4, lens=A, B=3, max_len=100, chosen=A, words=1, new=A + 64, st=0)
 
