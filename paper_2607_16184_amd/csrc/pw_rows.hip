@@ -706,6 +706,14 @@ __global__ __launch_bounds__(64 * kRowsWaves, rows_resident(BITS, D, C)) void k_
 // against the tile's maximum, two where a tile holds weights below 2^-29 of it.
 // 8-bit codes are widened by each wave (1479 us where 16 bits take 1177).
 
+// The scale is multiplied into the scores in one step with the maximum's subtraction: the
+// largest score keeps what the maximum was rounded by, a tile that is seen in part, where
+// the scale comes first, keeps nothing, and from some 2^24 on that is a factor past fp16's
+// end. So a workgroup with a column whose maximum reaches kFar (the factor then being at
+// most 2^(1/2048)) goes through its tiles once more, the scale first in all of them; and so
+// does one with outputs that are not all numbers.
+constexpr float kFar = 16384.0f;
+
 constexpr int kStages = 3;
 template <int BITS, int D>
 constexpr int stage_bytes() { return 64 * D * BITS / 8 + (BITS == 8 ? 256 : 0); }
@@ -763,8 +771,8 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
     const int64_t t = static_cast<int64_t>(it.t0 + begin + i) * kTile;
     return static_cast<int>(a.table[it.b * a.ld_table + (t >> __builtin_ctz(P))]);
   };
-  int ids = block_of(lane), chunk = 0;
-  uint64_t todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
+  int ids, chunk;
+  uint64_t todo;
   const size_t head_off = static_cast<size_t>(2 * h) * P * D * (BITS / 8);
   const size_t v_off = static_cast<size_t>(P) * D * (BITS / 8);
   const size_t sc_off = static_cast<size_t>(2) * a.kv.n_kv_heads * P * D + static_cast<size_t>(h) * P * 4;
@@ -798,244 +806,266 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
 
   f32x4 o[C][D / 16];
   float m[C], l[C];
+  while (true) {
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) o[c][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    m[c] = kNoMax;
-    l[c] = 0.0f;
-  }
-  int t = fetch(0), t1 = t < 0 ? -1 : fetch(1);
-  int stage = 0;
-  while (t >= 0) {
-    if (t1 >= 0) wait_vm<kMine>();
-    else wait_vm<0>();
-    wg_barrier();                                                // the stage is there, the one before it is read
-    const int t2 = t1 < 0 ? -1 : fetch(stage >= 1 ? stage - 1 : kStages - 1);
-    if (busy) {
-      const uint8_t* sk = lds + stage * stage_bytes<BITS, D>() + 16 * lane;
-      const uint8_t* sv = sk + 2 * kLoads * 1024;
-      const float* sc = reinterpret_cast<const float*>(lds + stage * stage_bytes<BITS, D>() + 4 * kLoads * 1024) + 4 * lg;
-      f32x4 s[C][2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) s[c][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-          const u32x4 kk = ld16(sk + (r * kLoads + j) * 1024);
-          if constexpr (BITS == 16) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(kk, q[c][j], s[c][r]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const u32x4 w = widen8<ACT>(kk[2 * e], kk[2 * e + 1]);
-#pragma unroll
-              for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(w, q[c][2 * j + e], s[c][r]);
-            }
-          }
-        }
-      }
-      f32x4 vs[2];
-      if constexpr (BITS == 8) {
+      for (int j = 0; j < D / 16; ++j) o[c][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      m[c] = kNoMax;
+      l[c] = 0.0f;
+    }
+    ids = block_of(lane);
+    chunk = 0;
+    todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
+    int t = fetch(0), t1 = t < 0 ? -1 : fetch(1);
+    int stage = 0;
+    while (t >= 0) {
+      if (t1 >= 0) wait_vm<kMine>();
+      else wait_vm<0>();
+      wg_barrier();                                                // the stage is there, the one before it is read
+      const int t2 = t1 < 0 ? -1 : fetch(stage >= 1 ? stage - 1 : kStages - 1);
+      if (busy) {
+        const uint8_t* sk = lds + stage * stage_bytes<BITS, D>() + 16 * lane;
+        const uint8_t* sv = sk + 2 * kLoads * 1024;
+        const float* sc = reinterpret_cast<const float*>(lds + stage * stage_bytes<BITS, D>() + 4 * kLoads * 1024) + 4 * lg;
+        f32x4 s[C][2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 16 * r);
-          vs[r] = *reinterpret_cast<const f32x4*>(sc + 32 + 16 * r);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float f = scale2 * ks[e];
+          for (int c = 0; c < C; ++c) s[c][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int c = 0; c < C; ++c) s[c][r][e] *= f;
-          }
-        }
-      }
-      const bool part = t < all_lo || t + kTile > all_hi;        // some column does not see all of it
-      uint32_t seen[C];
-      float mul = BITS == 8 ? 1.0f : scale2;                     // of the scores as they are
-      if (part) {
+          for (int j = 0; j < kLoads; ++j) {
+            const u32x4 kk = ld16(sk + (r * kLoads + j) * 1024);
+            if constexpr (BITS == 16) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          seen[c] = seen_of(a, it, x[c], first_word(a, x[c]), t) >> (4 * lg);
+              for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(kk, q[c][j], s[c][r]);
+            } else {
 #pragma unroll
-          for (int r = 0; r < 2; ++r)
+              for (int e = 0; e < 2; ++e) {
+                const u32x4 w = widen8<ACT>(kk[2 * e], kk[2 * e + 1]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[c][r][e] = (seen[c] >> (16 * r + e)) & 1u ? s[c][r][e] * mul : -INFINITY;
-        }
-        mul = 1.0f;
-      }
-      u32x4 p_hi[C], p_two[C];
-      float share[C], base[C], top[C];
-      bool low = false;                                          // fp16: weights that one term does not hold
-      bool raise = false;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        top[c] = s[c][0][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top[c] = fmaxf(top[c], s[c][e / 4][e & 3]);
-        top[c] *= mul;
-        if constexpr (kByTile) {
-          top[c] = fmaxf(column_max(top[c]), kNoMax);
-          raise |= top[c] > m[c];
-        } else {
-          raise |= top[c] > m[c] + kSlack;
-        }
-      }
-      if (__any(raise)) {                                        // (all columns at once: what follows is one piece)
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const float m_new = fmaxf(m[c], kByTile ? top[c] : column_max(top[c]));
-          const float f = __builtin_amdgcn_exp2f(m[c] - m_new);
-          m[c] = m_new;
-          l[c] *= f;
-#pragma unroll
-          for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[c][j][e] *= f;
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        base[c] = kByTile ? top[c] : m[c];
-        share[c] = kByTile ? __builtin_amdgcn_exp2f(top[c] - m[c]) : 1.0f;
-        float sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          float p[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int r = w / 2, y = 2 * (w & 1) + e;
-            p[e] = __builtin_amdgcn_exp2f(fmaf(s[c][r][y], mul, -base[c]));
-            sum += p[e];
-            if constexpr (BITS == 8) {
-              p[e] *= vs[r][y];
-              if (part) p[e] = (seen[c] >> (16 * r + y)) & 1u ? p[e] : 0.0f;
-            }
-            if constexpr (kByTile) {
-              p[e] *= kLift;
-              low |= p[e] < 0x1p-14f;
-              s[c][r][y] = p[e];
-            }
-          }
-          p_hi[c][w] = pack16<kPv>(p[0], p[1]);
-          if constexpr (kTwo)
-            p_two[c][w] = pack16<kPv>(p[0] - val16(p_hi[c][w] & 0xFFFFu, kPv), p[1] - val16(p_hi[c][w] >> 16, kPv));
-        }
-        l[c] = fmaf(share[c], sum, l[c]);
-        if constexpr (kByTile) share[c] *= 1.0f / kLift;
-      }
-      uint32_t keep[2][2], any = 0u;
-      if (part) {
-        // values that no column may see are left out, whatever their bits, and those
-        // that are no numbers for now
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          keep[r][0] = keep[r][1] = 0u;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int tok = t + 16 * r + 4 * lg + e;
-            const bool in = tok >= it.lo && tok < it.hi;
-            if constexpr (BITS == 8) keep[r][0] |= in ? 0xFFu << (8 * e) : 0u;
-            else keep[r][e / 2] |= in ? 0xFFFFu << (16 * (e & 1)) : 0u;
-          }
-        }
-      }
-      const auto values = [&](int j) {                           // the 1 KB piece j of the values
-        u32x4 v = ld16(sv + j * 1024);
-        if (part) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            v[w] &= BITS == 8 ? keep[w & 1][0] : keep[w / 2][w & 1];
-            const uint32_t z = odd_parts<BITS, kPv>(v[w]);
-            any |= z;
-            v[w] &= ~z;
-          }
-        }
-        return v;
-      };
-      if constexpr (kByTile) {
-        const bool two = __any(low);
-        u32x4 p_lo[C];
-        if (two) {
-#pragma unroll
-          for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-              p_lo[c][w] = pack16<kPv>((s[c][w / 2][2 * (w & 1)] - val16(p_hi[c][w] & 0xFFFFu, kPv)) * kLow,
-                                       (s[c][w / 2][2 * (w & 1) + 1] - val16(p_hi[c][w] >> 16, kPv)) * kLow);
-        }
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-          const u32x4 v = values(j);
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
-            f32x4 hi = mma<kPv>(v, p_hi[c], zero);
-            if (two) {
-              const f32x4 lo = mma<kPv>(v, p_lo[c], zero);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) hi[e] = fabsf(hi[e]) < INFINITY ? fmaf(lo[e], 1.0f / kLow, hi[e]) : hi[e];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[c][j][e] = fmaf(share[c], hi[e], o[c][j][e]);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 2 * kLoads; ++j) {
-          const u32x4 v = values(j);
-          if constexpr (BITS == 16) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) o[c][j] = mma<kPv>(v, p_hi[c], o[c][j]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const u32x4 w = widen8<kPv>(v[2 * e], v[2 * e + 1]);
-#pragma unroll
-              for (int c = 0; c < C; ++c) {
-                o[c][2 * j + e] = mma<kPv>(w, p_hi[c], o[c][2 * j + e]);
-                if constexpr (kTwo) o[c][2 * j + e] = mma<kPv>(w, p_two[c], o[c][2 * j + e]);
+                for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(w, q[c][2 * j + e], s[c][r]);
               }
             }
           }
         }
-      }
-      if (part && __any(any != 0u)) {
-        // one by one, to the columns that see them
-        const uint8_t* vm = lds + stage * stage_bytes<BITS, D>() + 2 * kLoads * 1024;
+        f32x4 vs[2];
+        if constexpr (BITS == 8) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 16 * r);
+            vs[r] = *reinterpret_cast<const f32x4*>(sc + 32 + 16 * r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float f = scale2 * ks[e];
+#pragma unroll
+              for (int c = 0; c < C; ++c) s[c][r][e] *= f;
+            }
+          }
+        }
+        const bool part = t < all_lo || t + kTile > all_hi;          // some column does not see all of it
+        uint32_t seen[C];
+        float mul = BITS == 8 ? 1.0f : scale2;                     // of the scores as they are
+        if (part) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            seen[c] = seen_of(a, it, x[c], first_word(a, x[c]), t) >> (4 * lg);
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[c][r][e] = (seen[c] >> (16 * r + e)) & 1u ? s[c][r][e] * mul : -INFINITY;
+          }
+          mul = 1.0f;
+        }
+        u32x4 p_hi[C], p_two[C];
+        float share[C], base[C], top[C];
+        bool low = false;                                          // fp16: weights that one term does not hold
+        bool raise = false;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          for (int i = 0; i < kTile; ++i) {
-            uint32_t w = p_hi[c][0];
-            const int at = 2 * (i / 16) + i % 4 / 2;             // token i's word in lanes 16 (i / 4 mod 4) ..
+          top[c] = s[c][0][0];
 #pragma unroll
-            for (int e = 1; e < 4; ++e) w = at == e ? p_hi[c][e] : w;
-            w = static_cast<uint32_t>(__shfl(static_cast<int>(w), 16 * (i / 4 % 4) + col));
-            const uint32_t on = static_cast<uint32_t>(__shfl(static_cast<int>(seen[c]), col)) >> i & 1u;   // (bits of lane group 0: all)
-            const float p = val16(w >> (16 * (i & 1)), kPv) * share[c];
+          for (int e = 1; e < 8; ++e) top[c] = fmaxf(top[c], s[c][e / 4][e & 3]);
+          top[c] *= mul;
+          if constexpr (kByTile) {
+            top[c] = fmaxf(column_max(top[c]), kNoMax);
+            raise |= top[c] > m[c];
+          } else {
+            raise |= top[c] > m[c] + kSlack;
+          }
+        }
+        if (__any(raise)) {                                        // (all columns at once: what follows is one piece)
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const float m_new = fmaxf(m[c], kByTile ? top[c] : column_max(top[c]));
+            const float f = __builtin_amdgcn_exp2f(m[c] - m_new);
+            m[c] = m_new;
+            l[c] *= f;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int place = 16 * (16 * (i / 4 % 4) + 4 * lg + e);
-                float y = 0.0f;
-                if constexpr (BITS == 16) {
-                  const uint32_t b = *reinterpret_cast<const any_u16*>(vm + j * 1024 + place + 2 * (4 * (i / 16) + i % 4));
-                  if (odd_parts<16, kPv>(b) & 0xFFFFu) y = val16(b, kPv);
-                } else {
-                  const uint32_t b = vm[(j / 2) * 1024 + place + 8 * (j & 1) + 4 * (i / 16) + i % 4];
-                  if ((b & 0x7Fu) == 0x7Fu) y = __builtin_nanf("");
-                }
-                if (on && y != 0.0f) o[c][j][e] = fmaf(p, y, o[c][j][e]);
+              for (int e = 0; e < 4; ++e) o[c][j][e] *= f;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          base[c] = kByTile ? top[c] : m[c];
+          share[c] = kByTile ? __builtin_amdgcn_exp2f(top[c] - m[c]) : 1.0f;
+          float sum = 0.0f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            float p[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int r = w / 2, y = 2 * (w & 1) + e;
+              p[e] = __builtin_amdgcn_exp2f(fmaf(s[c][r][y], mul, -base[c]));
+              sum += p[e];
+              if constexpr (BITS == 8) {
+                p[e] *= vs[r][y];
+                if (part) p[e] = (seen[c] >> (16 * r + y)) & 1u ? p[e] : 0.0f;
               }
+              if constexpr (kByTile) {
+                p[e] *= kLift;
+                low |= p[e] < 0x1p-14f;
+                s[c][r][y] = p[e];
+              }
+            }
+            p_hi[c][w] = pack16<kPv>(p[0], p[1]);
+            if constexpr (kTwo)
+              p_two[c][w] = pack16<kPv>(p[0] - val16(p_hi[c][w] & 0xFFFFu, kPv), p[1] - val16(p_hi[c][w] >> 16, kPv));
+          }
+          l[c] = fmaf(share[c], sum, l[c]);
+          if constexpr (kByTile) share[c] *= 1.0f / kLift;
+        }
+        uint32_t keep[2][2], any = 0u;
+        if (part) {
+          // values that no column may see are left out, whatever their bits, and those
+          // that are no numbers for now
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            keep[r][0] = keep[r][1] = 0u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int tok = t + 16 * r + 4 * lg + e;
+              const bool in = tok >= it.lo && tok < it.hi;
+              if constexpr (BITS == 8) keep[r][0] |= in ? 0xFFu << (8 * e) : 0u;
+              else keep[r][e / 2] |= in ? 0xFFFFu << (16 * (e & 1)) : 0u;
+            }
+          }
+        }
+        const auto values = [&](int j) {                           // the 1 KB piece j of the values
+          u32x4 v = ld16(sv + j * 1024);
+          if (part) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              v[w] &= BITS == 8 ? keep[w & 1][0] : keep[w / 2][w & 1];
+              const uint32_t z = odd_parts<BITS, kPv>(v[w]);
+              any |= z;
+              v[w] &= ~z;
+            }
+          }
+          return v;
+        };
+        if constexpr (kByTile) {
+          const bool two = __any(low);
+          u32x4 p_lo[C];
+          if (two) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                p_lo[c][w] = pack16<kPv>((s[c][w / 2][2 * (w & 1)] - val16(p_hi[c][w] & 0xFFFFu, kPv)) * kLow,
+                                         (s[c][w / 2][2 * (w & 1) + 1] - val16(p_hi[c][w] >> 16, kPv)) * kLow);
+          }
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) {
+            const u32x4 v = values(j);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+              const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+              f32x4 hi = mma<kPv>(v, p_hi[c], zero);
+              if (two) {
+                const f32x4 lo = mma<kPv>(v, p_lo[c], zero);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) hi[e] = fabsf(hi[e]) < INFINITY ? fmaf(lo[e], 1.0f / kLow, hi[e]) : hi[e];
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[c][j][e] = fmaf(share[c], hi[e], o[c][j][e]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2 * kLoads; ++j) {
+            const u32x4 v = values(j);
+            if constexpr (BITS == 16) {
+#pragma unroll
+              for (int c = 0; c < C; ++c) o[c][j] = mma<kPv>(v, p_hi[c], o[c][j]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const u32x4 w = widen8<kPv>(v[2 * e], v[2 * e + 1]);
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                  o[c][2 * j + e] = mma<kPv>(w, p_hi[c], o[c][2 * j + e]);
+                  if constexpr (kTwo) o[c][2 * j + e] = mma<kPv>(w, p_two[c], o[c][2 * j + e]);
+                }
+              }
+            }
+          }
+        }
+        if (part && __any(any != 0u)) {
+          // one by one, to the columns that see them
+          const uint8_t* vm = lds + stage * stage_bytes<BITS, D>() + 2 * kLoads * 1024;
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            for (int i = 0; i < kTile; ++i) {
+              uint32_t w = p_hi[c][0];
+              const int at = 2 * (i / 16) + i % 4 / 2;             // token i's word in lanes 16 (i / 4 mod 4) ..
+#pragma unroll
+              for (int e = 1; e < 4; ++e) w = at == e ? p_hi[c][e] : w;
+              w = static_cast<uint32_t>(__shfl(static_cast<int>(w), 16 * (i / 4 % 4) + col));
+              const uint32_t on = static_cast<uint32_t>(__shfl(static_cast<int>(seen[c]), col)) >> i & 1u;   // (bits of lane group 0: all)
+              const float p = val16(w >> (16 * (i & 1)), kPv) * share[c];
+#pragma unroll
+              for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int place = 16 * (16 * (i / 4 % 4) + 4 * lg + e);
+                  float y = 0.0f;
+                  if constexpr (BITS == 16) {
+                    const uint32_t b = *reinterpret_cast<const any_u16*>(vm + j * 1024 + place + 2 * (4 * (i / 16) + i % 4));
+                    if (odd_parts<16, kPv>(b) & 0xFFFFu) y = val16(b, kPv);
+                  } else {
+                    const uint32_t b = vm[(j / 2) * 1024 + place + 8 * (j & 1) + 4 * (i / 16) + i % 4];
+                    if ((b & 0x7Fu) == 0x7Fu) y = __builtin_nanf("");
+                  }
+                  if (on && y != 0.0f) o[c][j][e] = fmaf(p, y, o[c][j][e]);
+                }
+            }
           }
         }
       }
+      t = t1;
+      t1 = t2;
+      stage = stage + 1 < kStages ? stage + 1 : 0;
     }
-    t = t1;
-    t1 = t2;
-    stage = stage + 1 < kStages ? stage + 1 : 0;
+    if (BITS == 8 || all_lo == INT32_MAX) break;
+    bool bad = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      bad |= fabsf(m[c]) >= kFar && m[c] > kNoMax;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad |= !(fabsf(o[c][j][e]) < INFINITY);
+    }
+    __syncthreads();                                             // the last stage is read
+    if (__any(bad)) lds[wave] = 1u;
+    else lds[wave] = 0u;
+    __syncthreads();
+    if ((lds[0] | lds[1] | lds[2] | lds[3]) == 0u) break;        // (of all four: they share the tiles)
+    all_lo = INT32_MAX;                                          // all tiles as if seen in part
+    __syncthreads();                                             // the votes are read
   }
   if (!busy) return;
 #pragma unroll
