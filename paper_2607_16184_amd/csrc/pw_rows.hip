@@ -282,9 +282,12 @@ __device__ __forceinline__ uint32_t seen_of(const RowsArgs& a, const Item& it, c
 
 // Values that are no numbers would enter columns that do not see them (0 x NaN), so
 // in tiles that some columns see in part they are taken out of the product, and
-// added one by one to the columns that do. Where all columns see an infinity, the
-// product of a weight in two terms is none (inf - inf): a wave whose outputs are not
-// all numbers goes through its tiles once more, with that done in all of them.
+// added one by one to the columns that do, as they are: no weight but that of a score of
+// -infinity is nothing, however small the exponential came out. Where all columns see an
+// infinity, a product is none if the weight came out as 0, or is in two terms (inf - inf),
+// and so is what a later maximum scales down by 0: a wave (of k_attn_tiles a workgroup)
+// whose outputs are not all numbers goes through its tiles once more, with that done in
+// all of them and factors that are not 0.
 template <int BITS, int PV>
 __device__ __forceinline__ uint32_t odd_parts(uint32_t w) {      // ones over the parts of a word that are no numbers
   if constexpr (BITS == 8) {
@@ -295,6 +298,10 @@ __device__ __forceinline__ uint32_t odd_parts(uint32_t w) {      // ones over th
     return ((w & kExp) == kExp ? 0xFFFFu : 0u) | (((w >> 16) & kExp) == kExp ? 0xFFFF0000u : 0u);
   }
 }
+
+// A factor of what is there, at least the smallest number in place of 0: infinities stay,
+// and all else is nothing beside a weight of 1.
+constexpr float kLeast = 0x1p-149f;
 
 template <int D>
 struct RowsLds {
@@ -518,13 +525,19 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
           }
         }
         if (raise) {
+          if (BITS == 16 && careful) f = fmaxf(f, kLeast);
           l[c] *= f;
 #pragma unroll
           for (int j = 0; j < D / 16; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[c][j][e] *= f;
         }
-        float sum = 0.0f, pr[8];
+        uint32_t some = 0u;                                        // of the lane's tokens, those with a weight
+        if (odd) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) some |= s[c][e / 4][e & 3] > -INFINITY ? 1u << e : 0u;
+        }
+        float sum = 0.0f;
         u32x4 p_hi, p_lo;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -532,7 +545,7 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int r = w / 2, y = 2 * (w & 1) + e;
-            pr[2 * w + e] = p[e] = __builtin_amdgcn_exp2f(s[c][r][y] - base);
+            p[e] = __builtin_amdgcn_exp2f(s[c][r][y] - base);
             sum += p[e];
             if constexpr (BITS == 8) {
               p[e] *= vs[r][y];
@@ -550,10 +563,7 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
           const uint8_t* vm = values_at(id, t);
           for (int i = 0; i < kTile; ++i) {
             const int at = 4 * (i / 16) + i % 4;                   // token i's place in lanes 16 (i / 4 mod 4) ..
-            float p = pr[0];
-#pragma unroll
-            for (int e = 1; e < 8; ++e) p = at == e ? pr[e] : p;
-            p = __shfl(p, 16 * (i / 4 % 4) + col) * share;
+            const bool none = !(__shfl(static_cast<int>(some), 16 * (i / 4 % 4) + col) >> at & 1);
             const bool on = (seen >> i) & 1u;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j)
@@ -568,7 +578,7 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
                   const uint32_t w = vm[(j / 2) * 1024 + place + 8 * (j & 1) + 4 * (i / 16) + i % 4];
                   if ((w & 0x7Fu) == 0x7Fu) y = __builtin_nanf("");
                 }
-                if (on && y != 0.0f) o[c][j][e] = fmaf(p, y, o[c][j][e]);
+                if (on && y != 0.0f) o[c][j][e] += none ? __builtin_nanf("") : y;
               }
           }
         }
@@ -632,7 +642,7 @@ __device__ __forceinline__ void attend_rows(const RowsArgs& a, RowsLds<D>& lds, 
       float sum = 0.0f;
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const float f = __builtin_amdgcn_exp2f(lds.m[w][y] - mx);
+        const float f = fmaxf(__builtin_amdgcn_exp2f(lds.m[w][y] - mx), kLeast);
         sum = fmaf(f, lds.l[w][y], sum);
         const f32x4 z = *reinterpret_cast<const f32x4*>(&lds.o[w][y][d]);
 #pragma unroll
@@ -718,15 +728,18 @@ constexpr int kStages = 3;
 template <int BITS, int D>
 constexpr int stage_bytes() { return 64 * D * BITS / 8 + (BITS == 8 ? 256 : 0); }
 
-template <int ACT, int BITS, int D, int C>
-__device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, const Item& it, int begin, int end, bool whole,
-                                             int64_t slot) {
+// False: not done, outputs or a maximum want the careful form. (The same for all waves.)
+template <int ACT, int BITS, int D, int C, bool CAREFUL>
+__device__ __forceinline__ bool attend_tiles(const RowsArgs& a, uint8_t* lds, int* again, const Item& it, int begin, int end,
+                                             bool whole, int64_t slot) {
   constexpr int kPv = BITS == 8 ? PW_BF16 : ACT;
   constexpr bool kByTile = kPv == PW_F16;
   constexpr bool kTwo = BITS == 8 && ACT == PW_F16;   // weights in two terms: fp16 outputs show what one bf16 leaves
   constexpr int kLoads = D * BITS / 8 * 16 / 1024;    // 1 KB pieces of 16 tokens' keys
   constexpr int kMine = kLoads + (BITS == 8 ? 1 : 0); // loads of a wave for a tile: a quarter of the pieces, the scales
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  int lane = lane_id();
+  if constexpr (CAREFUL) asm volatile("" : "+v"(lane));         // (nothing of the other form is kept for this one)
   const int col = lane & 15, lg = lane >> 4;
   const int P = a.kv.block_tokens, h = it.h;
   const int g = a.n_q_heads / a.kv.n_kv_heads;
@@ -806,268 +819,268 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
 
   f32x4 o[C][D / 16];
   float m[C], l[C];
-  while (true) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
+  for (int c = 0; c < C; ++c) {
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) o[c][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      m[c] = kNoMax;
-      l[c] = 0.0f;
-    }
-    ids = block_of(lane);
-    chunk = 0;
-    todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
-    int t = fetch(0), t1 = t < 0 ? -1 : fetch(1);
-    int stage = 0;
-    while (t >= 0) {
-      if (t1 >= 0) wait_vm<kMine>();
-      else wait_vm<0>();
-      wg_barrier();                                                // the stage is there, the one before it is read
-      const int t2 = t1 < 0 ? -1 : fetch(stage >= 1 ? stage - 1 : kStages - 1);
-      if (busy) {
-        const uint8_t* sk = lds + stage * stage_bytes<BITS, D>() + 16 * lane;
-        const uint8_t* sv = sk + 2 * kLoads * 1024;
-        const float* sc = reinterpret_cast<const float*>(lds + stage * stage_bytes<BITS, D>() + 4 * kLoads * 1024) + 4 * lg;
-        f32x4 s[C][2];
+    for (int j = 0; j < D / 16; ++j) o[c][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    m[c] = kNoMax;
+    l[c] = 0.0f;
+  }
+  ids = block_of(lane);
+  chunk = 0;
+  todo = __ballot(ids >= 0 && ids < a.kv.n_blocks);
+  int t = fetch(0), t1 = t < 0 ? -1 : fetch(1);
+  int stage = 0;
+  while (t >= 0) {
+    if (t1 >= 0) wait_vm<kMine>();
+    else wait_vm<0>();
+    wg_barrier();                                                // the stage is there, the one before it is read
+    const int t2 = t1 < 0 ? -1 : fetch(stage >= 1 ? stage - 1 : kStages - 1);
+    if (busy) {
+      const uint8_t* sk = lds + stage * stage_bytes<BITS, D>() + 16 * lane;
+      const uint8_t* sv = sk + 2 * kLoads * 1024;
+      const float* sc = reinterpret_cast<const float*>(lds + stage * stage_bytes<BITS, D>() + 4 * kLoads * 1024) + 4 * lg;
+      f32x4 s[C][2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+      for (int r = 0; r < 2; ++r) {
 #pragma unroll
-          for (int c = 0; c < C; ++c) s[c][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int c = 0; c < C; ++c) s[c][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int j = 0; j < kLoads; ++j) {
-            const u32x4 kk = ld16(sk + (r * kLoads + j) * 1024);
-            if constexpr (BITS == 16) {
+        for (int j = 0; j < kLoads; ++j) {
+          const u32x4 kk = ld16(sk + (r * kLoads + j) * 1024);
+          if constexpr (BITS == 16) {
 #pragma unroll
-              for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(kk, q[c][j], s[c][r]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const u32x4 w = widen8<ACT>(kk[2 * e], kk[2 * e + 1]);
-#pragma unroll
-                for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(w, q[c][2 * j + e], s[c][r]);
-              }
-            }
-          }
-        }
-        f32x4 vs[2];
-        if constexpr (BITS == 8) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 16 * r);
-            vs[r] = *reinterpret_cast<const f32x4*>(sc + 32 + 16 * r);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float f = scale2 * ks[e];
-#pragma unroll
-              for (int c = 0; c < C; ++c) s[c][r][e] *= f;
-            }
-          }
-        }
-        const bool part = t < all_lo || t + kTile > all_hi;          // some column does not see all of it
-        uint32_t seen[C];
-        float mul = BITS == 8 ? 1.0f : scale2;                     // of the scores as they are
-        if (part) {
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            seen[c] = seen_of(a, it, x[c], first_word(a, x[c]), t) >> (4 * lg);
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[c][r][e] = (seen[c] >> (16 * r + e)) & 1u ? s[c][r][e] * mul : -INFINITY;
-          }
-          mul = 1.0f;
-        }
-        u32x4 p_hi[C], p_two[C];
-        float share[C], base[C], top[C];
-        bool low = false;                                          // fp16: weights that one term does not hold
-        bool raise = false;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          top[c] = s[c][0][0];
-#pragma unroll
-          for (int e = 1; e < 8; ++e) top[c] = fmaxf(top[c], s[c][e / 4][e & 3]);
-          top[c] *= mul;
-          if constexpr (kByTile) {
-            top[c] = fmaxf(column_max(top[c]), kNoMax);
-            raise |= top[c] > m[c];
+            for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(kk, q[c][j], s[c][r]);
           } else {
-            raise |= top[c] > m[c] + kSlack;
-          }
-        }
-        if (__any(raise)) {                                        // (all columns at once: what follows is one piece)
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            const float m_new = fmaxf(m[c], kByTile ? top[c] : column_max(top[c]));
-            const float f = __builtin_amdgcn_exp2f(m[c] - m_new);
-            m[c] = m_new;
-            l[c] *= f;
-#pragma unroll
-            for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[c][j][e] *= f;
-          }
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          base[c] = kByTile ? top[c] : m[c];
-          share[c] = kByTile ? __builtin_amdgcn_exp2f(top[c] - m[c]) : 1.0f;
-          float sum = 0.0f;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            float p[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int r = w / 2, y = 2 * (w & 1) + e;
-              p[e] = __builtin_amdgcn_exp2f(fmaf(s[c][r][y], mul, -base[c]));
-              sum += p[e];
-              if constexpr (BITS == 8) {
-                p[e] *= vs[r][y];
-                if (part) p[e] = (seen[c] >> (16 * r + y)) & 1u ? p[e] : 0.0f;
-              }
-              if constexpr (kByTile) {
-                p[e] *= kLift;
-                low |= p[e] < 0x1p-14f;
-                s[c][r][y] = p[e];
-              }
-            }
-            p_hi[c][w] = pack16<kPv>(p[0], p[1]);
-            if constexpr (kTwo)
-              p_two[c][w] = pack16<kPv>(p[0] - val16(p_hi[c][w] & 0xFFFFu, kPv), p[1] - val16(p_hi[c][w] >> 16, kPv));
-          }
-          l[c] = fmaf(share[c], sum, l[c]);
-          if constexpr (kByTile) share[c] *= 1.0f / kLift;
-        }
-        uint32_t keep[2][2], any = 0u;
-        if (part) {
-          // values that no column may see are left out, whatever their bits, and those
-          // that are no numbers for now
+              const u32x4 w = widen8<ACT>(kk[2 * e], kk[2 * e + 1]);
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            keep[r][0] = keep[r][1] = 0u;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int tok = t + 16 * r + 4 * lg + e;
-              const bool in = tok >= it.lo && tok < it.hi;
-              if constexpr (BITS == 8) keep[r][0] |= in ? 0xFFu << (8 * e) : 0u;
-              else keep[r][e / 2] |= in ? 0xFFFFu << (16 * (e & 1)) : 0u;
-            }
-          }
-        }
-        const auto values = [&](int j) {                           // the 1 KB piece j of the values
-          u32x4 v = ld16(sv + j * 1024);
-          if (part) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              v[w] &= BITS == 8 ? keep[w & 1][0] : keep[w / 2][w & 1];
-              const uint32_t z = odd_parts<BITS, kPv>(v[w]);
-              any |= z;
-              v[w] &= ~z;
-            }
-          }
-          return v;
-        };
-        if constexpr (kByTile) {
-          const bool two = __any(low);
-          u32x4 p_lo[C];
-          if (two) {
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-              for (int w = 0; w < 4; ++w)
-                p_lo[c][w] = pack16<kPv>((s[c][w / 2][2 * (w & 1)] - val16(p_hi[c][w] & 0xFFFFu, kPv)) * kLow,
-                                         (s[c][w / 2][2 * (w & 1) + 1] - val16(p_hi[c][w] >> 16, kPv)) * kLow);
-          }
-#pragma unroll
-          for (int j = 0; j < D / 16; ++j) {
-            const u32x4 v = values(j);
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-              const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
-              f32x4 hi = mma<kPv>(v, p_hi[c], zero);
-              if (two) {
-                const f32x4 lo = mma<kPv>(v, p_lo[c], zero);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) hi[e] = fabsf(hi[e]) < INFINITY ? fmaf(lo[e], 1.0f / kLow, hi[e]) : hi[e];
-              }
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[c][j][e] = fmaf(share[c], hi[e], o[c][j][e]);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 2 * kLoads; ++j) {
-            const u32x4 v = values(j);
-            if constexpr (BITS == 16) {
-#pragma unroll
-              for (int c = 0; c < C; ++c) o[c][j] = mma<kPv>(v, p_hi[c], o[c][j]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const u32x4 w = widen8<kPv>(v[2 * e], v[2 * e + 1]);
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                  o[c][2 * j + e] = mma<kPv>(w, p_hi[c], o[c][2 * j + e]);
-                  if constexpr (kTwo) o[c][2 * j + e] = mma<kPv>(w, p_two[c], o[c][2 * j + e]);
-                }
-              }
-            }
-          }
-        }
-        if (part && __any(any != 0u)) {
-          // one by one, to the columns that see them
-          const uint8_t* vm = lds + stage * stage_bytes<BITS, D>() + 2 * kLoads * 1024;
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            for (int i = 0; i < kTile; ++i) {
-              uint32_t w = p_hi[c][0];
-              const int at = 2 * (i / 16) + i % 4 / 2;             // token i's word in lanes 16 (i / 4 mod 4) ..
-#pragma unroll
-              for (int e = 1; e < 4; ++e) w = at == e ? p_hi[c][e] : w;
-              w = static_cast<uint32_t>(__shfl(static_cast<int>(w), 16 * (i / 4 % 4) + col));
-              const uint32_t on = static_cast<uint32_t>(__shfl(static_cast<int>(seen[c]), col)) >> i & 1u;   // (bits of lane group 0: all)
-              const float p = val16(w >> (16 * (i & 1)), kPv) * share[c];
-#pragma unroll
-              for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int place = 16 * (16 * (i / 4 % 4) + 4 * lg + e);
-                  float y = 0.0f;
-                  if constexpr (BITS == 16) {
-                    const uint32_t b = *reinterpret_cast<const any_u16*>(vm + j * 1024 + place + 2 * (4 * (i / 16) + i % 4));
-                    if (odd_parts<16, kPv>(b) & 0xFFFFu) y = val16(b, kPv);
-                  } else {
-                    const uint32_t b = vm[(j / 2) * 1024 + place + 8 * (j & 1) + 4 * (i / 16) + i % 4];
-                    if ((b & 0x7Fu) == 0x7Fu) y = __builtin_nanf("");
-                  }
-                  if (on && y != 0.0f) o[c][j][e] = fmaf(p, y, o[c][j][e]);
-                }
+              for (int c = 0; c < C; ++c) s[c][r] = mma<ACT>(w, q[c][2 * j + e], s[c][r]);
             }
           }
         }
       }
-      t = t1;
-      t1 = t2;
-      stage = stage + 1 < kStages ? stage + 1 : 0;
+      f32x4 vs[2];
+      if constexpr (BITS == 8) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 16 * r);
+          vs[r] = *reinterpret_cast<const f32x4*>(sc + 32 + 16 * r);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float f = scale2 * ks[e];
+#pragma unroll
+            for (int c = 0; c < C; ++c) s[c][r][e] *= f;
+          }
+        }
+      }
+      const bool part = CAREFUL || t < all_lo || t + kTile > all_hi;   // some column may not see all of it
+      uint32_t seen[C];
+      uint32_t some[C];                                          // CAREFUL: of the lane's tokens, those with a weight
+      float mul = BITS == 8 ? 1.0f : scale2;                     // of the scores as they are
+      if (part) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          seen[c] = seen_of(a, it, x[c], first_word(a, x[c]), t) >> (4 * lg);
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[c][r][e] = (seen[c] >> (16 * r + e)) & 1u ? s[c][r][e] * mul : -INFINITY;
+          if constexpr (CAREFUL) {
+            some[c] = 0u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) some[c] |= s[c][e / 4][e & 3] > -INFINITY ? 1u << e : 0u;
+          }
+        }
+        mul = 1.0f;
+      }
+      u32x4 p_hi[C], p_two[C];
+      float share[C], base[C], top[C];
+      bool low = false;                                          // fp16: weights that one term does not hold
+      bool raise = false;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        top[c] = s[c][0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top[c] = fmaxf(top[c], s[c][e / 4][e & 3]);
+        top[c] *= mul;
+        if constexpr (kByTile) {
+          top[c] = fmaxf(column_max(top[c]), kNoMax);
+          raise |= top[c] > m[c];
+        } else {
+          raise |= top[c] > m[c] + kSlack;
+        }
+      }
+      if (__any(raise)) {                                        // (all columns at once: what follows is one piece)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const float m_new = fmaxf(m[c], kByTile ? top[c] : column_max(top[c]));
+          const float f = fmaxf(__builtin_amdgcn_exp2f(m[c] - m_new), CAREFUL ? kLeast : 0.0f);
+          m[c] = m_new;
+          l[c] *= f;
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][j][e] *= f;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        base[c] = kByTile ? top[c] : m[c];
+        share[c] = kByTile ? __builtin_amdgcn_exp2f(top[c] - m[c]) : 1.0f;
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          float p[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = w / 2, y = 2 * (w & 1) + e;
+            p[e] = __builtin_amdgcn_exp2f(fmaf(s[c][r][y], mul, -base[c]));
+            sum += p[e];
+            if constexpr (BITS == 8) {
+              p[e] *= vs[r][y];
+              if (part) p[e] = (seen[c] >> (16 * r + y)) & 1u ? p[e] : 0.0f;
+            }
+            if constexpr (kByTile) {
+              p[e] *= kLift;
+              low |= p[e] < 0x1p-14f;
+              s[c][r][y] = p[e];
+            }
+          }
+          p_hi[c][w] = pack16<kPv>(p[0], p[1]);
+          if constexpr (kTwo)
+            p_two[c][w] = pack16<kPv>(p[0] - val16(p_hi[c][w] & 0xFFFFu, kPv), p[1] - val16(p_hi[c][w] >> 16, kPv));
+        }
+        l[c] = fmaf(share[c], sum, l[c]);
+        if constexpr (kByTile) share[c] *= 1.0f / kLift;
+      }
+      uint32_t keep[2][2], any = 0u;
+      if (part) {
+        // values that no column may see are left out, whatever their bits, and those
+        // that are no numbers for now
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          keep[r][0] = keep[r][1] = 0u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = t + 16 * r + 4 * lg + e;
+            const bool in = tok >= it.lo && tok < it.hi;
+            if constexpr (BITS == 8) keep[r][0] |= in ? 0xFFu << (8 * e) : 0u;
+            else keep[r][e / 2] |= in ? 0xFFFFu << (16 * (e & 1)) : 0u;
+          }
+        }
+      }
+      const auto values = [&](int j) {                           // the 1 KB piece j of the values
+        u32x4 v = ld16(sv + j * 1024);
+        if (part) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            v[w] &= BITS == 8 ? keep[w & 1][0] : keep[w / 2][w & 1];
+            const uint32_t z = odd_parts<BITS, kPv>(v[w]);
+            any |= z;
+            v[w] &= ~z;
+          }
+        }
+        return v;
+      };
+      if constexpr (kByTile) {
+        const bool two = __any(low);
+        u32x4 p_lo[C];
+        if (two) {
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              p_lo[c][w] = pack16<kPv>((s[c][w / 2][2 * (w & 1)] - val16(p_hi[c][w] & 0xFFFFu, kPv)) * kLow,
+                                       (s[c][w / 2][2 * (w & 1) + 1] - val16(p_hi[c][w] >> 16, kPv)) * kLow);
+        }
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          const u32x4 v = values(j);
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+            f32x4 hi = mma<kPv>(v, p_hi[c], zero);
+            if (two) {
+              const f32x4 lo = mma<kPv>(v, p_lo[c], zero);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) hi[e] = fabsf(hi[e]) < INFINITY ? fmaf(lo[e], 1.0f / kLow, hi[e]) : hi[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][j][e] = fmaf(share[c], hi[e], o[c][j][e]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2 * kLoads; ++j) {
+          const u32x4 v = values(j);
+          if constexpr (BITS == 16) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c][j] = mma<kPv>(v, p_hi[c], o[c][j]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const u32x4 w = widen8<kPv>(v[2 * e], v[2 * e + 1]);
+#pragma unroll
+              for (int c = 0; c < C; ++c) {
+                o[c][2 * j + e] = mma<kPv>(w, p_hi[c], o[c][2 * j + e]);
+                if constexpr (kTwo) o[c][2 * j + e] = mma<kPv>(w, p_two[c], o[c][2 * j + e]);
+              }
+            }
+          }
+        }
+      }
+      if constexpr (BITS == 16 && !CAREFUL) {
+        if (part && __any(any != 0u)) *again = 1;
+      } else if (part && __any(any != 0u)) {
+        // one by one, to the columns that see them
+        const uint8_t* vm = lds + stage * stage_bytes<BITS, D>() + 2 * kLoads * 1024;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          for (int i = 0; i < kTile; ++i) {
+            const int at = 4 * (i / 16) + i % 4;                   // token i's bit in lanes 16 (i / 4 mod 4) ..
+            const bool none = CAREFUL && !(__shfl(static_cast<int>(some[c]), 16 * (i / 4 % 4) + col) >> at & 1);
+            const uint32_t on = static_cast<uint32_t>(__shfl(static_cast<int>(seen[c]), col)) >> i & 1u;   // (bits of lane group 0: all)
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int place = 16 * (16 * (i / 4 % 4) + 4 * lg + e);
+                float y = 0.0f;
+                if constexpr (BITS == 16) {
+                  const uint32_t b = *reinterpret_cast<const any_u16*>(vm + j * 1024 + place + 2 * (4 * (i / 16) + i % 4));
+                  if (odd_parts<16, kPv>(b) & 0xFFFFu) y = val16(b, kPv);
+                } else {
+                  const uint32_t b = vm[(j / 2) * 1024 + place + 8 * (j & 1) + 4 * (i / 16) + i % 4];
+                  if ((b & 0x7Fu) == 0x7Fu) y = __builtin_nanf("");
+                }
+                if (on && y != 0.0f) o[c][j][e] += none ? __builtin_nanf("") : y;
+              }
+          }
+        }
+      }
     }
-    if (BITS == 8 || all_lo == INT32_MAX) break;
+    t = t1;
+    t1 = t2;
+    stage = stage + 1 < kStages ? stage + 1 : 0;
+  }
+  if constexpr (BITS == 16 && !CAREFUL) {                        // (an 8-bit NaN gives one, however often it is added)
     bool bad = false;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      bad |= fabsf(m[c]) >= kFar && m[c] > kNoMax;
+      f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};                      // 0, NaN where an output is no number
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= !(fabsf(o[c][j][e]) < INFINITY);
+        for (int e = 0; e < 4; ++e) sum[e] = fmaf(o[c][j][e], 0.0f, sum[e]);
+      bad |= !(sum[0] + sum[1] + sum[2] + sum[3] == 0.0f) || (fabsf(m[c]) >= kFar && m[c] > kNoMax);
     }
-    __syncthreads();                                             // the last stage is read
-    if (__any(bad)) lds[wave] = 1u;
-    else lds[wave] = 0u;
-    __syncthreads();
-    if ((lds[0] | lds[1] | lds[2] | lds[3]) == 0u) break;        // (of all four: they share the tiles)
-    all_lo = INT32_MAX;                                          // all tiles as if seen in part
-    __syncthreads();                                             // the votes are read
+    if (__any(bad)) *again = 1;
+    __syncthreads();                                             // (and the last stage is read)
+    if (*again != 0) return false;                               // (one wave is enough: they share the tiles)
   }
-  if (!busy) return;
+  if (!busy) return true;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     float sum = l[c];
@@ -1094,6 +1107,7 @@ __device__ __forceinline__ void attend_tiles(const RowsArgs& a, uint8_t* lds, co
       }
     }
   }
+  return true;
 }
 
 // Workgroups of k_attn_tiles on a CU, by its registers (fp16 caches: more of them)
@@ -1106,9 +1120,16 @@ constexpr int tiles_resident(int act, int bits, int D) {
 template <int ACT, int BITS, int D, int C>
 __global__ __launch_bounds__(256, tiles_resident(ACT, BITS, D)) void k_attn_tiles(RowsArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * stage_bytes<BITS, D>()];
+  __shared__ int again;
   Item it;
   Part p;
-  if (split_of(a, 64 * C, lane_id(), &it, &p)) attend_tiles<ACT, BITS, D, C>(a, lds, it, p.begin, p.end, p.whole, p.slot);
+  again = 0;
+  wait_lds<0>();                                                 // (a barrier of the first tile before any other write)
+  if (!split_of(a, 64 * C, lane_id(), &it, &p)) return;
+  const bool done = attend_tiles<ACT, BITS, D, C, false>(a, lds, &again, it, p.begin, p.end, p.whole, p.slot);
+  if constexpr (BITS == 16) {
+    if (!done) attend_tiles<ACT, BITS, D, C, true>(a, lds, &again, it, p.begin, p.end, p.whole, p.slot);
+  }
 }
 
 // Joins the parts of 4 `per` columns of an item, `per` a wave, in a fixed order (lanes
@@ -1150,7 +1171,7 @@ __global__ __launch_bounds__(256) void k_rows_join(RowsArgs a, int cols, int per
 #pragma unroll 4
     for (int s = sub; s < n; s += kAtOnce) {
       const int64_t y = at + static_cast<int64_t>(s) * cols;
-      const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * y] - mx);
+      const float f = fmaxf(__builtin_amdgcn_exp2f(a.part_ml[2 * y] - mx), kLeast);
       sum = fmaf(f, a.part_ml[2 * y + 1], sum);
       if (d < D) {
         const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + y * D + d);
