@@ -1203,11 +1203,12 @@ hipError_t launch_d(const RowsArgs& a, const RowsPlan& p, hipStream_t st) {
   if (grid >= (1 << 23) || p.items * a.kv.n_kv_heads >= (1 << 23)) return hipErrorInvalidConfiguration;
   const uint32_t n = static_cast<uint32_t>(grid);
   constexpr int kThreads = 64 * kRowsWaves;
+  constexpr int kTwo = BITS == 16 ? 2 : 1;                       // (8-bit caches have one column tile: rows_plan)
   if (p.many) k_attn_tiles<ACT, BITS, D, kTileCols><<<n, 256, 0, st>>>(a);
   else if (p.col_tiles == 1 && p.n_shares) k_attn_rows<ACT, BITS, D, 1, true><<<n, kThreads, 0, st>>>(a);
   else if (p.col_tiles == 1) k_attn_rows<ACT, BITS, D, 1, false><<<n, kThreads, 0, st>>>(a);
-  else if (p.n_shares) k_attn_rows<ACT, BITS, D, 2, true><<<n, kThreads, 0, st>>>(a);
-  else k_attn_rows<ACT, BITS, D, 2, false><<<n, kThreads, 0, st>>>(a);
+  else if (p.n_shares) k_attn_rows<ACT, BITS, D, kTwo, true><<<n, kThreads, 0, st>>>(a);
+  else k_attn_rows<ACT, BITS, D, kTwo, false><<<n, kThreads, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 0) return e;
   const int cols = (p.many ? 64 : 16) * p.col_tiles;
