@@ -31,6 +31,12 @@ def _need(ok: bool, what: str):
         raise ValueError(what)
 
 
+def _int32(x: int, name: str):
+    """A foreign-function call would cut a larger one down to its last 32 bits."""
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError("%s must fit 32 bits: %d" % (name, x))
+
+
 def _ptr(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.data_ptr()
 
@@ -230,6 +236,7 @@ def norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional[
     those of ``out``, which may be q and k themselves (pw_heads_norm_rotate)."""
     T, n, D = q.shape
     act, dev = q.dtype, q.get_device()
+    _int32(offset, "offset")
     _need((act is torch.bfloat16 or act is torch.float16) and dev >= 0, "q must be 16-bit heads on the device")
     rot, pos = _turned(rotation, positions, T, dev)
     q_ptr, n_q, ldq, ldqh = _rows(q, T, D, act, dev, "q")
@@ -298,6 +305,8 @@ class KVCache:
         ``window`` of them) -> [B, heads, head_dim] (pw_attn_decode)."""
         B, heads, D = q.shape
         dev = self.dev
+        _int32(max_len, "max_len")
+        _int32(window, "window")
         ldq, ldqh, inner = q.stride()
         if B <= 1:                         # a single sequence, or head, may have any stride
             ldq = 0
@@ -329,6 +338,7 @@ class KVCache:
         written to the slots as ``append`` does: q in a new tensor or in ``q_out``,
         which may be q itself (pw_kv_append_rotated)."""
         T, D, dev, act = k.shape[0], self.head_dim, self.dev, self.act
+        _int32(offset, "offset")
         k_ptr, n_k, ld, ldh = _rows(k, T, D, act, dev, "k")
         v_ptr, n_v, ldv, ldvh = _rows(v, T, D, act, dev, "v")
         _need(n_k == self.kv_heads and n_v == n_k and ld == ldv and ldh == ldvh,
@@ -349,6 +359,7 @@ class KVCache:
     def _table(self, block_table: torch.Tensor, B: int, max_len: int):
         """(address, row stride) of a block table."""
         rows, blocks = block_table.shape
+        _int32(max_len, "max_len")
         _need(block_table.dtype is torch.int32 and rows == B and block_table.get_device() == self.dev
               and (block_table.stride(1) == 1 or blocks <= 1), "block_table must be [B, blocks] int32 on the cache's device")
         _need(blocks * self.block_tokens >= max_len, "the block table is shorter than max_len")
@@ -365,6 +376,7 @@ class KVCache:
         (pw_attn_rows)."""
         T, heads, D = q.shape
         dev, B = self.dev, lens.shape[0]
+        _int32(window, "window")
         q_ptr, _, ldq, ldqh = _rows(q, T, self.head_dim, self.act, dev, "q")
         _packed(starts, (B + 1,), torch.int32, dev, "starts")
         _packed(lens, (B,), torch.int32, dev, "lens")
