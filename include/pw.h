@@ -690,7 +690,8 @@ pw_status pw_attn_decode(const pw_kv_cache* cache, const void* q, int64_t ldq, i
 
 /* Position rotation: of each head the first `dims` channels turn in pairs, pair i
  * by the angle position * inv_freq[i] (radians; both and their product in 64 bits,
- * reduced to a part of a turn before they leave them), times the amplitude:
+ * reduced to a part of a turn before they leave them; an angle of 2^51 and more is any
+ * angle), times the amplitude:
  *   (x, y) -> amplitude (x cos - y sin, x sin + y cos).
  * Channels past `dims` stay. A NULL rotation, or one of 0 channels, turns none.
  * Constraints (PW_EINVAL otherwise): dims >= 0, a multiple of 16, at most the head's

@@ -26,7 +26,9 @@ namespace {
 // append took 34.6 us, with this 29.1.)
 __device__ __forceinline__ void angle_of(const Rotate& r, double quarters, double freq, float* co, float* si) {
   const double t = fma(quarters, freq, 6755399441055744.0), n = t - 6755399441055744.0;
-  const float z = static_cast<float>(fma(quarters, freq, -n)) * 1.57079632679489662f, y = z * z;
+  // (past 2^51 quarters, where 64 bits no longer tell them, the rest is kept within its range)
+  const float part = __builtin_amdgcn_fmed3f(static_cast<float>(fma(quarters, freq, -n)), -0.5f, 0.5f);
+  const float z = part * 1.57079632679489662f, y = z * z;
   float s = fmaf(y, 2.7557319224e-6f, -1.98412698413e-4f);
   s = fmaf(fmaf(fmaf(y, s, 8.33333333333e-3f), y, -0.166666666667f), y * z, z);
   float c = fmaf(y, 2.48015873016e-5f, -1.38888888889e-3f);
