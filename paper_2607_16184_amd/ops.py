@@ -10,8 +10,9 @@ Work goes to the current stream, or to ``stream``: what this module allocates
 then belongs to that stream; the caller orders it after whatever wrote the
 inputs, and keeps them until it is done. A handle may be used on several
 streams; graphs that were captured on one stream share its workspace and are
-replayed one after the other. A call's tensors and its stream belong to one
-device, which need not be the current one.
+replayed one after the other. That holds for all handles together that are given
+one :class:`Workspace`, as the caches of a model's layers may be. A call's tensors
+and its stream belong to one device, which need not be the current one.
 """
 from __future__ import annotations
 
@@ -72,16 +73,16 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-class _Workspace:
-    """The device buffers of one handle, one for each stream that it is used on,
-    grown to what the calls need: a call is made with the buffer at hand, and
-    where that is too small (PW_ENOMEM, nothing launched) again with a larger
-    one. Sizes are powers of two and an outgrown buffer is kept, since a
-    captured graph may hold its address: together they are smaller than the
-    last one."""
+class Workspace:
+    """The device buffers of one handle, or of several that are used one after the
+    other on a stream: one buffer for each stream, grown to what the calls need. A
+    call is made with the buffer at hand, and where that is too small (PW_ENOMEM,
+    nothing launched) again with a larger one. Sizes are powers of two and an
+    outgrown buffer is kept, since a captured graph may hold its address: together
+    they are smaller than the last one."""
 
-    def __init__(self, device):
-        self.device, self.of, self.kept = device, {}, []
+    def __init__(self, device="cuda"):
+        self.device, self.of, self.kept = torch.empty(0, device=device).device, {}, []
 
     def run(self, dev: int, stream, fn, args, need):
         st = _on(dev, stream)
@@ -164,7 +165,7 @@ class Linear8:
               self.packed.data_ptr(), _on(dev, stream))
         if stream is not None:
             w8.record_stream(stream)       # the caller may drop it before the packing has run
-        self._ws = _Workspace(w8.device)
+        self._ws = Workspace(w8.device)
 
     def forward(self, x8: torch.Tensor, x_scale: torch.Tensor, out: torch.Tensor = None, dtype=torch.bfloat16,
                 stream=None) -> torch.Tensor:
@@ -263,10 +264,14 @@ class KVCache:
     """Paged keys and values of one attention layer: n_blocks blocks of
     block_tokens tokens, in ``act`` or (fp8) as e4m3 codes with a scale per
     token and head. ``pool``: a uint8 device tensor to keep the blocks in (e.g.
-    one that also holds weight pages), block i at byte i * block_stride."""
+    one that also holds weight pages), block i at byte i * block_stride.
+    ``workspace``: one that other caches have, too. The parts of split sequences
+    lie there, hundreds of MB for large batches of long ones (16 trees of 60
+    tokens after up to 32768: 392 MB, kept as 512): a model's layers, which run
+    one after the other, need them once."""
 
     def __init__(self, n_blocks: int, block_tokens: int, kv_heads: int, head_dim: int, act: torch.dtype, fp8: bool = False,
-                 pool: torch.Tensor = None, block_stride: int = None, device="cuda"):
+                 pool: torch.Tensor = None, block_stride: int = None, device="cuda", workspace: Workspace = None):
         _need(act in (torch.float16, torch.bfloat16), "act must be a 16-bit type")
         self.act, self.head_dim, self.kv_heads, self.block_tokens = act, head_dim, kv_heads, block_tokens
         self.desc = pw.pw_kv_cache(None, 0, n_blocks, block_tokens, kv_heads, head_dim, _TYPE[act], 8 if fp8 else 16)
@@ -279,7 +284,8 @@ class KVCache:
         _need(pool.numel() >= (n_blocks - 1) * self.desc.block_stride + self.block_bytes, "the pool is smaller than its blocks")
         self.pool = pool
         self.desc.pool = pool.data_ptr()
-        self._ws = _Workspace(pool.device)
+        _need(workspace is None or workspace.device == pool.device, "the workspace lies on another device")
+        self._ws = workspace or Workspace(pool.device)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None):
         """Write k, v [T, kv_heads, head_dim] to the slots [T] int64 (block *
