@@ -747,18 +747,21 @@ pw_status pw_kv_append_rotated(const pw_kv_cache* cache, const pw_rotation* rot,
  *   sequence's new tokens those j whose bit j mod 64 of word j / 64 of its mask is
  *   set (its own only if that bit is; bits from n on are not looked at, tokens
  *   past the words are not seen); window > 0: of the context the last window - m
- *   positions, m the bits set.
+ *   positions, m the bits set (a path of more than `window` tokens is seen whole,
+ *   where tokens decoded one by one would see its end: clear the bits before it).
  *   q, out and lse [T, n_q_heads]; q's strides, scale, head sharing, block_table,
  *   max_len and lse otherwise as in pw_attn_decode; positions from max_len on, or
  *   below 0, do not exist.
  * starts [B+1] int32 device, not decreasing, within 0 .. T: rows that no sequence
  * has are not written. Rows that see nothing give zeros and an lse of -infinity.
  * What lies in the cache at positions that a row does not see is not used for it,
- * NaN and infinities included. Scores, exponentials and sums are in fp32; weights
+ * NaN and infinities included; an infinite value that it sees is infinite in its
+ * output, however small the weight. Scores, exponentials and sums are in fp32; weights
  * enter the product with the values as in pw_attn_decode where T * (n_q_heads /
  * n_kv_heads) <= 64 B, and in 8-bit caches with act PW_F16; above that rounded once to
  * act: to bf16, off by at most 2^-8 of themselves, or to fp16, by at most 2^-11 and
- * 2^-52 of the row's largest weight.
+ * 2^-52 of the row's largest weight. T and B are the whole call's: the same rows may
+ * come out otherwise, within these bounds, beside other sequences.
  * Constraints: B, T >= 0; n_q_heads a multiple of n_kv_heads; 1 <= words <= 1024;
  * 0 <= max_len < 2^31 - 256; window >= 0; scale finite (PW_EINVAL otherwise); B <
  * 65536, T * n_q_heads < 2^23, min(B, T) * n_kv_heads < 2^21 (PW_EUNSUPPORTED: split

@@ -19,7 +19,7 @@ namespace {
 //     Bound by the cache's bytes and, with 32 columns or fp16, by vector instructions:
 //     64 ragged trees of up to 16 tokens, contexts to 4096, 8 key heads x 4, heads of
 //     128 in 16 bits (509 MB) 135 us, in 8 bits (267 MB) 115; heads of 64 in fp16,
-//     window 1500 (156 MB), 45; 8 tokens after 300 (one sequence) 9.0, a chain of
+//     window 1500 (156 MB), 45; 8 tokens after 300 (one sequence) 9.1, a chain of
 //     starts, table, tiles and the join of the waves. 64 columns a wave were slower
 //     everywhere (the first 176 us, the second 186): their registers leave one wave
 //     per SIMD, and groups are rarely full.
@@ -701,8 +701,8 @@ __global__ __launch_bounds__(64 * kRowsWaves, rows_resident(BITS, D, C)) void k_
 // them in: 1 KB per instruction, without bank conflicts.
 // The matrix unit is the bound (busy 382 us of 4096 rows after 12288 tokens, 8 key
 // heads x 4 of 128 in bf16, 0.96 TFLOP), with about as much time of vector
-// instructions (exponentials, maxima, roundings) and of LDS reads beside it: 900 us,
-// 1.07 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches 1.27.
+// instructions (exponentials, maxima, roundings) and of LDS reads beside it: 910 us,
+// 1.06 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches 1.27.
 // What counts is waves per SIMD that are at another of the three: C = 2 has 168
 // registers and three waves, 1155 us (24 sequences of 1152 rows after 2048 tokens); with
 // two waves 1360; C = 3 with two waves 1194; C = 4 spills with two waves (3029) and has
@@ -721,7 +721,9 @@ __global__ __launch_bounds__(64 * kRowsWaves, rows_resident(BITS, D, C)) void k_
 // the scale comes first, keeps nothing, and from some 2^24 on that is a factor past fp16's
 // end. So a workgroup with a column whose maximum reaches kFar (the factor then being at
 // most 2^(1/2048)) goes through its tiles once more, the scale first in all of them; and so
-// does one with outputs that are not all numbers.
+// does one with outputs that are not all numbers. (Asking costs 24 sequences of 1152 rows 1
+// per cent, in fp16 2. One form for both, with a flag, cost 500 rows beside 31 single ones
+// 81 us where this takes 79; a branch for large scores in every tile 15 us of 900.)
 constexpr float kFar = 16384.0f;
 
 constexpr int kStages = 3;
