@@ -1003,10 +1003,14 @@ hipError_t append_runs(const HeadsArgs& t, hipStream_t st) {
 
 }  // namespace
 
-// By runs where pw_kv_append goes by them, and a pair lies in one lane there.
+// By runs, where a pair lies in one lane there: from 16384 tokens x heads on. By runs each
+// key head has the angles of its tokens for itself, so in 16 bits that is later than in
+// pw_kv_append. 32 query and 8 key heads of 128 in bf16, consecutive positions, by runs
+// and by tokens (us): 16 bits 768 tokens 18.9 and 13.4, 1536 tokens 22.5
+// and 19.8; 2304 tokens 25.3 and 31.3, 4001 29.8 and 40.4; 8 bits 2304 tokens 26.9 and 27.5,
+// 4001 31.0 and 33.2. Slots in no order: 16 bits 768 tokens 25.7 and 13.5.
 bool append_by_runs(const HeadsArgs& a) {
-  return a.T >= kAppendMany && static_cast<int64_t>(a.T) * a.n_k >= (a.kv.bits == 16 ? kRunItems16 : kRunItems8) &&
-         (a.rot.interleaved || a.rot.R % 64 == 0);
+  return a.T >= kAppendMany && static_cast<int64_t>(a.T) * a.n_k >= kRunItems8 && (a.rot.interleaved || a.rot.R % 64 == 0);
 }
 
 hipError_t launch_append_runs(const HeadsArgs& a, hipStream_t st) {

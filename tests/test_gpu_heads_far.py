@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("freq", [2.0 ** 16, 1e6, 3.7e8, 1e13, 1e100])
 @pytest.mark.parametrize("act", [BF, FP])
 @pytest.mark.parametrize("inter", [False, True])
-@pytest.mark.parametrize("T", [5, 1100])
+@pytest.mark.parametrize("T", [5, 2100])
 def test_angles_past_64_bits(freq, act, inter, T):
     """An angle in 64 bits is off by 2^-53 of itself, so from 2^53 radians on nothing is
     known of it; sines and cosines stay within 1 all the same, and a pair's values
